@@ -14,6 +14,10 @@
  *     of §4.1, as a reverse scan over packed trajectories;
  *   - sao_value_loss             : the value error (V - R)^2 (Preliminaries)
  *     and the explained-variance sums of §4.4.
+ * Beside them, auxiliary losses of the same training step:
+ *   - sao_distill_loss_fwd/bwd   : distillation from a teacher's top logits
+ *     over the LM head;
+ *   - sao_balance_loss_fwd/bwd   : load balance of a mixture of experts.
  *
  * Conventions shared by every entry point:
  *   - Every array argument is a DEVICE pointer owned by the caller; the
@@ -81,6 +85,8 @@ typedef enum sao_dtype {
 #define SAO_DEVERR_SCAN_TIMEOUT 0x4u /* advantage scan gave up waiting for a carry */
 #define SAO_DEVERR_PIPE_TIMEOUT 0x8u /* a GEMM pipeline wait gave up */
 #define SAO_DEVERR_CACHE_ROW 0x10u   /* cached backward: a row with grad != 0 the forward skipped */
+#define SAO_DEVERR_TOP_ID 0x20u      /* a teacher's entry with an id >= V, or one id twice in a row */
+#define SAO_DEVERR_EXPERT_ID 0x40u   /* some expert id >= E */
 
 /* Library version, major * 10000 + minor * 100 + patch. */
 SAO_API int sao_version(void);
@@ -426,6 +432,116 @@ SAO_API sao_status sao_policy_loss_bwd(const float *logp, const float *old_logp,
 SAO_API sao_status sao_value_loss(const float *values, const float *ret, const uint8_t *loss_mask,
                           int64_t N, int64_t n_norm, float *loss, float *grad_values, double *ev_sums,
                           void *ws, size_t ws_bytes, sao_stream_t stream);
+
+/* Most entries a row that sao_distill_loss_fwd/bwd take. */
+#define SAO_DISTILL_MAX_K 1024
+
+/*
+ * Distillation from a teacher's top logits over the LM head (an auxiliary loss
+ * beside the RL objective; the paper has no counterpart). Row t of the student
+ * has logits z_v = H_t . W_v / T over the vocabulary; the teacher gives K
+ * entries a row, ids with logits, of which those with a negative id are none
+ * (a row that the teacher answered with fewer). With a_k = top_logits / T:
+ *   la   = log sum_k e^a_k (teacher_lse NULL: the entries are renormalised), or
+ *          teacher_lse[t] = the teacher's log sum e^(logit / T) over its whole
+ *          vocabulary, whose mass outside the entries is then one more outcome:
+ *   p_k  = e^(a_k - la),  rho = max(0, 1 - sum_k p_k)  (renormalised: 0)
+ *   loss[t] = sum_k p_k (a_k - la - z_k + lse) + rho (log rho - (lse_rest - lse))
+ * the Kullback-Leibler divergence from the teacher's distribution to the
+ * student's, with lse over all columns and lse_rest over those without an entry
+ * (-inf, and rho = 0, where the entries are the whole vocabulary). Not scaled by
+ * T^2. The [N, V] logits are never stored.
+ *   H [N, h], W [V, h] dt      top_ids [N, K] int32 in any order, each below V and
+ *                              at most once a row
+ *   top_logits [N, K] top_dt   teacher_lse [N] fp32 or NULL
+ *   row_mask [N] uint8 or NULL: rows with 0 are not computed, loss = lse = 0
+ *   loss, lse, lse_rest [N] fp32, z_top [N, K] fp32 (the entries' z_k, 0 where
+ *   there is none): outputs; the last three go to the backward
+ * Sizes as sao_token_logprobs_fwd, and 1 <= K <= SAO_DISTILL_MAX_K; T > 0.
+ * A row without an entry, or renormalised without one of a logit above -inf, has
+ * loss 0 and no gradient. A row with an id out of range or there twice has loss
+ * NaN (and SAO_DEVERR_TOP_ID). lse_rest is NaN on the rows that take no gradient:
+ * masked ones, and those whose loss is not finite or has nothing to learn from.
+ * bf16 logits are added up in fp32 every 256 elements of h (the tensor cores'
+ * own sums truncate): lse within 3e-7 of itself at h = 2,048.
+ * The workspace of both calls: sao_distill_workspace_bytes.
+ */
+SAO_API size_t sao_distill_workspace_bytes(int64_t N, int32_t h, int32_t V, int32_t K, sao_dtype dt);
+SAO_API sao_status sao_distill_loss_fwd(const void *H, const void *W, sao_dtype dt, const int32_t *top_ids,
+                                        const void *top_logits, sao_dtype top_dt, const float *teacher_lse,
+                                        const uint8_t *row_mask, int64_t N, int32_t h, int32_t V, int32_t K,
+                                        float temperature, float *loss, float *lse, float *lse_rest, float *z_top,
+                                        void *ws, size_t ws_bytes, sao_stream_t stream);
+
+/*
+ * Gradient of sum_t grad_loss[t] * loss[t]: with q = e^(z - lse),
+ *   dz_k = q_k - p_k at the entries, dz_v = e^(z_v - lse_rest) (e^(lse_rest - lse)
+ *   - rho) elsewhere, dZ = grad_loss dz / T, dH = dZ W, dW = dZ^T H.
+ *   lse, lse_rest, z_top  from the forward on the same inputs
+ *   grad_loss [N] fp32    rows with 0 contribute nothing
+ *   dH [N, h] dt          overwritten (zeros on rows without a gradient)
+ *   dW [V, h] dw_dt       SAO_F32, overwritten or (accumulate_dW != 0) added to,
+ *                         so that it adds to another loss's dW; or for a bf16 head
+ *                         SAO_BF16, overwritten only (a sum over calls needs fp32)
+ * For a bf16 head dZ is rounded to bf16 once before the two products (as in
+ * sao_token_logprobs_bwd): 2^-9 of each of its elements.
+ */
+SAO_API sao_status sao_distill_loss_bwd(const void *H, const void *W, sao_dtype dt, const int32_t *top_ids,
+                                        const void *top_logits, sao_dtype top_dt, const float *teacher_lse,
+                                        const float *lse, const float *lse_rest, const float *z_top,
+                                        const float *grad_loss, int64_t N, int32_t h, int32_t V, int32_t K,
+                                        float temperature, void *dH, void *dW, sao_dtype dw_dt, int accumulate_dW,
+                                        void *ws, size_t ws_bytes, sao_stream_t stream);
+
+/* How sao_balance_loss_fwd/bwd turn a token's E router logits into probabilities. */
+#define SAO_SCORE_SOFTMAX 0 /* s_e = softmax(x)_e */
+#define SAO_SCORE_SIGMOID 1 /* s_e = sigmoid(x_e) / sum_j sigmoid(x_j) */
+
+/* Most experts that sao_balance_loss_fwd/bwd take. */
+#define SAO_BALANCE_MAX_EXPERTS 1024
+
+/*
+ * Load-balance loss of a mixture-of-experts router, with per-expert counts (an
+ * auxiliary loss beside the RL objective; the paper has no counterpart). Over the
+ * n counted rows of a segment, with the k experts that each token was sent to:
+ *   counts_e = how often expert e was chosen, prob_sums_e = sum_t s_te,
+ *   loss = E / (k n^2) sum_e counts_e prob_sums_e        (1 when both are even)
+ * cu_seqlens NULL: one segment, the batch (B is taken as 1). Otherwise each of
+ * the B packed trajectories is balanced by itself and the loss is the mean over
+ * those with a counted row (0 without any).
+ *   logits [N, E] dt           expert_ids [N, k] int32; negative: no expert (a
+ *                              dropped choice), E or more: none either (and
+ *                              SAO_DEVERR_EXPERT_ID)
+ *   row_mask [N] uint8 or NULL: rows with 0 are not counted
+ *   cu_seqlens [B + 1] int32 or NULL, as for sao_advantages
+ *   loss [1] fp32, counts [B, E] int64, prob_sums [B, E] fp32, rows [B] int64
+ *   (the counted rows): outputs. The loss is a function of the last three, so
+ *   data-parallel ranks that balance their joint batch (cu_seqlens NULL) add
+ *   those up before the backward and form the loss from the sums.
+ * A row of logits that are all -inf has no probabilities and no gradient.
+ * Deterministic. 1 <= k <= E <= SAO_BALANCE_MAX_EXPERTS. Workspace of
+ * the forward: sao_balance_workspace_bytes(N, E, B); the backward needs the error
+ * word's 256 bytes only.
+ */
+SAO_API size_t sao_balance_workspace_bytes(int64_t N, int32_t E, int32_t B);
+SAO_API sao_status sao_balance_loss_fwd(const void *logits, sao_dtype dt, const int32_t *expert_ids,
+                                        const uint8_t *row_mask, const int32_t *cu_seqlens, int32_t B, int64_t N,
+                                        int32_t E, int32_t k, int score, float *loss, int64_t *counts,
+                                        float *prob_sums, int64_t *rows, void *ws, size_t ws_bytes,
+                                        sao_stream_t stream);
+
+/*
+ * grad_logits = grad_loss[0] * d loss / d logits (counts are not differentiated):
+ * with w_e = grad_loss E counts_e / (k n^2 segments), d x_te = s_te (w_e -
+ * sum_j s_tj w_j), times 1 - sigmoid(x_te) for SAO_SCORE_SIGMOID; 0 on rows that
+ * are not counted. counts and rows are the forward's, or sums of several ranks'.
+ *   grad_logits [N, E] dt, overwritten; grad_loss is a device scalar
+ */
+SAO_API sao_status sao_balance_loss_bwd(const void *logits, sao_dtype dt, const uint8_t *row_mask,
+                                        const int32_t *cu_seqlens, int32_t B, int64_t N, int32_t E, int32_t k,
+                                        int score, const int64_t *counts, const int64_t *rows,
+                                        const float *grad_loss, void *grad_logits, void *ws, size_t ws_bytes,
+                                        sao_stream_t stream);
 
 /*
  * Kernel timing for profiling. When enabled, every kernel the library

@@ -36,6 +36,13 @@ Optimization for Agentic Reinforcement Learning" (arxiv 2607.07508):
                           policy, weighted by the old/rollout ratio, with a
                           double-sided mask on that weight
 
+and, of the auxiliary losses beside the paper's objective,
+
+* ``distill_loss``        distillation from a teacher's top logits: the
+                          Kullback-Leibler divergence over the entries and the
+                          rest of the vocabulary as one outcome
+* ``balance_loss``        load balance of a mixture of experts
+
 Readings taken where the paper is silent or ambiguous (each one is listed with
 its reason in the design notes):
 
@@ -574,3 +581,113 @@ def decoupled_loss(logp, prox_logp, rollout_logp, adv, loss_mask, eps_low: float
                        int((flags == FLAG_NONFINITE).sum()), int((flags == MIS_LOW).sum()),
                        int((flags == MIS_HIGH).sum())], np.int64)
     return {"loss": loss, "coef": coef, "flags": flags, "counts": counts}
+
+
+# ---------------------------------------------------------------------------
+# Auxiliary losses: distillation from a teacher's top logits, expert balance
+# ---------------------------------------------------------------------------
+
+def distill_loss(H, W, top_ids, top_logits, temperature: float, teacher_lse=None, row_mask=None,
+                 grad=None) -> Dict[str, np.ndarray]:
+    """Row by row: KL(teacher || student) between the distributions over the
+    teacher's entries S (ids >= 0) and the vocabulary outside S as one outcome.
+    teacher_lse None: the teacher is renormalised over S and gives the rest no
+    mass; otherwise log sum exp(logit / T) over the teacher's vocabulary, whose
+    mass outside S is max(0, 1 - sum p) (0 when S is the whole vocabulary).
+    Returns loss, lse, lse_rest, z_top and, for d sum(grad * loss), dH and dW.
+    Masked rows: loss = lse = 0; without anything to learn from: loss 0. Rows
+    with an id out of range or twice: loss NaN. None of these has a gradient,
+    nor has a row whose loss is not finite; their lse_rest is NaN."""
+    Hd, Wd = _f64(H), _f64(W)
+    N, V = Hd.shape[0], Wd.shape[0]
+    ids = np.asarray(top_ids)
+    a_all = _f64(top_logits) / temperature
+    out = {"loss": np.zeros(N), "lse": np.zeros(N), "lse_rest": np.full(N, np.nan),
+           "z_top": np.zeros(ids.shape), "dH": np.zeros_like(Hd), "dW": np.zeros_like(Wd)}
+    with np.errstate(all="ignore"):
+        for t in range(N):
+            if row_mask is not None and row_mask[t] == 0:
+                continue
+            z = Wd @ Hd[t] / temperature
+            m = z.max()
+            lse = m + np.log(np.exp(z - m).sum())
+            out["lse"][t] = lse
+            slots = np.flatnonzero(ids[t] >= 0)
+            S = ids[t][slots]
+            if len(np.unique(S)) != len(S) or (S >= V).any():
+                out["loss"][t] = np.nan
+                continue
+            zk, a = z[S], a_all[t][slots]
+            out["z_top"][t][slots] = zk
+            rest = np.ones(V, bool)
+            rest[S] = False
+            m_rest = z[rest].max() if rest.any() else 0.0
+            lse_rest = m_rest + np.log(np.exp(z[rest] - m_rest).sum()) if rest.any() else -np.inf
+            if teacher_lse is None:
+                if len(a) == 0 or a.max() == -np.inf:
+                    continue
+                la = a.max() + np.log(np.exp(a - a.max()).sum())
+            else:
+                la = float(teacher_lse[t])
+            p = np.exp(a - la)
+            rho = max(0.0, 1.0 - p.sum()) if teacher_lse is not None and rest.any() else 0.0
+            on = p != 0
+            loss = (p[on] * (a[on] - la - zk[on] + lse)).sum()
+            if rho > 0:
+                loss += rho * (np.log(rho) - (lse_rest - lse))
+            out["loss"][t] = loss
+            if not np.isfinite(loss):
+                continue
+            out["lse_rest"][t] = lse_rest
+            if grad is not None and grad[t] != 0:
+                dz = np.exp(z - lse_rest) * (np.exp(lse_rest - lse) - rho) if rest.any() else np.zeros(V)
+                dz[S] = np.exp(zk - lse) - p
+                dz *= float(grad[t]) / temperature
+                out["dH"][t] = dz @ Wd
+                out["dW"] += np.outer(dz, Hd[t])
+    return out
+
+
+def balance_loss(logits, expert_ids, score: str, row_mask=None, cu_seqlens=None) -> Dict[str, object]:
+    """E / (k n^2) sum_e counts_e P_e of each segment (the batch, or each packed
+    trajectory), P_e the sum of the tokens' probabilities over its n counted
+    rows, and the mean over the segments with n > 0. score "softmax" or
+    "sigmoid" (normalised over the experts). Counts are not differentiated;
+    ids outside [0, E) count for no expert; a row of -inf alone has no scores."""
+    x = _f64(logits)
+    ids = np.asarray(expert_ids)
+    N, E = x.shape
+    k = ids.shape[1]
+    keep = np.ones(N, bool) if row_mask is None else np.asarray(row_mask) != 0
+    cu = [0, N] if cu_seqlens is None else [int(c) for c in cu_seqlens]
+    B = len(cu) - 1
+    counts, sums, rows = np.zeros((B, E), np.int64), np.zeros((B, E)), np.zeros(B, np.int64)
+    s, slope = np.zeros((N, E)), np.zeros((N, E))
+    with np.errstate(all="ignore"):
+        for t in np.flatnonzero(keep):
+            # log sigmoid(x) up to a constant of the row: far below 0 the sigmoids themselves vanish
+            v = x[t] if score == "softmax" else np.minimum(x[t], 0.0) - np.log1p(np.exp(-np.abs(x[t])))
+            m = v.max()
+            if m == -np.inf:
+                continue
+            e = np.exp(v - m)
+            s[t] = e / e.sum()
+            slope[t] = s[t] if score == "softmax" else s[t] / (1.0 + np.exp(x[t]))
+    loss, used = 0.0, 0
+    w = np.zeros((N, E))
+    for b in range(B):
+        on = np.flatnonzero(keep[cu[b]:cu[b + 1]]) + cu[b]
+        rows[b] = n = len(on)
+        if n == 0:
+            continue
+        used += 1
+        chosen = ids[on]
+        chosen = chosen[(chosen >= 0) & (chosen < E)]
+        counts[b] = np.bincount(chosen, minlength=E)
+        sums[b] = s[on].sum(0)
+        f = counts[b] * (E / (k * float(n) ** 2))
+        loss += (f * sums[b]).sum()
+        w[on] = f
+    w /= max(used, 1)
+    d = slope * (w - (s * w).sum(1, keepdims=True))
+    return {"loss": loss / max(used, 1), "counts": counts, "sums": sums, "rows": rows, "dlogits": d, "s": s, "w": w}

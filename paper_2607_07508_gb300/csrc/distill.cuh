@@ -1,0 +1,105 @@
+// Distillation from a teacher's top logits: what the row kernels (distill.cu) and the
+// logit kernels of the two head types (logprobs_tc.cu, logprobs_f32.cu) share.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/sao.h"
+#include "logprobs_common.cuh"
+#include "rows.cuh"
+#include "sao_common.cuh"
+
+namespace sao {
+
+constexpr int kTopTile = 256;  // vocabulary columns that an offset of TopRef counts by
+
+// The teacher's entries of each row, sorted by token id, for the forward's epilogues:
+// they keep the student's logit of each entry and leave it out of their tile's
+// (max, sum). Row t has entries off[t][tiles], of which off[t][j] have ids below
+// 256 j.
+struct TopRef {
+  const int32_t *id;    // [N][K] ascending
+  const uint16_t *off;  // [N][tiles + 1]
+  float *z;             // [N][K] out, in the order of id
+  int K, tiles;
+  float inv_t;          // 1 / temperature
+};
+
+// The backward's view of the rows: dZ[t, v] = g[t] exp(z[t, v] / T - rest[t]) on the
+// columns outside the entries, dz_top[t][k] / T at id ids[t][k].
+struct TopGrad {
+  const uint8_t *mask;   // [N] rows with a gradient
+  const float *g, *rest; // [N]
+  const float *dz_top;   // [N][K]
+  const int32_t *ids;    // [N][K], the caller's order; < 0: no entry
+  int K;
+  float inv_t;
+};
+
+// A bf16 head of up to this many rows keeps its dZ as two bf16 pieces, the second one's
+// rows kFewRows after the first's in the same 128-row tile, with a copy of H's row, so
+// that both products take in 16 bits of dZ at no cost. With many rows the rounding of
+// dZ's elements averages out in dH and dW (1.4 times the error of rounding the outputs
+// alone); with one row a single entry may be most of dZ, and its rounding, up to 2^-9,
+// all of dW's error.
+constexpr int kFewRows = 64;
+
+// The rows with mask != 0 of up to kFewRows: rows p and kFewRows + p of Hc are that
+// token's, idx = -1 (and zeros) past the last one; count: rows of the products (0 or
+// kFewRows + the active ones).
+sao_status distill_few_rows(const uint8_t *mask, int64_t N, const __nv_bfloat16 *H, int32_t h, CompactRows *out,
+                            Carver &c, cudaStream_t s);
+// dH[t] = bf16(the sum of rows pos[t] and kFewRows + pos[t] over the parts), 0 where pos < 0.
+sao_status distill_few_dH(const float *acc, const DhParts &parts, int32_t h, const int *pos, const int *count,
+                          int64_t N, __nv_bfloat16 *dH, cudaStream_t s);
+
+// Writes dz_top into a chunk of dZ (vocabulary [v0, v0 + vc), rows in the order of
+// `idx`): one bf16 plane (`few`: the second pieces in the rows from kFewRows on), or the
+// three planes of the fp32 path, whose class word `range` then takes the magnitudes.
+sao_status patch_top_bf16(const TopGrad &t, const int *idx, const int *count, int64_t rows, bool few, int v0, int vc,
+                          __nv_bfloat16 *dz, int64_t ldz, cudaStream_t s);
+sao_status patch_top_f32(const TopGrad &t, const int *idx, const int *count, int64_t rows, int v0, int vc,
+                         __nv_bfloat16 *dz, int64_t ldz, int64_t plane, unsigned int *range, cudaStream_t s);
+
+// Merges the partials of the columns outside the entries and forms each row's loss.
+struct TopFinish {
+  const void *a;               // teacher logits [N][K]
+  sao_dtype adt;
+  const float *teacher_lse;    // [N] or null
+  const uint16_t *slot;        // [N][K] sorted position -> the caller's
+  const int32_t *entries;      // [N] entries, or -1 (an id out of range or there twice)
+  const uint8_t *row_mask;     // [N] or null
+  float *loss, *lse, *lse_rest, *z_top;
+  int V;
+};
+sao_status distill_finish(const TopRef &top, const TopFinish &f, const float2 *part, int nvt, const int *pos,
+                          int64_t N, cudaStream_t s);
+
+// logprobs_tc.cu / logprobs_f32.cu: the logits of a call and its backward, each on what
+// is left of the call's workspace.
+size_t tc_distill_fwd_bytes(int64_t N, int32_t h, int32_t V);
+size_t tc_distill_bwd_bytes(int64_t N, int32_t h, int32_t V);
+sao_status tc_distill_fwd(const void *H, const void *W, const uint8_t *row_mask, int64_t N, int32_t h, int32_t V,
+                          const TopRef &top, const TopFinish &f, unsigned int *err, Carver &c, cudaStream_t s);
+sao_status tc_distill_bwd(const void *H, const void *W, const TopGrad &t, int64_t N, int32_t h, int32_t V, void *dH,
+                          void *dW, sao_dtype dw_dt, int accumulate, unsigned int *err, Carver &c, cudaStream_t s);
+sao_status f32_distill_fwd(const float *H, const float *W, const uint8_t *row_mask, int64_t N, int32_t h, int32_t V,
+                           const TopRef &top, const TopFinish &f, unsigned int *err, Carver &c, cudaStream_t s);
+sao_status f32_distill_bwd(const float *H, const float *W, const TopGrad &t, int64_t N, int32_t h, int32_t V,
+                           float *dH, float *dW, int accumulate, unsigned int *err, Carver &c, cudaStream_t s);
+
+// distill.cu, called by the C entry points
+size_t distill_ws_bytes(int64_t N, int32_t h, int32_t V, int32_t K, sao_dtype dt);
+sao_status distill_fwd_launch(const void *H, const void *W, sao_dtype dt, const int32_t *ids, const void *a,
+                              sao_dtype adt, const float *teacher_lse, const uint8_t *row_mask, int64_t N, int32_t h,
+                              int32_t V, int32_t K, float temperature, float *loss, float *lse, float *lse_rest,
+                              float *z_top, unsigned int *err, void *ws, size_t ws_bytes, cudaStream_t s);
+sao_status distill_bwd_launch(const void *H, const void *W, sao_dtype dt, const int32_t *ids, const void *a,
+                              sao_dtype adt, const float *teacher_lse, const float *lse, const float *lse_rest,
+                              const float *z_top, const float *grad, int64_t N, int32_t h, int32_t V, int32_t K,
+                              float temperature, void *dH, void *dW, sao_dtype dw_dt, int accumulate,
+                              unsigned int *err, void *ws, size_t ws_bytes, cudaStream_t s);
+
+}  // namespace sao

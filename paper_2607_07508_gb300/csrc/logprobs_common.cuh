@@ -1,6 +1,7 @@
 // Pieces shared by the fp32 and tensor-core log-prob paths.
 #pragma once
 
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -70,6 +71,12 @@ __device__ __forceinline__ int dh_parts(const DhParts &d, int rows) {
 sao_status lse_merge_launch(const float2 *part, int nvt, const float *zy, const int32_t *y,
                             const uint8_t *row_mask, const int *pos, int64_t N, int32_t V, float *logp, float *lse,
                             unsigned int *err, cudaStream_t s);
+
+// 2-D bf16 tensor map over a row-major [outer][inner] array with row pitch
+// `pitch_elems`, box {box_inner (64 = 128 bytes), box_outer}, 128-byte swizzle,
+// zero fill outside the array.
+sao_status make_map(CUtensorMap *m, const void *ptr, uint64_t inner, uint64_t outer, uint64_t pitch_elems,
+                    uint32_t box_inner, uint32_t box_outer);
 
 size_t f32_ws_bytes(int64_t N, int32_t h, int32_t V);
 sao_status f32_fwd(const float *H, const float *W, const int32_t *y, const uint8_t *row_mask, int64_t N,

@@ -40,6 +40,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include "distill.cuh"
+#include "f32_planes.cuh"
 #include "logprobs_common.cuh"
 #include "per_device.h"
 #include "rows.cuh"
@@ -71,12 +73,16 @@ constexpr int HN = TN / 4;                   // columns per accumulating warp: f
 // first four warps hand theirs to the sixteen that hold 64 sums a thread.
 constexpr int LAUNCH_REGS = 96, ISSUE_REGS = 40, SUM_REGS = 104;
 static_assert(128 * ISSUE_REGS + 512 * SUM_REGS <= NUM_THREADS * LAUNCH_REGS, "split within the launch's registers");
-constexpr float CLASS_LIMIT[3] = {0x1p26f, 0x1p62f, 0x1p100f};
 constexpr unsigned SAFE_CLASSES = 2;  // 2^26 x 2^100, 2^62 x 2^62: products up to 2^126
 enum Operand : int { kOpH = 0, kOpW = 1, kOpDZ = 2, kOperands = 3 };
 constexpr int64_t MAX_ROWS = int64_t(65535) * 64;
 
-enum Kind : int { kLogits = 0, kDLogits = 1, kDH = 2, kDW = 3 };
+// kTopLogits, kTopDLogits: the two of a teacher's top logits (distill.cu)
+enum Kind : int { kLogits = 0, kDLogits = 1, kDH = 2, kDW = 3, kTopLogits = 4, kTopDLogits = 5 };
+template <int kKind>
+constexpr bool kFwdKind = kKind == kLogits || kKind == kTopLogits;
+template <int kKind>
+constexpr bool kDzKind = kKind == kDLogits || kKind == kTopDLogits;
 
 struct F32Params {
   int nM, nN, nK;     // tiles along M and N, 32-element steps along K
@@ -96,6 +102,8 @@ struct F32Params {
   int64_t part_ld;
   float *zy;
   const float *lse, *G;
+  TopRef top;         // kTopLogits
+  float inv_t;        // kTopDLogits: dZ = G exp(z inv_t - lse)
   __nv_bfloat16 *dz;  // three planes [rows][ldz]
   int64_t ldz, dz_plane;
   float *out;         // kDH, kDW: [split][M][ldo]
@@ -115,23 +123,6 @@ struct __align__(8) SmemCtl {
   int abort;
 };
 
-// a = p0 + p1 + p2, for |a| below 2^100
-__device__ __forceinline__ void split3(float a, float &p0, float &p1, float &p2) {
-  p0 = __bfloat162float(__float2bfloat16_rn(a));
-  const float r = a - p0;
-  p1 = __bfloat162float(__float2bfloat16_rn(r));
-  p2 = r - p1;
-}
-// Largest magnitude (NaN if there is one), and its class.
-__device__ __forceinline__ float larger(float most, float a) {
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(most), "f"(fabsf(a)));
-  return r;
-}
-__device__ __forceinline__ void raise_class(unsigned int *word, float most) {
-  const unsigned c = !(most < CLASS_LIMIT[0]) + !(most < CLASS_LIMIT[1]) + !(most < CLASS_LIMIT[2]);
-  if (c > 0) atomicMax(word, c);
-}
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
   return *reinterpret_cast<const uint32_t *>(&v);
@@ -207,16 +198,6 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map
       "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(y), "r"(z)
       : "memory");
 }
-// 32 TMEM lanes x 16 consecutive 32-bit columns (lane i: row i).
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(taddr)
-      : "memory");
-}
 // K-major operand of 64-byte rows (32 bf16) under the 64-byte swizzle: 8-row
 // groups 512 bytes apart, swizzle mode 4 in bits 61-63.
 __device__ __forceinline__ uint64_t sdesc_sw64(uint32_t addr) {
@@ -287,7 +268,7 @@ __device__ __forceinline__ void fma_fill(const F32Params &p, float *dst, int64_t
                                          int64_t kend, bool wide) {
   constexpr int kRows = kOpA ? TM : TN, kLd = kOpA ? FLD_A : FLD_B;
   // contiguous along K: H and W of the logits, dZ of dH
-  constexpr bool kAlongK = kKind == kLogits || kKind == kDLogits || (kKind == kDH && kOpA);
+  constexpr bool kAlongK = kFwdKind<kKind> || kDzKind<kKind> || (kKind == kDH && kOpA);
   constexpr int kPer = kAlongK ? FK / 4 : kRows / 4;  // 4-element pieces of a source row
   constexpr int kPieces = kRows * FK / 4 / 128;       // per thread
   constexpr int kU = 4;
@@ -299,7 +280,7 @@ __device__ __forceinline__ void fma_fill(const F32Params &p, float *dst, int64_t
       const int e = (u0 + u) * 128 + threadIdx.x;
       const int i = e / kPer, c = e % kPer * 4;  // source row of the slab, first element
       x[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if constexpr (kKind == kLogits || kKind == kDLogits) {
+      if constexpr (kFwdKind<kKind> || kDzKind<kKind>) {
         const int64_t r = r0 + i;
         if (kOpA ? r < M : r < p.cols) {
           const int64_t t = kOpA && p.row_idx ? int64_t(ld(p.row_idx + r)) : r;
@@ -418,7 +399,24 @@ __device__ __noinline__ void fma_consume(const F32Params &p, int64_t M, int64_t 
       const int64_t row = t.m0 + r_in + i;
       const bool ok = row < M;
       const int64_t tok = (ok && p.row_idx) ? int64_t(ld(p.row_idx + row)) : row;
-      if constexpr (kKind == kLogits) {
+      if constexpr (kFwdKind<kKind>) {
+        if constexpr (kKind == kTopLogits) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) acc[i][j] *= p.top.inv_t;
+          if (ok) {
+            const uint16_t *off = p.top.off + tok * (p.top.tiles + 1) + (p.v0 + t.n0) / TN;
+            for (int q = ld(off), end = ld(off + 1); q < end; ++q) {
+              const int64_t c = int64_t(ld(p.top.id + tok * p.top.K + q)) - p.v0;
+#pragma unroll
+              for (int j = 0; j < 8; ++j)
+                if (col(j) == c) {
+                  p.top.z[tok * p.top.K + q] = acc[i][j];
+                  acc[i][j] = -INFINITY;
+                }
+            }
+          }
+          __syncwarp();
+        }
         float mx = -INFINITY;
 #pragma unroll
         for (int j = 0; j < 8; ++j)
@@ -428,26 +426,32 @@ __device__ __noinline__ void fma_consume(const F32Params &p, int64_t M, int64_t 
         float s = 0.f;
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          if (col(j) < p.cols) s += expf(acc[i][j] - mx);
+          if (col(j) < p.cols && (kKind == kLogits || mx != -INFINITY)) s += expf(acc[i][j] - mx);
 #pragma unroll
         for (int o = 1; o < 8; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
         if (ok) {
           if ((lane & 7) == 0)
             p.part[int64_t(p.tile0 + 4 * int(t.n0 / TN) + quarter) * p.part_ld + row] = make_float2(mx, s);
-          const int yy = ld(p.y + tok) - p.v0;
+          if constexpr (kKind == kLogits) {
+            const int yy = ld(p.y + tok) - p.v0;
 #pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if (col(j) == yy && yy < p.cols) p.zy[row] = acc[i][j];
+            for (int j = 0; j < 8; ++j)
+              if (col(j) == yy && yy < p.cols) p.zy[row] = acc[i][j];
+          }
         }
-      } else if constexpr (kKind == kDLogits) {
+      } else if constexpr (kDzKind<kKind>) {
         if (row >= p.rows) continue;
         const float g = ok ? ld(p.G + tok) : 0.f, l = ok ? ld(p.lse + tok) : 0.f;
-        const int yy = ok ? ld(p.y + tok) - p.v0 : -1;
+        const int yy = kKind == kDLogits && ok ? ld(p.y + tok) - p.v0 : -1;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           if (col(j) >= p.cols) continue;
           float d = 0.f;
-          if (g != 0.f) d = g * ((col(j) == yy ? 1.f : 0.f) - expf(acc[i][j] - l));
+          if constexpr (kKind == kTopDLogits) {
+            if (g != 0.f) d = g * expf(acc[i][j] * p.inv_t - l);
+          } else {
+            if (g != 0.f) d = g * ((col(j) == yy ? 1.f : 0.f) - expf(acc[i][j] - l));
+          }
           most = larger(most, d);
           float p0, p1, p2;  // (a NaN remainder where d is infinite or rounds to infinity)
           split3(d, p0, p1, p2);
@@ -463,7 +467,7 @@ __device__ __noinline__ void fma_consume(const F32Params &p, int64_t M, int64_t 
           if (col(j) < p.cols) dst[col(j)] = p.accumulate ? dst[col(j)] + acc[i][j] : acc[i][j];
       }
     }
-    if constexpr (kKind == kDLogits) raise_class(p.range + kOpDZ, most);
+    if constexpr (kDzKind<kKind>) raise_class(p.range + kOpDZ, most);
   }
 }
 
@@ -692,14 +696,45 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
       if (!live) continue;
       const int64_t tok = (row_ok && p.row_idx) ? int64_t(ld(p.row_idx + row)) : row;
 
-      if constexpr (kKind == kLogits) {
+      if constexpr (kFwdKind<kKind>) {
         const int valid = p.cols - col0;  // > 0
-        const int rel = row_ok ? ld(p.y + tok) - p.v0 - col0 : -1;
-        if (rel >= 0 && rel < HN && rel < valid) {
-          float v = z[0];
+        if constexpr (kKind == kTopLogits) {
 #pragma unroll
-          for (int j = 1; j < HN; ++j) v = j == rel ? z[j] : v;
-          p.zy[row] = v;
+          for (int j = 0; j < HN; ++j) z[j] *= p.top.inv_t;
+          uint32_t bits[2] = {0u, 0u};
+          float *dst = nullptr;
+          if (row_ok) {
+            const uint16_t *off = p.top.off + tok * (p.top.tiles + 1) + p.v0 / TN + n;
+            int first = ld(off);
+            for (int q = first, end = ld(off + 1); q < end; ++q) {
+              const int cc = ld(p.top.id + tok * p.top.K + q) - p.v0 - col0;
+              if (cc < 0)
+                first = q + 1;
+              else if (cc < 32)
+                bits[0] |= 1u << cc;
+              else if (cc < HN)
+                bits[1] |= 1u << (cc - 32);
+              else
+                break;
+            }
+            dst = p.top.z + tok * p.top.K + first;
+          }
+          if (__any_sync(0xffffffffu, (bits[0] | bits[1]) != 0u)) {
+#pragma unroll
+            for (int j = 0; j < HN; ++j)
+              if ((bits[j / 32] >> (j % 32)) & 1u) {
+                *dst++ = z[j];
+                z[j] = -INFINITY;
+              }
+          }
+        } else {
+          const int rel = row_ok ? ld(p.y + tok) - p.v0 - col0 : -1;
+          if (rel >= 0 && rel < HN && rel < valid) {
+            float v = z[0];
+#pragma unroll
+            for (int j = 1; j < HN; ++j) v = j == rel ? z[j] : v;
+            p.zy[row] = v;
+          }
         }
         if (valid < HN) {
 #pragma unroll
@@ -709,22 +744,27 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
 #pragma unroll
         for (int j = 1; j < HN; ++j) mx = fmaxf(mx, z[j]);
         float s[4] = {0.f, 0.f, 0.f, 0.f};
+        if (kKind == kLogits || mx != -INFINITY) {  // (the entries may be all of the quarter tile)
 #pragma unroll
-        for (int j = 0; j < HN; ++j) s[j & 3] += expf(z[j] - mx);
+          for (int j = 0; j < HN; ++j) s[j & 3] += expf(z[j] - mx);
+        }
         if (row_ok)
           p.part[int64_t(p.tile0 + 4 * n + quarter) * p.part_ld + row] = make_float2(mx, (s[0] + s[1]) + (s[2] + s[3]));
-      } else if constexpr (kKind == kDLogits) {
+      } else if constexpr (kDzKind<kKind>) {
         float g = 0.f, l = 0.f;
         int yy = -1;
         if (row_ok) {
           g = ld(p.G + tok);
           l = ld(p.lse + tok);
-          yy = ld(p.y + tok) - p.v0 - col0;
+          if constexpr (kKind == kDLogits) yy = ld(p.y + tok) - p.v0 - col0;
         }
         float most = 0.f;
 #pragma unroll
         for (int j = 0; j < HN; ++j) {
-          z[j] = g != 0.f ? g * ((j == yy ? 1.f : 0.f) - expf(z[j] - l)) : 0.f;
+          if constexpr (kKind == kTopDLogits)
+            z[j] = g != 0.f ? g * expf(z[j] * p.inv_t - l) : 0.f;
+          else
+            z[j] = g != 0.f ? g * ((j == yy ? 1.f : 0.f) - expf(z[j] - l)) : 0.f;
           most = larger(most, z[j]);
         }
         raise_class(p.range + kOpDZ, most);
@@ -940,13 +980,21 @@ sao_status split_launch(const float *H, const RowList *list, int64_t N, const fl
 
 }  // namespace
 
-sao_status f32_fwd(const float *H, const float *W, const int32_t *y, const uint8_t *row_mask, int64_t N, int32_t h,
-                   int32_t V, float *logp, float *lse, unsigned int *err, void *ws, size_t ws_bytes,
-                   cudaStream_t s) {
+namespace {
+
+// The logits of a call, reduced to partials: of the log-probs (y, and zy for the sampled
+// tokens' logits), or of a teacher's top logits.
+struct Partials {
+  float2 *part;
+  float *zy;
+  int nvt;
+  const int *pos;  // token -> row, or null: every row is its own
+};
+sao_status f32_logits(const float *H, const float *W, const int32_t *y, const TopRef *top, const uint8_t *row_mask,
+                      int64_t N, int32_t h, int32_t V, Partials *out, unsigned int *err, Carver &c, cudaStream_t s) {
   if (N > MAX_ROWS) return fail(SAO_ERR_SHAPE, "fp32 path supports at most %lld tokens", (long long)MAX_ROWS);
   const F32Plan q = f32_plan(N, h, V);
   const int nvt = (V + HN - 1) / HN;  // partials: quarter tiles that hold a column
-  Carver c(ws, ws_bytes);
   unsigned int *range = c.take<unsigned int>(kOperands);
   RowList list{};
   SAO_TRY(clear_scratch(range, kOperands * sizeof(unsigned int), s));
@@ -989,22 +1037,47 @@ sao_status f32_fwd(const float *H, const float *W, const int32_t *y, const uint8
     p.zy = zy;
     p.range = range;
     p.err = err;
-    SAO_TRY((launch_f32<kLogits>("f32_logits_fwd", ma, mb, p, s)));
+    if (top) {
+      p.top = *top;
+      SAO_TRY((launch_f32<kTopLogits>("f32_distill_logits", ma, mb, p, s)));
+    } else {
+      SAO_TRY((launch_f32<kLogits>("f32_logits_fwd", ma, mb, p, s)));
+    }
   }
-  return lse_merge_launch(part, nvt, zy, y, listed ? nullptr : row_mask, listed ? list.pos : nullptr, N, V, logp, lse,
-                          err, s);
+  *out = Partials{part, zy, nvt, listed ? list.pos : nullptr};
+  return SAO_OK;
 }
 
-sao_status f32_bwd(const float *H, const float *W, const int32_t *y, const float *lse, const float *G, int64_t N,
-                   int32_t h, int32_t V, float *dH, float *dW, int accumulate, unsigned int *err, void *ws,
-                   size_t ws_bytes, cudaStream_t s) {
+}  // namespace
+
+sao_status f32_fwd(const float *H, const float *W, const int32_t *y, const uint8_t *row_mask, int64_t N, int32_t h,
+                   int32_t V, float *logp, float *lse, unsigned int *err, void *ws, size_t ws_bytes,
+                   cudaStream_t s) {
+  Carver c(ws, ws_bytes);
+  Partials q;
+  SAO_TRY(f32_logits(H, W, y, nullptr, row_mask, N, h, V, &q, err, c, s));
+  return lse_merge_launch(q.part, q.nvt, q.zy, y, q.pos ? nullptr : row_mask, q.pos, N, V, logp, lse, err, s);
+}
+
+sao_status f32_distill_fwd(const float *H, const float *W, const uint8_t *row_mask, int64_t N, int32_t h, int32_t V,
+                           const TopRef &top, const TopFinish &f, unsigned int *err, Carver &c, cudaStream_t s) {
+  Partials q;
+  SAO_TRY(f32_logits(H, W, nullptr, &top, row_mask, N, h, V, &q, err, c, s));
+  return distill_finish(top, f, q.part, q.nvt, q.pos, N, s);
+}
+
+namespace {
+
+// The backward of the log-probs, or with `top` (y, lse, G unused) of a teacher's top logits.
+sao_status f32_backward(const float *H, const float *W, const int32_t *y, const float *lse, const float *G,
+                        const TopGrad *top, int64_t N, int32_t h, int32_t V, float *dH, float *dW, int accumulate,
+                        unsigned int *err, Carver &c, cudaStream_t s) {
   if (N > MAX_ROWS || (int64_t(h) + 63) / 64 > 65535) return fail(SAO_ERR_SHAPE, "fp32 path size limit exceeded");
   const F32Plan q = f32_plan(N, h, V);
-  Carver c(ws, ws_bytes);
   unsigned int *range = c.take<unsigned int>(kOperands);
   RowList list{};
   SAO_TRY(clear_scratch(range, kOperands * sizeof(unsigned int), s));
-  SAO_TRY(list_rows(nullptr, G, N, &list, c, s));
+  SAO_TRY(list_rows(top ? top->mask : nullptr, G, N, &list, c, s));
   __nv_bfloat16 *hpl = c.take<__nv_bfloat16>(size_t(PL) * size_t(q.cap) * size_t(q.hp));
   __nv_bfloat16 *wpl = c.take<__nv_bfloat16>(size_t(PL) * size_t(q.vc_bwd) * size_t(q.hp));
   __nv_bfloat16 *dz = c.take<__nv_bfloat16>(size_t(PL) * size_t(q.cap) * size_t(q.vc_bwd));
@@ -1051,7 +1124,15 @@ sao_status f32_bwd(const float *H, const float *W, const int32_t *y, const float
       p.rows = q.cap;
       p.cols = vc;
       p.m_count = list.count;
-      SAO_TRY((launch_f32<kDLogits>("f32_dlogits", mH_K, mW_K, p, s)));
+      if (top) {
+        p.lse = top->rest;
+        p.G = top->g;
+        p.inv_t = top->inv_t;
+        SAO_TRY((launch_f32<kTopDLogits>("f32_distill_dlogits", mH_K, mW_K, p, s)));
+        SAO_TRY(patch_top_f32(*top, list.idx, list.count, N, v0, vc, dz, q.vc_bwd, zplane, range + kOpDZ, s));
+      } else {
+        SAO_TRY((launch_f32<kDLogits>("f32_dlogits", mH_K, mW_K, p, s)));
+      }
     }
     {  // dH parts (+)= dZ W
       F32Params p = b;
@@ -1097,6 +1178,20 @@ sao_status f32_bwd(const float *H, const float *W, const int32_t *y, const float
   pdl(f32_reduce_kernel, unsigned(di.sm_count * 8), 256, 0, s)(dh_part, q.s_dh, q.cap * int64_t(q.hq), q.hq, list.pos,
                                                               N, h, dH, 0);
   return launch_end(slot, s);
+}
+
+}  // namespace
+
+sao_status f32_bwd(const float *H, const float *W, const int32_t *y, const float *lse, const float *G, int64_t N,
+                   int32_t h, int32_t V, float *dH, float *dW, int accumulate, unsigned int *err, void *ws,
+                   size_t ws_bytes, cudaStream_t s) {
+  Carver c(ws, ws_bytes);
+  return f32_backward(H, W, y, lse, G, nullptr, N, h, V, dH, dW, accumulate, err, c, s);
+}
+
+sao_status f32_distill_bwd(const float *H, const float *W, const TopGrad &t, int64_t N, int32_t h, int32_t V,
+                           float *dH, float *dW, int accumulate, unsigned int *err, Carver &c, cudaStream_t s) {
+  return f32_backward(H, W, nullptr, nullptr, nullptr, &t, N, h, V, dH, dW, accumulate, err, c, s);
 }
 
 }  // namespace sao

@@ -10,6 +10,8 @@
 //                                   one shift kappa per row)
 //   backward  Z = H W^T (again)  -> dZ = G (1[v == y] - exp(z - lse)), bf16,
 //                                   into a [N, Vc] chunk buffer
+//             (a teacher's top logits: dZ = g exp(z / T - rest), the entries patched
+//             afterwards)
 //             dH (+)= dZ W_chunk    (A K-major, B = W MN-major)
 //             dW_chunk = dZ^T H     (A = dZ MN-major, B = H MN-major)
 //   cached backward (dZ = s e row by row, s = -G exp(kappa - lse)):
@@ -31,6 +33,7 @@
 
 #include <mutex>
 
+#include "distill.cuh"
 #include "logprobs_common.cuh"
 #include "per_device.h"
 #include "rows.cuh"
@@ -62,8 +65,13 @@ enum EpiKind : int {
   kStoreBF16 = 3,
   kSoftmaxStore = 4,
   kBulkStore = 5,  // fp32 output in staged boxes
-  kBulkAdd = 6     // the same, added to the output's contents
+  kBulkAdd = 6,    // the same, added to the output's contents
+  kTopDLogits = 7,  // kDLogits without a sampled token, at a temperature
+  kTopDLogits2 = 8, // the same in two pieces: see kFewRows in distill.cuh
+  kBulkBF16 = 9     // bf16 output in staged boxes
 };
+template <int kEpi>
+constexpr bool kTopEpi = (kEpi == kTopDLogits || kEpi == kTopDLogits2);
 
 // fp32 output in boxes of 128 rows x 32 columns, written with TMA stores; for
 // kBulkAdd the old contents arrive in the same boxes with TMA loads issued up to
@@ -77,7 +85,8 @@ constexpr bool kBulkEpi = (kEpi == kBulkStore || kEpi == kBulkAdd);
 // Epilogues that stage boxes in shared memory and write them with TMA stores;
 // their 4 warps synchronise with named barriers.
 template <int kEpi>
-constexpr bool kTmaStoreEpi = (kEpi == kDLogits || kEpi == kSoftmaxStore || kBulkEpi<kEpi>);
+constexpr bool kTmaStoreEpi =
+    (kEpi == kDLogits || kTopEpi<kEpi> || kEpi == kSoftmaxStore || kBulkEpi<kEpi> || kEpi == kBulkBF16);
 
 struct GemmParams {
   int nM, nN, nK;      // tiles along M, N and 64-wide K blocks
@@ -93,6 +102,7 @@ struct GemmParams {
   float2 *part;        // softmax partials [nN][rows]
   float *zy;           // gathered logit of the sampled token
   const float *lse, *G;
+  float zscale;        // log2(e) / temperature (kTopDLogits)
   __nv_bfloat16 *dz;   // dlogits output [rows][ldz]
   int64_t ldz;
   float *cf;           // store f32 output (row-major, ldc)
@@ -434,7 +444,7 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
       const int64_t row0 = int64_t(m) * kTM + int64_t(rank) * BM;
       const int64_t row = row0 + r;
       const bool row_ok = row < rows;
-      const int64_t orig = (row_ok && p.row_idx) ? int64_t(ld(p.row_idx + row)) : row;
+      const int64_t orig = (row_ok && p.row_idx) ? int64_t(ld(p.row_idx + row)) : row;  // (kTopDLogits2: may be -1)
 
       if constexpr (kEpi == kSoftmax) {
         const int col0 = n * BN;
@@ -614,25 +624,28 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
           p.part[int64_t(n) * p.rows + row] = part;  // compacted row, stride N
           if (have) p.zy[row] = zsel;
         }
-      } else if constexpr (kEpi == kDLogits) {
+      } else if constexpr (kEpi == kDLogits || kTopEpi<kEpi>) {
         // dZ goes out through two swizzled 128x64 staging boxes and TMA
         // stores; one epilogue thread issues the stores and tracks them.
         const bool issuer = (warp == 2 && lane == 0);
         const int lc0 = n * BN;  // column inside the chunk
         int yy = -1;
         float g = 0.f, l2 = 0.f;
-        if (row_ok) {
-          yy = ld(p.y + orig) - p.v0;
+        if (row_ok && (kEpi != kTopDLogits2 || orig >= 0)) {
+          if constexpr (kEpi == kDLogits) yy = ld(p.y + orig) - p.v0;
           g = ld(p.G + orig);
+          if constexpr (kTopEpi<kEpi>) g = -g;
           l2 = ld(p.lse + orig) * kLog2e;
         }
+        const float zs = kTopEpi<kEpi> ? p.zscale : kLog2e;
+        const bool second = kEpi == kTopDLogits2 && r >= kFewRows;  // this row holds the second pieces
         // Per pair of columns: one fused multiply-add, two exponentials, one
         // multiply, one conversion. The 32 columns that hold the sampled token's
         // take a path of their own, and so does a row with g = 0 (the padding
         // rows), whose dZ is 0 whatever its logits are. (Both checks in each
         // column made the epilogue outlast a main loop of h = 1024 by 1.7-2.2 k
         // cycles per tile: 98,304 x 32,000 logits at h = 1024 3.42 ms, 3.3 so.)
-        const f32x2 log2e2 = pack_f32x2(kLog2e, kLog2e), nl2 = pack_f32x2(-l2, -l2), ng2 = pack_f32x2(-g, -g);
+        const f32x2 log2e2 = pack_f32x2(zs, zs), nl2 = pack_f32x2(-l2, -l2), ng2 = pack_f32x2(-g, -g);
 #pragma unroll 1
         for (int box = 0; box < BN / 64; ++box) {
           const uint32_t buf = out_base + uint32_t(box & 1) * STAGE_OUT_BYTES;
@@ -655,8 +668,8 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
               for (int j = 0; j < 32; j += 2) {
                 float d0 = 0.f, d1 = 0.f;
                 if (g != 0.f) {
-                  d0 = -g * ex2_approx(fmaf(__uint_as_float(u[j]), kLog2e, -l2));
-                  d1 = -g * ex2_approx(fmaf(__uint_as_float(u[j + 1]), kLog2e, -l2));
+                  d0 = -g * ex2_approx(fmaf(__uint_as_float(u[j]), zs, -l2));
+                  d1 = -g * ex2_approx(fmaf(__uint_as_float(u[j + 1]), zs, -l2));
                   if (lc + j == yy) d0 += g;
                   if (lc + j + 1 == yy) d1 += g;
                 }
@@ -670,7 +683,9 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
                 unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(u[j]), __uint_as_float(u[j + 1])), log2e2, nl2), t0,
                              t1);
                 unpack_f32x2(mul_f32x2(pack_f32x2(ex2_approx(t0), ex2_approx(t1)), ng2), d0, d1);
-                const __nv_bfloat162 b2 = __floats2bfloat162_rn(d0, d1);
+                __nv_bfloat162 b2 = __floats2bfloat162_rn(d0, d1);
+                if (kEpi == kTopDLogits2 && second)
+                  b2 = __floats2bfloat162_rn(d0 - __low2float(b2), d1 - __high2float(b2));
                 pk[j / 2] = *reinterpret_cast<const uint32_t *>(&b2);
               }
             }
@@ -688,6 +703,45 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
           named_barrier(EPI_BARRIER, 128);
           if (issuer && row0 < rows) {
             tma_store_2d(&map_c, buf, lc0 + box * 64, int(row0));
+            bulk_commit_group();
+          }
+        }
+      } else if constexpr (kEpi == kBulkBF16) {
+        const bool issuer = (warp == 2 && lane == 0);
+#pragma unroll 1
+        for (int box = 0; box < BN / 64; ++box) {
+          const uint32_t buf = out_base + uint32_t(box & 1) * STAGE_OUT_BYTES;
+          if (issuer) bulk_wait_group_read<1>();  // the store that last read `buf` is done
+          named_barrier(EPI_BARRIER, 128);
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            uint32_t u[32];
+            tmem_ld32(taddr + (box * 2 + half) * 32, u);
+            tmem_wait_ld();
+            if (box == BN / 64 - 1 && half == 1) {
+              fence_before_sync();
+              release_acc(acc);
+            }
+            uint32_t pk[16];
+#pragma unroll
+            for (int j = 0; j < 32; j += 2) {
+              const __nv_bfloat162 b2 = __floats2bfloat162_rn(__uint_as_float(u[j]), __uint_as_float(u[j + 1]));
+              pk[j / 2] = kzero ? 0u : *reinterpret_cast<const uint32_t *>(&b2);
+            }
+            // 128-byte swizzle: 16-byte chunk j of row r sits at chunk j ^ (r % 8)
+            const uint32_t row_addr = buf + uint32_t(r) * 128u;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const uint32_t chunk = uint32_t(half * 4 + q) ^ uint32_t(r & 7);
+              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(row_addr + chunk * 16u),
+                           "r"(pk[4 * q]), "r"(pk[4 * q + 1]), "r"(pk[4 * q + 2]), "r"(pk[4 * q + 3])
+                           : "memory");
+            }
+          }
+          fence_proxy_async_smem();
+          named_barrier(EPI_BARRIER, 128);
+          if (issuer) {
+            if (n * BN + box * 64 < p.cols) tma_store_2d(&map_c, buf, n * BN + box * 64, int(row0));
             bulk_commit_group();
           }
         }
@@ -1006,7 +1060,9 @@ __global__ void __launch_bounds__(32 * kRowWarps) bwd_scale_kernel(const __nv_bf
 // ---------------------------------------------------------------------------
 // host side: tensor maps and launches
 // ---------------------------------------------------------------------------
-PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
+}  // namespace
+
+PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder() {
   static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
   static std::once_flag once;
   std::call_once(once, [] {
@@ -1020,12 +1076,9 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_fn() {
   return fn;
 }
 
-// 2-D bf16 tensor map over a row-major [outer][inner] array with row pitch
-// `pitch_elems`, box {box_inner (64 = 128 bytes), box_outer}, 128-byte swizzle,
-// zero fill outside the array.
 sao_status make_map(CUtensorMap *m, const void *ptr, uint64_t inner, uint64_t outer, uint64_t pitch_elems,
                     uint32_t box_inner, uint32_t box_outer) {
-  auto fn = encode_fn();
+  auto fn = tensor_map_encoder();
   if (!fn) return fail(SAO_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
   if ((reinterpret_cast<uintptr_t>(ptr) & 15u) != 0) return fail(SAO_ERR_INVALID_ARG, "bf16 operand not 16-byte aligned");
   cuuint64_t dims[2] = {inner, outer};
@@ -1039,9 +1092,11 @@ sao_status make_map(CUtensorMap *m, const void *ptr, uint64_t inner, uint64_t ou
   return SAO_OK;
 }
 
+namespace {
+
 // 2-D fp32 tensor map of boxes of 32 columns x 128 rows, 128-byte swizzle.
 sao_status make_map_f32(CUtensorMap *m, const float *ptr, uint64_t inner, uint64_t outer) {
-  auto fn = encode_fn();
+  auto fn = tensor_map_encoder();
   if (!fn) return fail(SAO_ERR_CUDA, "cuTensorMapEncodeTiled is not available from the driver");
   cuuint64_t dims[2] = {inner, outer};
   cuuint64_t strides[1] = {inner * 4};
@@ -1157,6 +1212,12 @@ void set_f32_out(GemmParams &p, float *out, int64_t ldc) {
 // part of dH at 517, 1,000, 1,280, 3,072 and 8,192 tokens: 1.03 to 3.1 times.)
 constexpr int64_t kBulkTokens = 1280, kSingleStoreTokens = 3072, kSingleAddTokens = 8192;
 
+// Where dW goes: one of the two.
+struct DwOut {
+  float *f32;
+  __nv_bfloat16 *bf16;
+};
+
 // M tiles per CTA tile (1 or 2) for a long-K product with `rows` output rows
 // and `cols` output columns, and the tiles along M that gives.
 struct MTiles {
@@ -1176,14 +1237,29 @@ MTiles m_tiles(int64_t rows, int cols, int cg, int sms) {
 // boxes; up to a few thousand tokens one M tile per CTA tile, so that a tile's
 // output overlaps the next one's main loop; a long one shares each B stage
 // between two M tiles.
-sao_status launch_dw(const char *name, const CUtensorMap &ma, const CUtensorMap &mb, GemmParams p, float *dW, int v0,
-                     int vc, int h, int64_t K, int accumulate, int cg, int sms, cudaStream_t s) {
+// A bf16 dW is written once, from its whole sum.
+sao_status launch_dw(const char *name, const CUtensorMap &ma, const CUtensorMap &mb, GemmParams p, const DwOut &dst,
+                     int v0, int vc, int h, int64_t K, int accumulate, int cg, int sms, cudaStream_t s) {
   p.nN = (h + BN - 1) / BN;
   p.group_m = 1;
   p.rows = vc;
   p.cols = h;
   p.nK = int((K + BK - 1) / BK);
-  float *out = dW + int64_t(v0) * h;
+  if (dst.bf16) {
+    if (cg == 1 && K < kBulkTokens) {
+      CUtensorMap mo;
+      SAO_TRY(make_map(&mo, dst.bf16 + int64_t(v0) * h, uint64_t(h), uint64_t(vc), uint64_t(h), 64, BM));
+      p.nM = (vc + BM - 1) / BM;
+      return launch_gemm<kBulkBF16, true, true>(name, ma, mb, mo, p, s);
+    }
+    const MTiles mt = cg == 1 && K < kSingleStoreTokens ? MTiles{1, (vc + BM - 1) / BM} : m_tiles(vc, h, cg, sms);
+    p.nM = mt.nM;
+    p.cb = dst.bf16;
+    p.ldc = h;
+    p.c_row_off = v0;
+    return launch_gemm_cfg<kStoreBF16, true, true>(name, mt.kmt, cg, ma, mb, ma, p, s);
+  }
+  float *dW = dst.f32, *out = dW + int64_t(v0) * h;
   if (cg == 1 && K < kBulkTokens && (reinterpret_cast<uintptr_t>(out) & 15u) == 0) {
     CUtensorMap mo;
     SAO_TRY(make_map_f32(&mo, out, uint64_t(h), uint64_t(vc)));
@@ -1229,8 +1305,9 @@ struct BwdPlan {
 // and writes once per extra chunk; several row blocks make the dW GEMM add
 // into dW once per extra block. The plan takes the split with the least of
 // that extra traffic (plus a fixed cost per block and chunk for the launches
-// and the partial last wave).
-BwdPlan bwd_plan(int64_t N, int32_t h, int32_t V) {
+// and the partial last wave). one_block: a single block of rows whatever it costs (an
+// output that cannot be added to).
+BwdPlan bwd_plan(int64_t N, int32_t h, int32_t V, bool one_block = false) {
   const int64_t vpad = (int64_t(V) + BN - 1) / BN * BN;
   const double budget = double(dz_budget());
   BwdPlan best{N > 0 ? N : 1, int(vpad), 1};
@@ -1239,7 +1316,7 @@ BwdPlan bwd_plan(int64_t N, int32_t h, int32_t V) {
     return best;
   }
   double best_cost = -1.0;
-  const int64_t max_blocks = (N + BM - 1) / BM;
+  const int64_t max_blocks = one_block ? 1 : (N + BM - 1) / BM;
   for (int64_t nb = 1; nb <= max_blocks && nb <= 4096; ++nb) {
     int64_t rows = (N + nb - 1) / nb;
     rows = (rows + BM - 1) / BM * BM;
@@ -1264,7 +1341,14 @@ BwdPlan bwd_plan(int64_t N, int32_t h, int32_t V) {
 
 }  // namespace
 
-PFN_cuTensorMapEncodeTiled_v12000 tensor_map_encoder() { return encode_fn(); }
+namespace {
+size_t recompute_bytes(const BwdPlan &pl, int32_t h, int32_t V, bool f32_dh = false) {
+  size_t rec = compact_ws_bytes(pl.rows, h) + round256(size_t(pl.rows) * size_t(pl.vc) * 2);
+  if (pl.vc < V || pl.splits > 1 || f32_dh)
+    rec += round256(size_t(pl.splits) * size_t(pl.rows) * size_t(h) * sizeof(float));
+  return rec;
+}
+}  // namespace
 
 // Workspace of the log-prob calls: the forward's row compaction, tile
 // partials and gathered logits; the backward's row compaction of one row
@@ -1276,10 +1360,7 @@ size_t tc_ws_bytes(int64_t N, int32_t h, int32_t V) {
   const int64_t cap = (N + BM - 1) / BM * BM;
   const size_t fwd = compact_ws_bytes(N, h) + round256(sizeof(float2) * size_t(nvt) * size_t(N)) +
                      round256(sizeof(float) * size_t(N));
-  const BwdPlan pl = bwd_plan(N, h, V);
-  size_t rec = compact_ws_bytes(pl.rows, h) + round256(size_t(pl.rows) * size_t(pl.vc) * 2);
-  if (pl.vc < V || pl.splits > 1)
-    rec += round256(size_t(pl.splits) * size_t(pl.rows) * size_t(h) * sizeof(float));
+  const size_t rec = recompute_bytes(bwd_plan(N, h, V), h, V);
   const size_t cached = round256(sizeof(float) * size_t(cap)) + round256(size_t(cap) * size_t(h) * 2) +
                         round256(size_t(N));
   // the cached path's dH parts are done with before its flagged rows use the recompute scratch
@@ -1383,23 +1464,31 @@ namespace {
 // (mask given) or G[t] != 0: dZ per vocabulary chunk by the dlogits GEMM, then
 // dH and dW. overwrite_dH: dH is written on every row (zeros on inactive
 // ones); otherwise only the active rows of dH are written. `names` label the
-// three GEMMs' launches for the library's timers.
+// three GEMMs' launches for the library's timers. With `top` (y, lse, G, mask
+// unused) dZ is that of a teacher's top logits.
 struct BwdNames {
   const char *dlogits, *dH, *dW;
 };
 constexpr BwdNames kBwdNames{"tc_dlogits", "tc_dH_gemm", "tc_dW_gemm"};
 constexpr BwdNames kFlaggedNames{"flagged_dlogits", "flagged_dH_gemm", "flagged_dW_gemm"};
+constexpr BwdNames kDistillNames{"distill_dlogits", "distill_dH_gemm", "distill_dW_gemm"};
 
 sao_status bwd_recompute_block(const void *H, const void *W, const int32_t *y, const float *lse, const float *G,
                                const uint8_t *mask, int64_t N, int32_t h, int32_t V, const BwdPlan &pl, void *dH,
-                               float *dW, int accumulate, bool overwrite_dH, const BwdNames &names,
-                               unsigned int *err, Carver &c, cudaStream_t s) {
+                               const DwOut &dW, int accumulate, bool overwrite_dH, const BwdNames &names,
+                               const TopGrad *top, unsigned int *err, Carver &c, cudaStream_t s) {
   const int Vc = pl.vc;
+  const bool few = top != nullptr && N <= kFewRows;  // dZ in two pieces, in 128 rows
   const bool multi = Vc < V;                      // several vocabulary chunks
-  const bool f32_dh = multi || pl.splits > 1;     // dH through fp32 rows, rounded at the end
+  const bool f32_dh = multi || pl.splits > 1 || few;  // dH through fp32 rows, rounded at the end
   // Rows whose incoming gradient is zero contribute nothing: compact the rest.
   CompactRows cr{};
-  SAO_TRY(compact_rows(mask, mask ? nullptr : G, N, static_cast<const __nv_bfloat16 *>(H), h, &cr, c, s));
+  if (few)
+    SAO_TRY(distill_few_rows(mask, N, static_cast<const __nv_bfloat16 *>(H), h, &cr, c, s));
+  else
+    SAO_TRY(compact_rows(mask, mask ? nullptr : G, N, static_cast<const __nv_bfloat16 *>(H), h, &cr, c, s));
+  const int64_t tokens = N;
+  if (few) N = 2 * kFewRows;  // rows of the products from here on
   __nv_bfloat16 *dz = c.take<__nv_bfloat16>(size_t(N) * size_t(Vc));
   const DhParts parts = dh_scratch(pl.splits, pl.rows, h, Vc < V ? Vc : V);
   float *dh_acc = f32_dh ? c.take<float>(size_t(pl.splits) * size_t(pl.rows) * size_t(h)) : nullptr;
@@ -1408,7 +1497,7 @@ sao_status bwd_recompute_block(const void *H, const void *W, const int32_t *y, c
 
   CUtensorMap mHc_K, mW_K, mHc_MN, mW_MN;
   SAO_TRY(make_map(&mHc_K, cr.Hc, uint64_t(h), uint64_t(cr.cap), uint64_t(h), 64, BM));
-  const int cg = cta_group();
+  const int cg = few ? 1 : cta_group();
   SAO_TRY(make_map(&mW_K, W, uint64_t(h), uint64_t(V), uint64_t(h), 64, BN / cg));
   SAO_TRY(make_map(&mHc_MN, cr.Hc, uint64_t(h), uint64_t(cr.cap), uint64_t(h), 64, 64));
   SAO_TRY(make_map(&mW_MN, W, uint64_t(h), uint64_t(V), uint64_t(h), 64, 64));
@@ -1441,7 +1530,18 @@ sao_status bwd_recompute_block(const void *H, const void *W, const int32_t *y, c
       p.err = err;
       p.m_count = cr.count;
       p.row_idx = cr.idx;
-      SAO_TRY((launch_gemm_cfg<kDLogits, false, false>(names.dlogits, 1, cg, mHc_K, mW_K, mZ_K, p, s)));
+      if (top) {
+        p.lse = top->rest;
+        p.G = top->g;
+        p.zscale = kLog2e * top->inv_t;
+        if (few)
+          SAO_TRY((launch_gemm_cfg<kTopDLogits2, false, false>(names.dlogits, 1, 1, mHc_K, mW_K, mZ_K, p, s)));
+        else
+          SAO_TRY((launch_gemm_cfg<kTopDLogits, false, false>(names.dlogits, 1, cg, mHc_K, mW_K, mZ_K, p, s)));
+        SAO_TRY(patch_top_bf16(*top, cr.idx, cr.count, N, few, v0, vc, dz, Vc, s));
+      } else {
+        SAO_TRY((launch_gemm_cfg<kDLogits, false, false>(names.dlogits, 1, cg, mHc_K, mW_K, mZ_K, p, s)));
+      }
     }
     {  // dH (+)= dZ W[v0:v0+vc]: two 128-row tiles per CTA tile share each W stage when enough tiles remain
       GemmParams p{};
@@ -1473,7 +1573,9 @@ sao_status bwd_recompute_block(const void *H, const void *W, const int32_t *y, c
       p.k_count = cr.count;
       SAO_TRY(launch_dw(names.dW, mZ_MN, mHc_MN, p, dW, v0, vc, h, N, accumulate, cg, sms, s));
     }
-    if (f32_dh && last)
+    if (few && last)
+      SAO_TRY(distill_few_dH(dh_acc, parts, h, cr.pos, cr.count, tokens, static_cast<__nv_bfloat16 *>(dH), s));
+    else if (f32_dh && last)
       SAO_TRY(scatter_rows_to_bf16(dh_acc, parts, h, nullptr, cr.pos, cr.idx, cr.count, N,
                                    static_cast<__nv_bfloat16 *>(dH), overwrite_dH, s));
   }
@@ -1493,13 +1595,29 @@ sao_status bwd_recompute(const void *H, const void *W, const int32_t *y, const f
     const int64_t nr = (N - r0) < pl.rows ? (N - r0) : pl.rows;
     Carver cb = c;
     SAO_TRY(bwd_recompute_block(Hb + r0 * h, W, y + r0, lse + r0, G + r0, mask ? mask + r0 : nullptr, nr, h, V,
-                                pl, dHb + r0 * h, dW, r0 == 0 ? accumulate : 1, overwrite_dH, names, err, cb,
-                                s));
+                                pl, dHb + r0 * h, DwOut{dW, nullptr}, r0 == 0 ? accumulate : 1, overwrite_dH, names,
+                                nullptr, err, cb, s));
   }
   return SAO_OK;
 }
 
 }  // namespace
+
+// The plan takes one block of rows: a bf16 dW is written from its whole sum. Few rows
+// take 128 (see kFewRows).
+namespace {
+int64_t distill_rows(int64_t N) { return N <= kFewRows ? 2 * kFewRows : N; }
+}  // namespace
+size_t tc_distill_bwd_bytes(int64_t N, int32_t h, int32_t V) {
+  return recompute_bytes(bwd_plan(distill_rows(N), h, V, true), h, V, N <= kFewRows);
+}
+sao_status tc_distill_bwd(const void *H, const void *W, const TopGrad &t, int64_t N, int32_t h, int32_t V, void *dH,
+                          void *dW, sao_dtype dw_dt, int accumulate, unsigned int *err, Carver &c, cudaStream_t s) {
+  const DwOut out = dw_dt == SAO_BF16 ? DwOut{nullptr, static_cast<__nv_bfloat16 *>(dW)}
+                                      : DwOut{static_cast<float *>(dW), nullptr};
+  return bwd_recompute_block(H, W, nullptr, nullptr, nullptr, t.mask, N, h, V, bwd_plan(distill_rows(N), h, V, true),
+                             dH, out, accumulate, true, kDistillNames, &t, err, c, s);
+}
 
 sao_status tc_bwd(const void *H, const void *W, const int32_t *y, const float *lse, const float *G, int64_t N,
                   int32_t h, int32_t V, void *dH, float *dW, int accumulate, unsigned int *err, void *ws,
@@ -1564,7 +1682,7 @@ sao_status tc_bwd(const void *H, const void *W, const int32_t *y, const float *l
     GemmParams p{};
     p.err = err;
     p.k_count = cache->count;
-    SAO_TRY(launch_dw("tc_dW_gemm", mE_MN, mHs_MN, p, dW, 0, V, h, N, accumulate, cg, sms, s));
+    SAO_TRY(launch_dw("tc_dW_gemm", mE_MN, mHs_MN, p, DwOut{dW, nullptr}, 0, V, h, N, accumulate, cg, sms, s));
   }
   // Flagged rows (a sampled token more than kFlagExponent - kKappaOffset nats
   // below its row's maximum) got sc = 0 above: recompute their logits, write

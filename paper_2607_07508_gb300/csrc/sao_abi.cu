@@ -7,6 +7,8 @@
 
 #include <nvtx3/nvToolsExt.h>
 
+#include "balance.cuh"
+#include "distill.cuh"
 #include "logprobs_common.cuh"
 #include "sao_common.cuh"
 #include "sao_internal.h"
@@ -463,6 +465,139 @@ sao_status sao_running_mean_advantages(const float *rewards, const int32_t *prom
   SAO_TRY(begin_call(ws, s));
   SAO_TRY(running_mean_launch(rewards, prompt_ids, B, num_prompts, history, seen, window, loss_mask, cu_seqlens, N,
                               adv, w.body, w.body_bytes, s));
+  return finish_call(ws, s);
+}
+
+static sao_status check_distill(sao_dtype dt, sao_dtype top_dt, int64_t N, int32_t h, int32_t V, int32_t K,
+                                float temperature) {
+  SAO_TRY(check_logprob_shapes(dt, N, h, V));
+  if (bad_dtype(top_dt)) return fail(SAO_ERR_UNSUPPORTED, "unknown dtype %d of the teacher's logits", int(top_dt));
+  if (K < 1 || K > SAO_DISTILL_MAX_K) return fail(SAO_ERR_SHAPE, "K = %d not in 1..%d", K, SAO_DISTILL_MAX_K);
+  // tiles of 128 rows x 256 columns are numbered in 32 bits
+  if (((N + 127) / 128) * ((int64_t(V) + 255) / 256) >= (int64_t(1) << 31))
+    return fail(SAO_ERR_SHAPE, "N = %lld rows of V = %d are too many tiles", (long long)N, V);
+  if (!(temperature > 0.f) || !isfinite(temperature) || !isfinite(1.f / temperature))
+    return fail(SAO_ERR_INVALID_ARG, "temperature must be positive and finite (%g)", temperature);
+  return SAO_OK;
+}
+
+size_t sao_distill_workspace_bytes(int64_t N, int32_t h, int32_t V, int32_t K, sao_dtype dt) {
+  if (N < 0 || h < 1 || V < 1 || K < 1 || K > SAO_DISTILL_MAX_K || bad_dtype(dt)) return 0;
+  return kWsHeader + distill_ws_bytes(N, h, V, K, dt);
+}
+
+sao_status sao_distill_loss_fwd(const void *H, const void *W, sao_dtype dt, const int32_t *top_ids,
+                                const void *top_logits, sao_dtype top_dt, const float *teacher_lse,
+                                const uint8_t *row_mask, int64_t N, int32_t h, int32_t V, int32_t K,
+                                float temperature, float *loss, float *lse, float *lse_rest, float *z_top, void *ws,
+                                size_t ws_bytes, sao_stream_t stream) {
+  SAO_RANGE();
+  SAO_TRY(check_distill(dt, top_dt, N, h, V, K, temperature));
+  if (N == 0) return SAO_OK;
+  if (!H || !W || !top_ids || !top_logits || !loss || !lse || !lse_rest || !z_top)
+    return fail(SAO_ERR_INVALID_ARG, "NULL array argument");
+  SAO_TRY(check_tc_device(dt));
+  Ws w;
+  SAO_TRY(take_ws(ws, ws_bytes, distill_ws_bytes(N, h, V, K, dt), &w));
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  SAO_TRY(begin_call(ws, s));
+  SAO_TRY(distill_fwd_launch(H, W, dt, top_ids, top_logits, top_dt, teacher_lse, row_mask, N, h, V, K, temperature,
+                             loss, lse, lse_rest, z_top, w.err, w.body, w.body_bytes, s));
+  return finish_call(ws, s);
+}
+
+sao_status sao_distill_loss_bwd(const void *H, const void *W, sao_dtype dt, const int32_t *top_ids,
+                                const void *top_logits, sao_dtype top_dt, const float *teacher_lse, const float *lse,
+                                const float *lse_rest, const float *z_top, const float *grad_loss, int64_t N,
+                                int32_t h, int32_t V, int32_t K, float temperature, void *dH, void *dW,
+                                sao_dtype dw_dt, int accumulate_dW, void *ws, size_t ws_bytes, sao_stream_t stream) {
+  SAO_RANGE();
+  SAO_TRY(check_distill(dt, top_dt, N, h, V, K, temperature));
+  if (bad_dtype(dw_dt) || (dw_dt == SAO_BF16 && dt != SAO_BF16))
+    return fail(SAO_ERR_UNSUPPORTED, "dW is fp32, or bf16 for a bf16 head");
+  if (dw_dt == SAO_BF16 && accumulate_dW)
+    return fail(SAO_ERR_UNSUPPORTED, "a bf16 dW is overwritten: only an fp32 one can be added to");
+  if (!W || !dW) return fail(SAO_ERR_INVALID_ARG, "NULL array argument");
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  if (N == 0) {
+    if (!accumulate_dW) SAO_CUDA_TRY(cudaMemsetAsync(dW, 0, (dw_dt == SAO_BF16 ? 2 : 4) * size_t(V) * size_t(h), s));
+    return SAO_OK;
+  }
+  if (!H || !top_ids || !top_logits || !lse || !lse_rest || !z_top || !grad_loss || !dH)
+    return fail(SAO_ERR_INVALID_ARG, "NULL array argument");
+  if (dt == SAO_BF16 && (!aligned16(dH) || !aligned16(dW)))
+    return fail(SAO_ERR_INVALID_ARG, "dH and dW of a bf16 head must be 16-byte aligned");
+  SAO_TRY(check_tc_device(dt));
+  Ws w;
+  SAO_TRY(take_ws(ws, ws_bytes, distill_ws_bytes(N, h, V, K, dt), &w));
+  SAO_TRY(begin_call(ws, s));
+  SAO_TRY(distill_bwd_launch(H, W, dt, top_ids, top_logits, top_dt, teacher_lse, lse, lse_rest, z_top, grad_loss, N, h,
+                             V, K, temperature, dH, dW, dw_dt, accumulate_dW, w.err, w.body, w.body_bytes, s));
+  return finish_call(ws, s);
+}
+
+static sao_status check_balance(sao_dtype dt, const int32_t *cu, int32_t B, int64_t N, int32_t E, int32_t k,
+                                int score) {
+  if (bad_dtype(dt)) return fail(SAO_ERR_UNSUPPORTED, "unknown dtype %d", int(dt));
+  if (N < 0 || N >= (int64_t(1) << 31)) return fail(SAO_ERR_SHAPE, "N = %lld out of range", (long long)N);
+  if (E < 1 || E > SAO_BALANCE_MAX_EXPERTS || k < 1 || k > E)
+    return fail(SAO_ERR_SHAPE, "E = %d experts, k = %d: 1 <= k <= E <= %d", E, k, SAO_BALANCE_MAX_EXPERTS);
+  if (cu && (B < 0 || (N > 0 && B == 0))) return fail(SAO_ERR_SHAPE, "N > 0 tokens need at least one trajectory");
+  if (cu && int64_t(B) * ((E + 31) / 32) >= (int64_t(1) << 31))
+    return fail(SAO_ERR_SHAPE, "B = %d trajectories of %d experts are too many", B, E);
+  if (score != SAO_SCORE_SOFTMAX && score != SAO_SCORE_SIGMOID)
+    return fail(SAO_ERR_INVALID_ARG, "unknown score %d", score);
+  return SAO_OK;
+}
+
+size_t sao_balance_workspace_bytes(int64_t N, int32_t E, int32_t B) {
+  if (N < 0 || E < 1 || E > SAO_BALANCE_MAX_EXPERTS || B < 0) return 0;
+  return kWsHeader + balance_ws_bytes(N, E, B < 1 ? 1 : B);
+}
+
+sao_status sao_balance_loss_fwd(const void *logits, sao_dtype dt, const int32_t *expert_ids, const uint8_t *row_mask,
+                                const int32_t *cu_seqlens, int32_t B, int64_t N, int32_t E, int32_t k, int score,
+                                float *loss, int64_t *counts, float *prob_sums, int64_t *rows, void *ws,
+                                size_t ws_bytes, sao_stream_t stream) {
+  SAO_RANGE();
+  SAO_TRY(check_balance(dt, cu_seqlens, B, N, E, k, score));
+  if (!loss) return fail(SAO_ERR_INVALID_ARG, "NULL loss");
+  const int32_t segments = cu_seqlens ? B : 1;
+  if (segments > 0 && (!counts || !prob_sums || !rows)) return fail(SAO_ERR_INVALID_ARG, "NULL array argument");
+  if (N > 0 && (!logits || !expert_ids)) return fail(SAO_ERR_INVALID_ARG, "NULL array argument");
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  if (N == 0) {
+    SAO_CUDA_TRY(cudaMemsetAsync(loss, 0, sizeof(float), s));
+    if (segments > 0) {
+      SAO_CUDA_TRY(cudaMemsetAsync(counts, 0, sizeof(int64_t) * size_t(segments) * size_t(E), s));
+      SAO_CUDA_TRY(cudaMemsetAsync(prob_sums, 0, sizeof(float) * size_t(segments) * size_t(E), s));
+      SAO_CUDA_TRY(cudaMemsetAsync(rows, 0, sizeof(int64_t) * size_t(segments), s));
+    }
+    return SAO_OK;
+  }
+  Ws w;
+  SAO_TRY(take_ws(ws, ws_bytes, balance_ws_bytes(N, E, segments), &w));
+  SAO_TRY(begin_call(ws, s));
+  SAO_TRY(balance_fwd_launch(logits, dt, expert_ids, row_mask, cu_seqlens, segments, N, E, k, score, loss, counts,
+                             prob_sums, rows, w.err, w.body, w.body_bytes, s));
+  return finish_call(ws, s);
+}
+
+sao_status sao_balance_loss_bwd(const void *logits, sao_dtype dt, const uint8_t *row_mask, const int32_t *cu_seqlens,
+                                int32_t B, int64_t N, int32_t E, int32_t k, int score, const int64_t *counts,
+                                const int64_t *rows, const float *grad_loss, void *grad_logits, void *ws,
+                                size_t ws_bytes, sao_stream_t stream) {
+  SAO_RANGE();
+  SAO_TRY(check_balance(dt, cu_seqlens, B, N, E, k, score));
+  if (N == 0) return SAO_OK;
+  if (!logits || !counts || !rows || !grad_loss || !grad_logits)
+    return fail(SAO_ERR_INVALID_ARG, "NULL array argument");
+  Ws w;
+  SAO_TRY(take_ws(ws, ws_bytes, 0, &w));
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  SAO_TRY(begin_call(ws, s));
+  SAO_TRY(balance_bwd_launch(logits, dt, row_mask, cu_seqlens, cu_seqlens ? B : 1, N, E, k, score, counts, rows,
+                             grad_loss, grad_logits, w.err, s));
   return finish_call(ws, s);
 }
 

@@ -20,6 +20,8 @@ LIB_PATH = os.path.join(_HERE, "libsao.so")
 SAO_F32, SAO_BF16 = 0, 1
 SAO_STEP_AVERAGE, SAO_STEP_LAST = 0, 1
 SAO_NORM_TOKEN, SAO_NORM_SEQUENCE = 0, 1
+SAO_SCORE_SOFTMAX, SAO_SCORE_SIGMOID = 0, 1
+SAO_DISTILL_MAX_K, SAO_BALANCE_MAX_EXPERTS = 1024, 1024
 STATUS = {0: "SAO_OK", 1: "SAO_ERR_INVALID_ARG", 2: "SAO_ERR_SHAPE", 3: "SAO_ERR_WORKSPACE",
           4: "SAO_ERR_UNSUPPORTED", 5: "SAO_ERR_CUDA", 6: "SAO_ERR_DEVICE_CHECK"}
 FLAG_IN, FLAG_LOW, FLAG_HIGH, FLAG_NONFINITE, FLAG_NOT_ACTION = 0, 1, 2, 3, 4
@@ -33,6 +35,8 @@ EXPORTS = ("sao_version", "sao_last_error_string", "sao_set_checked", "sao_get_c
            "sao_group_advantages", "sao_running_mean_advantages", "sao_decoupled_loss_fwd",
            "sao_decoupled_loss_bwd", "sao_logprob_cache_bytes", "sao_token_logprobs_fwd_cached",
            "sao_token_logprobs_bwd_cached",
+           "sao_distill_workspace_bytes", "sao_distill_loss_fwd", "sao_distill_loss_bwd",
+           "sao_balance_workspace_bytes", "sao_balance_loss_fwd", "sao_balance_loss_bwd",
            "sao_value_loss", "sao_profile_enable", "sao_profile_reset", "sao_profile_read")
 
 
@@ -87,6 +91,16 @@ def load(path: Optional[str] = None):
         "sao_clip_loss_bwd": (ctypes.c_int, [P, P, P, P, P, I32, I64, F, F, ctypes.c_int, P, P, P, SZ, P]),
         "sao_group_advantages": (ctypes.c_int, [P, P, I32, P, P, I64, F, P, P, SZ, P]),
         "sao_running_mean_advantages": (ctypes.c_int, [P, P, I32, I32, P, P, I32, P, P, I64, P, P, SZ, P]),
+        "sao_distill_workspace_bytes": (SZ, [I64, I32, I32, I32, ctypes.c_int]),
+        "sao_distill_loss_fwd": (ctypes.c_int, [P, P, ctypes.c_int, P, P, ctypes.c_int, P, P, I64, I32, I32, I32, F, P,
+                                                P, P, P, P, SZ, P]),
+        "sao_distill_loss_bwd": (ctypes.c_int, [P, P, ctypes.c_int, P, P, ctypes.c_int, P, P, P, P, P, I64, I32, I32,
+                                                I32, F, P, P, ctypes.c_int, ctypes.c_int, P, SZ, P]),
+        "sao_balance_workspace_bytes": (SZ, [I64, I32, I32]),
+        "sao_balance_loss_fwd": (ctypes.c_int, [P, ctypes.c_int, P, P, P, I32, I64, I32, I32, ctypes.c_int, P, P, P, P,
+                                                P, SZ, P]),
+        "sao_balance_loss_bwd": (ctypes.c_int, [P, ctypes.c_int, P, P, I32, I64, I32, I32, ctypes.c_int, P, P, P, P, P,
+                                                SZ, P]),
         "sao_profile_enable": (None, [ctypes.c_int]),
         "sao_profile_reset": (None, []),
         "sao_profile_read": (ctypes.c_int, [P, P, P, ctypes.c_int]),
@@ -153,7 +167,7 @@ def _dtype_code(t: torch.Tensor) -> int:
         return SAO_BF16
     if t.dtype is _F32:
         return SAO_F32
-    raise ValueError(f"H and W must be bf16 or fp32, got {t.dtype}")
+    raise ValueError(f"bf16 or fp32 expected, got {t.dtype}")
 
 
 _F32, _F64, _BF16 = torch.float32, torch.float64, torch.bfloat16
@@ -408,6 +422,92 @@ def sao_running_mean_advantages(rewards, prompt_ids, history, seen, loss_mask, c
                                               _arg(loss_mask, _U8, N, "loss_mask"),
                                               _arg(cu_seqlens, _I32, B + 1, "cu_seqlens"), N,
                                               _arg(adv, _F32, N, "adv"), _ptr(ws), ws.numel(), _stream(stream)))
+
+
+def sao_distill_workspace_bytes(N: int, h: int, V: int, K: int, dtype=torch.bfloat16) -> int:
+    code = SAO_BF16 if dtype == torch.bfloat16 else SAO_F32
+    return int(load().sao_distill_workspace_bytes(int(N), int(h), int(V), int(K), code))
+
+
+def distill_workspace(N: int, h: int, V: int, K: int, dtype=torch.bfloat16, device=None) -> torch.Tensor:
+    """Allocate the workspace of sao_distill_loss_fwd/bwd."""
+    n = sao_distill_workspace_bytes(N, h, V, K, dtype)
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=device or "cuda")
+
+
+def _entries(top_ids, top_logits, N):
+    """K of the teacher's entries [N, K] and the code of their logits' dtype."""
+    if top_ids.dim() != 2 or top_ids.shape[0] != N or top_logits.shape != top_ids.shape:
+        raise ValueError("top_ids and top_logits must be [N, K]")
+    if top_logits.dtype is not _F32 and top_logits.dtype is not _BF16:
+        raise ValueError(f"top_logits must be bf16 or fp32, got {top_logits.dtype}")
+    return top_ids.shape[1], _dtype_code(top_logits)
+
+
+def sao_distill_loss_fwd(H, W, top_ids, top_logits, temperature, loss, lse, lse_rest, z_top, ws, teacher_lse=None,
+                         row_mask=None, stream=None):
+    N, h, V = _head(H, W)
+    K, code = _entries(top_ids, top_logits, N)
+    _check(load().sao_distill_loss_fwd(_ptr(H), _ptr(W), _dtype_code(H), _arg(top_ids, _I32, N * K, "top_ids"),
+                                       _ptr(top_logits), code, _arg(teacher_lse, _F32, N, "teacher_lse"),
+                                       _arg(row_mask, _U8, N, "row_mask"), N, h, V, K, float(temperature),
+                                       _arg(loss, _F32, N, "loss"), _arg(lse, _F32, N, "lse"),
+                                       _arg(lse_rest, _F32, N, "lse_rest"), _arg(z_top, _F32, N * K, "z_top"),
+                                       _ptr(ws), ws.numel(), _stream(stream)))
+
+
+def sao_distill_loss_bwd(H, W, top_ids, top_logits, temperature, lse, lse_rest, z_top, grad_loss, dH, dW, ws,
+                         teacher_lse=None, accumulate_dW=False, stream=None):
+    """dW fp32, or bf16 for a bf16 head (overwritten only)."""
+    N, h, V = _head(H, W)
+    K, code = _entries(top_ids, top_logits, N)
+    if dH.dtype is not H.dtype or tuple(dH.shape) != (N, h):
+        raise ValueError("dH must be [N, h] with the dtype of H")
+    if tuple(dW.shape) != (V, h):
+        raise ValueError("dW must be [V, h]")
+    _check(load().sao_distill_loss_bwd(_ptr(H), _ptr(W), _dtype_code(H), _arg(top_ids, _I32, N * K, "top_ids"),
+                                       _ptr(top_logits), code, _arg(teacher_lse, _F32, N, "teacher_lse"),
+                                       _arg(lse, _F32, N, "lse"), _arg(lse_rest, _F32, N, "lse_rest"),
+                                       _arg(z_top, _F32, N * K, "z_top"), _arg(grad_loss, _F32, N, "grad_loss"), N, h,
+                                       V, K, float(temperature), _ptr(dH), _ptr(dW), _dtype_code(dW),
+                                       1 if accumulate_dW else 0, _ptr(ws), ws.numel(), _stream(stream)))
+
+
+def sao_balance_workspace_bytes(N: int, E: int, B: int = 1) -> int:
+    return int(load().sao_balance_workspace_bytes(int(N), int(E), int(B)))
+
+
+def balance_workspace(N: int, E: int, B: int = 1, device=None) -> torch.Tensor:
+    """Allocate the workspace of sao_balance_loss_fwd/bwd (B trajectories, or 1 for the batch)."""
+    return torch.empty(max(sao_balance_workspace_bytes(N, E, B), 256), dtype=torch.uint8, device=device or "cuda")
+
+
+def sao_balance_loss_fwd(logits, expert_ids, score, loss, counts, prob_sums, rows, ws, row_mask=None, cu_seqlens=None,
+                         stream=None):
+    N, E = logits.shape
+    if expert_ids.dim() != 2 or expert_ids.shape[0] != N:
+        raise ValueError("expert_ids must be [N, k]")
+    k = expert_ids.shape[1]
+    B = 1 if cu_seqlens is None else cu_seqlens.numel() - 1
+    _check(load().sao_balance_loss_fwd(_ptr(logits), _dtype_code(logits), _arg(expert_ids, _I32, N * k, "expert_ids"),
+                                       _arg(row_mask, _U8, N, "row_mask"),
+                                       _arg(cu_seqlens, _I32, B + 1, "cu_seqlens"), B, N, E, k, int(score),
+                                       _arg(loss, _F32, 1, "loss"), _arg(counts, _I64, B * E, "counts"),
+                                       _arg(prob_sums, _F32, B * E, "prob_sums"), _arg(rows, _I64, B, "rows"),
+                                       _ptr(ws), ws.numel(), _stream(stream)))
+
+
+def sao_balance_loss_bwd(logits, k, score, counts, rows, grad_loss, grad_logits, ws, row_mask=None, cu_seqlens=None,
+                         stream=None):
+    """k: the experts chosen per token, as in the forward's expert_ids [N, k]."""
+    N, E = logits.shape
+    B = 1 if cu_seqlens is None else cu_seqlens.numel() - 1
+    _check(load().sao_balance_loss_bwd(_ptr(logits), _dtype_code(logits), _arg(row_mask, _U8, N, "row_mask"),
+                                       _arg(cu_seqlens, _I32, B + 1, "cu_seqlens"), B, N, E, int(k), int(score),
+                                       _arg(counts, _I64, B * E, "counts"), _arg(rows, _I64, B, "rows"),
+                                       _arg(grad_loss, _F32, 1, "grad_loss"),
+                                       _arg(grad_logits, logits.dtype, N * E, "grad_logits"), _ptr(ws), ws.numel(),
+                                       _stream(stream)))
 
 
 # ---------------------------------------------------------------------------
