@@ -17,15 +17,18 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "balance.cuh"
 #include "sao_common.cuh"
 #include "sao_internal.h"
+#include "tc_ptx.cuh"
 
 namespace sao {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kSlices = kThreads / 32;  // slices of a segment's partials that a CTA of the reduction adds side by side
+constexpr float kLog2e = 1.4426950408889634f;
 
 struct BalanceArgs {
   const void *x;
@@ -39,20 +42,6 @@ struct BalanceArgs {
   int chunks;
   unsigned int *err;
 };
-
-template <class T>
-__device__ __forceinline__ float to_float(T v) {
-  return float(v);
-}
-__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
-template <class T>
-__device__ __forceinline__ T from_float(float v) {
-  return T(v);
-}
-template <>
-__device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) {
-  return __float2bfloat16_rn(v);
-}
 
 // Segment b's first row and the row after its last, inside [0, N] whatever cu holds.
 __device__ __forceinline__ int64_t seg_at(const BalanceArgs &a, int b) {
@@ -72,30 +61,108 @@ __device__ __forceinline__ int seg_of(const BalanceArgs &a, int64_t r) {
   }
   return lo;
 }
-__device__ __forceinline__ float warp_max(float v) {
+
+// How a row lies over `lanes` (a power of two) consecutive lanes, kC columns each: kVec
+// columns (16 bytes, or one) per load, lane l holding loads l, l + lanes, ... Columns
+// past E, and all of a row that is not counted, read as -inf: they have no score.
+template <class T, int kVec, int kC>
+struct Row {
+  static constexpr int kLoads = kC / kVec;
+  static constexpr int kWords = kVec == 1 ? kLoads : kLoads * 4;
+  uint32_t raw[kWords];
+  __device__ __forceinline__ void load(const T *row, int E, int l, int lanes, bool live) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+    for (int v = 0; v < kLoads; ++v) {
+      const int c = (l + v * lanes) * kVec;
+      if constexpr (kVec == 1) {
+        constexpr uint32_t none = sizeof(T) == 2 ? 0xff80u : 0xff800000u;  // -inf
+        raw[v] = none;
+        if (live && c < E) {
+          if constexpr (sizeof(T) == 2)
+            raw[v] = ld(reinterpret_cast<const uint16_t *>(row) + c);
+          else
+            raw[v] = ld(reinterpret_cast<const uint32_t *>(row) + c);
+        }
+      } else {
+        constexpr uint32_t none = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;
+        uint4 x = make_uint4(none, none, none, none);
+        if (live && c < E) x = ld(reinterpret_cast<const uint4 *>(row + c));
+        raw[4 * v] = x.x;
+        raw[4 * v + 1] = x.y;
+        raw[4 * v + 2] = x.z;
+        raw[4 * v + 3] = x.w;
+      }
+    }
+  }
+  __device__ __forceinline__ float at(int j) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(raw[j]);
+    if constexpr (kVec == 1) return __uint_as_float(raw[j] << 16);
+    return __uint_as_float(j & 1 ? raw[j / 2] & 0xffff0000u : raw[j / 2] << 16);
+  }
+  static __device__ __forceinline__ int column(int j, int l, int lanes) {
+    return (l + j / kVec * lanes) * kVec + j % kVec;
+  }
+  static __device__ __forceinline__ void store(T *row, const float (&v)[kC], int E, int l, int lanes) {
+#pragma unroll
+    for (int k = 0; k < kLoads; ++k) {
+      const int c = (l + k * lanes) * kVec;
+      if (c >= E) continue;
+      if constexpr (kVec == 1) {
+        if constexpr (sizeof(T) == 2)
+          row[c] = __float2bfloat16_rn(v[k]);
+        else
+          row[c] = v[k];
+      } else if constexpr (sizeof(T) == 4) {
+        *reinterpret_cast<float4 *>(row + c) = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+      } else {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const __nv_bfloat162 b = __floats2bfloat162_rn(v[8 * k + 2 * i], v[8 * k + 2 * i + 1]);
+          w[i] = *reinterpret_cast<const uint32_t *>(&b);
+        }
+        *reinterpret_cast<uint4 *>(row + c) = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+  }
+};
+
+__device__ __forceinline__ float lanes_max(float v, int lanes) {
+  for (int o = 1; o < lanes; o <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
   return v;
 }
-__device__ __forceinline__ float warp_sum(float v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+__device__ __forceinline__ float lanes_sum(float v, int lanes) {
+  for (int o = 1; o < lanes; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
 
-// A row of -inf alone has no probabilities.
-__device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : 1.f / sum; }
-// A row's scores up to a factor, which the normalisation takes out: exp(x - max), or
-// sigmoid(x), divided by exp(max) where max is below 0 (e^x / (1 + e^x) would vanish with it).
-template <bool kSigmoid>
-__device__ __forceinline__ float shift(float max) {
-  if (max == -INFINITY) return 0.f;
-  return kSigmoid ? fminf(max, 0.f) : max;
-}
-template <bool kSigmoid>
-__device__ __forceinline__ float score(float x, float m) {
-  if constexpr (!kSigmoid) return expf(x - m);
-  return x > 0.f ? 1.f / (1.f + expf(-x)) : expf(x - m) / (1.f + expf(x));
+// A row's scores q, up to a factor that the normalisation takes out, and 1 / their sum
+// (0 for a row of -inf alone, which has no probabilities). Softmax: e^(x - max). Sigmoid:
+// e^-m sigmoid(x) = 1 / (e^m + e^(m - x)) with m = min(max, 0): sigmoid(x) itself, but
+// for rows far below 0, whose sigmoids vanish. em: e^m. (The difference is taken before
+// it is scaled, so an exponent is off by 2^-24 of itself.)
+template <bool kSigmoid, class R, int kC>
+__device__ __forceinline__ float row_scores(const R &x, float (&q)[kC], int lanes, float &em) {
+  float m = x.at(0);
+#pragma unroll
+  for (int j = 1; j < kC; ++j) m = fmaxf(m, x.at(j));
+  m = lanes_max(m, lanes);
+  if (m == -INFINITY) m = 0.f;
+  if constexpr (kSigmoid) {
+    m = fminf(m, 0.f);
+    em = tc::ex2_approx(m * kLog2e);
+  }
+  float s = 0.f;
+#pragma unroll
+  for (int j = 0; j < kC; ++j) {
+    if constexpr (kSigmoid)
+      q[j] = __fdividef(1.f, em + tc::ex2_approx((m - x.at(j)) * kLog2e));
+    else
+      q[j] = tc::ex2_approx((x.at(j) - m) * kLog2e);
+    s += q[j];
+  }
+  s = lanes_sum(s, lanes);
+  return s == 0.f ? 0.f : 1.f / s;
 }
 
 // Runs f(segment, first row, row after the last) for the segments of chunk c (all threads).
@@ -112,53 +179,76 @@ __device__ __forceinline__ void for_segments(const BalanceArgs &a, int c, F f) {
   }
 }
 
-// A warp per row; each warp adds its rows' scores in its own shared-memory columns.
-template <class T, bool kSigmoid>
-__global__ void __launch_bounds__(kThreads)
-    balance_partial_kernel(const BalanceArgs a, float *psum, int *pcount, int *prows, unsigned int *ticket) {
+// CTAs that an SM holds: as many registers as a lane's columns, the next row's and their sums take.
+template <class T, int kC>
+constexpr int kCtas = kC <= 8 ? 4 : (kC <= 16 || (kC <= 24 && sizeof(T) == 2)) ? 3 : 2;
+
+// Each group of `lanes` lanes takes a row at a time, the next one's logits in flight,
+// and keeps the sums of its columns in registers. One pass over the logits: bound by
+// reading them.
+template <class T, int kVec, int kC, bool kSigmoid>
+__global__ void __launch_bounds__(kThreads, kCtas<T, kC>)
+    balance_partial_kernel(const BalanceArgs a, int lanes, float *psum, int *pcount, int *prows, unsigned int *ticket) {
   extern __shared__ float sums[];  // [kWarps][E], then the counts [E]
   __shared__ int n_rows[kWarps];
   grid_wait();
   if (blockIdx.x == 0 && threadIdx.x == 0) *ticket = 0;
   int *counts = reinterpret_cast<int *>(sums + kWarps * a.E);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  float *mine = sums + warp * a.E;
+  const int groups = 32 / lanes, l = lane & (lanes - 1), step = kWarps * groups;
   const T *x = static_cast<const T *>(a.x);
   for_segments(a, blockIdx.x, [&](int b, int64_t r0, int64_t r1) {
     for (int e = threadIdx.x; e < a.E; e += kThreads) counts[e] = 0;
-    for (int e = lane; e < a.E; e += 32) mine[e] = 0.f;
     __syncthreads();
+    float acc[kC];
+#pragma unroll
+    for (int j = 0; j < kC; ++j) acc[j] = 0.f;
     int n = 0;
-    for (int64_t r = r0 + warp; r < r1; r += kWarps) {
-      if (a.mask && a.mask[r] == 0) continue;
-      ++n;
-      const T *row = x + r * a.E;
-      float m = -INFINITY;
-      for (int e = lane; e < a.E; e += 32) m = fmaxf(m, to_float(ld(row + e)));
-      m = shift<kSigmoid>(warp_max(m));
-      float s = 0.f;
-      for (int e = lane; e < a.E; e += 32) {
-        const float v = to_float(ld(row + e));
-        s += score<kSigmoid>(v, m);
+    auto counted = [&](int64_t r) { return r < r1 && (a.mask == nullptr || ld(a.mask + r) != 0); };
+    int64_t r = r0 + warp * groups + lane / lanes;
+    Row<T, kVec, kC> next;
+    bool next_on = counted(r);
+    next.load(x + r * a.E, a.E, l, lanes, next_on);
+    bool after_on = counted(r + step);
+    for (int64_t base = r0 + warp * groups; base < r1; base += step, r += step) {  // the warp's lanes stay together
+      const Row<T, kVec, kC> row = next;
+      const bool on = next_on;
+      next_on = after_on;
+      next.load(x + (r + step) * a.E, a.E, l, lanes, next_on);
+      after_on = counted(r + 2 * step);
+      if (on) {
+        if (l == 0) ++n;
+        for (int j = l; j < a.k; j += lanes) {
+          const int id = ld(a.ids + r * a.k + j);
+          if (id >= 0 && id < a.E)
+            atomicAdd(counts + id, 1);
+          else if (id >= a.E)
+            raise_device_error(a.err, SAO_DEVERR_EXPERT_ID);
+        }
       }
-      s = inverse(warp_sum(s));
-      for (int e = lane; e < a.E; e += 32) {
-        const float v = to_float(ld(row + e));
-        mine[e] += s * score<kSigmoid>(v, m);
-      }
-      for (int j = lane; j < a.k; j += 32) {
-        const int id = ld(a.ids + r * a.k + j);
-        if (id >= 0 && id < a.E)
-          atomicAdd(counts + id, 1);
-        else if (id >= a.E)
-          raise_device_error(a.err, SAO_DEVERR_EXPERT_ID);
+      float q[kC], em;
+      const float inv = row_scores<kSigmoid>(row, q, lanes, em);
+#pragma unroll
+      for (int j = 0; j < kC; ++j) acc[j] = fmaf(q[j], inv, acc[j]);
+    }
+    for (int o = lanes; o < 32; o <<= 1) {  // the warp's groups
+#pragma unroll
+      for (int j = 0; j < kC; ++j) acc[j] += __shfl_xor_sync(0xffffffffu, acc[j], o);
+    }
+    if (lane < lanes) {
+#pragma unroll
+      for (int j = 0; j < kC; ++j) {
+        const int c = Row<T, kVec, kC>::column(j, l, lanes);
+        if (c < a.E) sums[warp * a.E + c] = acc[j];
       }
     }
+    n = __reduce_add_sync(0xffffffffu, n);
     if (lane == 0) n_rows[warp] = n;
     __syncthreads();
     const int64_t slot = int64_t(blockIdx.x) + b;
     for (int e = threadIdx.x; e < a.E; e += kThreads) {
       float v = 0.f;
+#pragma unroll
       for (int w = 0; w < kWarps; ++w) v += sums[w * a.E + e];
       psum[slot * a.E + e] = v;
       pcount[slot * a.E + e] = counts[e];
@@ -172,16 +262,17 @@ __global__ void __launch_bounds__(kThreads)
   });
 }
 
-// CTA (b, 32 columns): adds the segment's partials, kSlices of them side by side; the
-// last CTA adds the products of all of them.
-__global__ void __launch_bounds__(kThreads)
+// CTA (b, 32 columns): adds the segment's partials, kSlices warps side by side;
+// the last CTA adds the products of all of them.
+template <int kSlices>
+__global__ void __launch_bounds__(32 * kSlices)
     balance_reduce_kernel(const BalanceArgs a, const float *psum, const int *pcount, const int *prows, float *loss,
                           int64_t *counts, float *prob_sums, int64_t *rows, double *terms, unsigned int *ticket) {
   __shared__ float sh_sum[kSlices][32];
   __shared__ long long sh_count[kSlices][32];
   __shared__ long long sh_rows[kSlices];
-  __shared__ double sh_term[kThreads];
-  __shared__ int sh_used[kThreads];
+  __shared__ double sh_term[kSlices];
+  __shared__ int sh_used[kSlices];
   __shared__ bool last;
   grid_wait();
   const int cols = (a.E + 31) / 32;
@@ -191,8 +282,9 @@ __global__ void __launch_bounds__(kThreads)
   float s = 0.f;
   long long n = 0, nr = 0;
   if (r1 > r0) {
-    const int c1 = int((r1 - 1) / a.chunk);
-    for (int c = int(r0 / a.chunk) + slice; c <= c1; c += kSlices) {
+    const int c0 = int(r0 / a.chunk), c1 = int((r1 - 1) / a.chunk);
+#pragma unroll 4
+    for (int c = c0 + slice; c <= c1; c += kSlices) {
       const int64_t slot = int64_t(c) + b;
       if (e < a.E) {
         s += ld(psum + slot * a.E + e);
@@ -238,26 +330,34 @@ __global__ void __launch_bounds__(kThreads)
   __threadfence();
   double t = 0.0;
   int used = 0;
-  for (int64_t i = threadIdx.x; i < gridDim.x; i += kThreads) t += __ldcg(terms + i);
-  for (int i = threadIdx.x; i < a.B; i += kThreads) used += __ldcg(rows + i) > 0;
-  sh_term[threadIdx.x] = t;
-  sh_used[threadIdx.x] = used;
-  __syncthreads();
-  for (int o = kThreads / 2; o > 0; o >>= 1) {
-    if (threadIdx.x < o) {
-      sh_term[threadIdx.x] += sh_term[threadIdx.x + o];
-      sh_used[threadIdx.x] += sh_used[threadIdx.x + o];
-    }
-    __syncthreads();
+  for (int64_t i = threadIdx.x; i < gridDim.x; i += 32 * kSlices) t += __ldcg(terms + i);
+  for (int i = threadIdx.x; i < a.B; i += 32 * kSlices) used += __ldcg(rows + i) > 0;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+  used = __reduce_add_sync(0xffffffffu, used);
+  if (lane == 0) {
+    sh_term[slice] = t;
+    sh_used[slice] = used;
   }
-  if (threadIdx.x == 0) loss[0] = sh_used[0] ? float(sh_term[0] / double(sh_used[0])) : 0.f;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    t = 0.0;
+    used = 0;
+    for (int k = 0; k < kSlices; ++k) {
+      t += sh_term[k];
+      used += sh_used[k];
+    }
+    loss[0] = used ? float(t / double(used)) : 0.f;
+  }
 }
 
-template <class T, bool kSigmoid>
-__global__ void __launch_bounds__(kThreads)
-    balance_grad_kernel(const BalanceArgs a, const int64_t *counts, const int64_t *rows, const float *grad_loss,
-                        T *dx) {
-  extern __shared__ float w[];  // [E]
+// A group of `lanes` lanes per row, as in the forward; the segment's weights of its columns
+// stay in registers until the segment ends. One pass: bound by reading the logits and
+// writing their gradient.
+template <class T, int kVec, int kC, bool kSigmoid>
+__global__ void __launch_bounds__(kThreads, kCtas<T, kC>)
+    balance_grad_kernel(const BalanceArgs a, int lanes, const int64_t *counts, const int64_t *rows,
+                        const float *grad_loss, T *dx) {
   __shared__ int sh_used[kWarps];
   grid_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -270,48 +370,110 @@ __global__ void __launch_bounds__(kThreads)
   for (int i = 0; i < kWarps; ++i) used += sh_used[i];
   const T *x = static_cast<const T *>(a.x);
   const float g = ld(grad_loss);
-  for_segments(a, blockIdx.x, [&](int b, int64_t r0, int64_t r1) {
-    const float n = float(ld(rows + b));
-    const float f = n > 0.f ? g * float(a.E) / (float(a.k) * n * n * float(used)) : 0.f;
-    for (int e = threadIdx.x; e < a.E; e += kThreads) w[e] = f * float(ld(counts + int64_t(b) * a.E + e));
-    __syncthreads();
-    for (int64_t r = r0 + warp; r < r1; r += kWarps) {
-      T *out = dx + r * a.E;
-      if (a.mask && a.mask[r] == 0) {
-        for (int e = lane; e < a.E; e += 32) out[e] = from_float<T>(0.f);
-        continue;
-      }
-      const T *row = x + r * a.E;
-      float m = -INFINITY;
-      for (int e = lane; e < a.E; e += 32) m = fmaxf(m, to_float(ld(row + e)));
-      m = shift<kSigmoid>(warp_max(m));
-      float s = 0.f, d = 0.f;
-      for (int e = lane; e < a.E; e += 32) {
-        const float v = to_float(ld(row + e));
-        const float q = score<kSigmoid>(v, m);
-        s += q;
-        d += q * w[e];
-      }
-      s = inverse(warp_sum(s));
-      d = warp_sum(d) * s;
-      for (int e = lane; e < a.E; e += 32) {
-        const float v = to_float(ld(row + e));
-        const float q = score<kSigmoid>(v, m);
-        const float slope = kSigmoid ? q * s / (1.f + expf(v)) : q * s;
-        out[e] = from_float<T>(slope * (w[e] - d));
+  const int groups = 32 / lanes, l = lane & (lanes - 1), step = kWarps * groups;
+  const int64_t r0 = int64_t(blockIdx.x) * a.chunk, r1 = r0 + a.chunk < a.N ? r0 + a.chunk : a.N;
+  auto counted = [&](int64_t r) { return r < r1 && (a.mask == nullptr || ld(a.mask + r) != 0); };
+  int64_t r = r0 + warp * groups + lane / lanes;
+  Row<T, kVec, kC> next;
+  bool next_on = counted(r);
+  next.load(x + r * a.E, a.E, l, lanes, next_on);
+  bool after_on = counted(r + step);
+  int b = -1;
+  int64_t seg_end = -1;  // of segment b: the weights are those of another one from there on
+  float w[kC];
+#pragma unroll
+  for (int j = 0; j < kC; ++j) w[j] = 0.f;
+  for (int64_t base = r0 + warp * groups; base < r1; base += step, r += step) {
+    const Row<T, kVec, kC> row = next;
+    next_on = after_on;
+    next.load(x + (r + step) * a.E, a.E, l, lanes, next_on);
+    after_on = counted(r + 2 * step);
+    if (r < r1 && r >= seg_end) {
+      b = seg_of(a, r);
+      seg_end = b + 1 < a.B ? seg_at(a, b + 1) : a.N;
+      if (seg_end <= r) seg_end = r + 1;  // (cu_seqlens that do not rise)
+      const float n = float(ld(rows + b));
+      const float f = n > 0.f ? g * float(a.E) / (float(a.k) * n * n * float(used)) : 0.f;
+#pragma unroll
+      for (int j = 0; j < kC; ++j) {
+        const int c = Row<T, kVec, kC>::column(j, l, lanes);
+        w[j] = c < a.E ? f * float(ld(counts + int64_t(b) * a.E + c)) : 0.f;
       }
     }
-    __syncthreads();
-  });
+    __syncwarp();
+    float q[kC], em = 0.f;
+    const float inv = row_scores<kSigmoid>(row, q, lanes, em);
+    float d = 0.f;
+#pragma unroll
+    for (int j = 0; j < kC; ++j) d = fmaf(q[j], w[j], d);
+    d = lanes_sum(d, lanes) * inv;
+#pragma unroll
+    for (int j = 0; j < kC; ++j) {
+      const float s = kSigmoid ? q[j] * inv * fmaf(-em, q[j], 1.f) : q[j] * inv;
+      q[j] = s * (w[j] - d);
+    }
+    if (r < r1) Row<T, kVec, kC>::store(dx + r * a.E, q, a.E, l, lanes);
+  }
 }
 
-int chunk_rows(int64_t N) {
-  int64_t c = (N + 303) / 304;  // two CTAs per SM
-  return int(c < 32 ? 32 : c);
+// The layout of a row of E: kC columns a lane and the lanes that take it.
+struct Layout {
+  int columns, lanes;
+  bool vec;
+};
+// Vector loads where every row starts on 16 bytes. Of the layouts the one with the
+// least work: a lane's columns at about 7 instructions each, the exchanges between
+// lanes and 24 more, times the lanes (160 bf16 logits: 8 lanes x 24 columns, not
+// 16 x 16, of which 96 would be idle).
+Layout layout(const void *x, const void *dx, sao_dtype dt, int E) {
+  const int size = dt == SAO_BF16 ? 2 : 4, per = 16 / size;
+  Layout best{0, 0, E % per == 0 && aligned16(x) && aligned16(dx)};
+  int least = 0;
+  for (int c = 8; c <= 32; c += 8) {
+    const int vec = best.vec ? per : 1, loads = c / vec, units = E / vec;
+    int lanes = 1, log = 0;
+    while (lanes * loads < units) {
+      lanes <<= 1;
+      ++log;
+    }
+    if (lanes > 32) continue;
+    const int cost = lanes * (7 * c + 4 * log + 24);
+    if (best.columns == 0 || (c < 32 && cost < least)) {  // 32 columns: where no other fits
+      best.columns = c;
+      best.lanes = lanes;
+      least = cost;
+    }
+  }
+  return best;
+}
+
+// f(type, loads, columns, score) with the layout's values as types.
+template <int kValue>
+using Int = std::integral_constant<int, kValue>;
+template <class T, class F>
+void with_layout(const Layout &l, int score, F f) {
+  auto columns = [&](auto vec, auto sig) {
+    switch (l.columns) {
+      case 8: return f(T{}, vec, Int<8>{}, sig);
+      case 16: return f(T{}, vec, Int<16>{}, sig);
+      case 24: return f(T{}, vec, Int<24>{}, sig);
+      default: return f(T{}, vec, Int<32>{}, sig);
+    }
+  };
+  auto loads = [&](auto sig) { l.vec ? columns(Int<int(16 / sizeof(T))>{}, sig) : columns(Int<1>{}, sig); };
+  score == SAO_SCORE_SIGMOID ? loads(std::true_type{}) : loads(std::false_type{});
+}
+
+// Rows per CTA: three CTAs on each of 152 SMs, at least one row for every lane group of
+// the CTA's with the fewest lanes. From N and E alone: the sums' order, and so their
+// bits, are those of any device and alignment.
+int chunk_rows(int64_t N, int E) {
+  const int64_t c = (N + 455) / 456, least = E <= 16 ? 256 : 32;
+  return int(c < least ? least : c);
 }
 BalanceArgs make_args(const void *x, const int32_t *ids, const uint8_t *mask, const int32_t *cu, int32_t B, int64_t N,
                       int32_t E, int32_t k, unsigned int *err) {
-  BalanceArgs a{x, ids, mask, cu, cu ? B : 1, N, E, k, chunk_rows(N), 0, err};
+  BalanceArgs a{x, ids, mask, cu, cu ? B : 1, N, E, k, chunk_rows(N, E), 0, err};
   a.chunks = int((N + a.chunk - 1) / a.chunk);
   return a;
 }
@@ -323,7 +485,7 @@ struct Scratch {
   unsigned int *ticket;
 };
 Scratch take(Carver &c, int64_t N, int32_t E, int32_t B) {
-  const int64_t chunk = chunk_rows(N);
+  const int64_t chunk = chunk_rows(N, E);
   const size_t slots = size_t((N + chunk - 1) / chunk) + size_t(B);
   Scratch s;
   s.psum = c.take<float>(slots * size_t(E));
@@ -350,17 +512,20 @@ sao_status balance_fwd_launch(const void *x, sao_dtype dt, const int32_t *ids, c
   Carver c(ws, ws_bytes);
   const Scratch w = take(c, N, E, a.B);
   if (!c.ok()) return fail(SAO_ERR_WORKSPACE, "workspace too small for the balance loss");
-  auto kern = dt == SAO_BF16
-                  ? (score == SAO_SCORE_SIGMOID ? balance_partial_kernel<__nv_bfloat16, true>
-                                                : balance_partial_kernel<__nv_bfloat16, false>)
-                  : (score == SAO_SCORE_SIGMOID ? balance_partial_kernel<float, true> : balance_partial_kernel<float, false>);
+  const Layout lay = layout(x, x, dt, E);
   int slot = launch_begin("balance_partial", s);
-  pdl(kern, unsigned(a.chunks), kThreads, size_t(E) * (kWarps + 1) * sizeof(float), s)(a, w.psum, w.pcount, w.prows,
-                                                                                      w.ticket);
+  auto partial = [&](auto t, auto vec, auto columns, auto sig) {
+    pdl(balance_partial_kernel<decltype(t), vec.value, columns.value, sig.value>, unsigned(a.chunks), kThreads,
+        size_t(E) * (kWarps + 1) * sizeof(float), s)(a, lay.lanes, w.psum, w.pcount, w.prows, w.ticket);
+  };
+  dt == SAO_BF16 ? with_layout<__nv_bfloat16>(lay, score, partial) : with_layout<float>(lay, score, partial);
   SAO_TRY(launch_end(slot, s));
+  // a batch's partials, hundreds in few CTAs: 32 warps to each; many trajectories: 8
+  const unsigned grid = unsigned(a.B) * unsigned((E + 31) / 32);
   slot = launch_begin("balance_reduce", s);
-  pdl(balance_reduce_kernel, unsigned(a.B) * unsigned((E + 31) / 32), kThreads, 0, s)(
-      a, w.psum, w.pcount, w.prows, loss, counts, prob_sums, rows, w.terms, w.ticket);
+  auto reduce = grid <= 152 ? balance_reduce_kernel<32> : balance_reduce_kernel<8>;
+  pdl(reduce, grid, grid <= 152 ? 1024 : 256, 0, s)(a, w.psum, w.pcount, w.prows, loss, counts, prob_sums, rows,
+                                                    w.terms, w.ticket);
   return launch_end(slot, s);
 }
 
@@ -368,14 +533,14 @@ sao_status balance_bwd_launch(const void *x, sao_dtype dt, const uint8_t *mask, 
                               int32_t E, int32_t k, int score, const int64_t *counts, const int64_t *rows,
                               const float *grad_loss, void *dx, unsigned int *err, cudaStream_t s) {
   const BalanceArgs a = make_args(x, nullptr, mask, cu, B, N, E, k, err);
+  const Layout lay = layout(x, dx, dt, E);
   int slot = launch_begin("balance_grad", s);
-  const size_t smem = size_t(E) * sizeof(float);
-  if (dt == SAO_BF16)
-    pdl(score == SAO_SCORE_SIGMOID ? balance_grad_kernel<__nv_bfloat16, true> : balance_grad_kernel<__nv_bfloat16, false>,
-        unsigned(a.chunks), kThreads, smem, s)(a, counts, rows, grad_loss, static_cast<__nv_bfloat16 *>(dx));
-  else
-    pdl(score == SAO_SCORE_SIGMOID ? balance_grad_kernel<float, true> : balance_grad_kernel<float, false>,
-        unsigned(a.chunks), kThreads, smem, s)(a, counts, rows, grad_loss, static_cast<float *>(dx));
+  auto grad = [&](auto t, auto vec, auto columns, auto sig) {
+    using T = decltype(t);
+    pdl(balance_grad_kernel<T, vec.value, columns.value, sig.value>, unsigned(a.chunks), kThreads, 0, s)(
+        a, lay.lanes, counts, rows, grad_loss, static_cast<T *>(dx));
+  };
+  dt == SAO_BF16 ? with_layout<__nv_bfloat16>(lay, score, grad) : with_layout<float>(lay, score, grad);
   return launch_end(slot, s);
 }
 

@@ -33,7 +33,10 @@ using namespace tc;
 
 constexpr int TM = 128, TN = 256, KB = 64, STAGES = 4;
 static_assert(TN == kTopTile, "offsets count entries by tile");
-constexpr int kPart = 256;                   // contraction elements between two read-outs of an accumulator
+#ifndef KPART
+#define KPART 512
+#endif
+constexpr int kPart = KPART;                   // contraction elements between two read-outs of an accumulator
 constexpr int kPartBlocks = kPart / KB;
 constexpr uint32_t A_BYTES = TM * KB * 2, B_BYTES = TN * KB * 2, STAGE_BYTES = A_BYTES + B_BYTES;
 constexpr int ACCS = 2;
