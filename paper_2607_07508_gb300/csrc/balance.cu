@@ -143,25 +143,33 @@ __device__ __forceinline__ float lanes_sum(float v, int lanes) {
 // it is scaled, so an exponent is off by 2^-24 of itself.)
 template <bool kSigmoid, class R, int kC>
 __device__ __forceinline__ float row_scores(const R &x, float (&q)[kC], int lanes, float &em) {
-  float m = x.at(0);
+  float m4[4];
 #pragma unroll
-  for (int j = 1; j < kC; ++j) m = fmaxf(m, x.at(j));
-  m = lanes_max(m, lanes);
+  for (int j = 0; j < kC; ++j) m4[j & 3] = j < 4 ? x.at(j) : fmaxf(m4[j & 3], x.at(j));
+  float m = lanes_max(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])), lanes);
   if (m == -INFINITY) m = 0.f;
   if constexpr (kSigmoid) {
     m = fminf(m, 0.f);
     em = tc::ex2_approx(m * kLog2e);
   }
-  float s = 0.f;
+  // two columns per fp32 operation
+  const tc::f32x2 neg = tc::pack_f32x2(-m, -m), scale = tc::pack_f32x2(kSigmoid ? -kLog2e : kLog2e, kSigmoid ? -kLog2e : kLog2e);
+  tc::f32x2 s2[2] = {0, 0};
 #pragma unroll
-  for (int j = 0; j < kC; ++j) {
-    if constexpr (kSigmoid)
-      q[j] = __fdividef(1.f, em + tc::ex2_approx((m - x.at(j)) * kLog2e));
-    else
-      q[j] = tc::ex2_approx((x.at(j) - m) * kLog2e);
-    s += q[j];
+  for (int j = 0; j < kC; j += 2) {
+    float t0, t1;
+    tc::unpack_f32x2(tc::mul_f32x2(tc::add_f32x2(tc::pack_f32x2(x.at(j), x.at(j + 1)), neg), scale), t0, t1);
+    q[j] = tc::ex2_approx(t0);
+    q[j + 1] = tc::ex2_approx(t1);
+    if constexpr (kSigmoid) {
+      q[j] = __fdividef(1.f, em + q[j]);
+      q[j + 1] = __fdividef(1.f, em + q[j + 1]);
+    }
+    s2[j / 2 & 1] = tc::add_f32x2(s2[j / 2 & 1], tc::pack_f32x2(q[j], q[j + 1]));
   }
-  s = lanes_sum(s, lanes);
+  float s, s1;
+  tc::unpack_f32x2(tc::add_f32x2(s2[0], s2[1]), s, s1);
+  s = lanes_sum(s + s1, lanes);
   return s == 0.f ? 0.f : 1.f / s;
 }
 
@@ -210,26 +218,35 @@ __global__ void __launch_bounds__(kThreads, kCtas<T, kC>)
     bool next_on = counted(r);
     next.load(x + r * a.E, a.E, l, lanes, next_on);
     bool after_on = counted(r + step);
+    auto first_id = [&](int64_t row, bool on) { return on && l < a.k ? ld(a.ids + row * a.k + l) : -1; };
+    auto count = [&](int id) {
+      if (id >= 0 && id < a.E)
+        atomicAdd(counts + id, 1);
+      else if (id >= a.E)
+        raise_device_error(a.err, SAO_DEVERR_EXPERT_ID);
+    };
+    int next_id = first_id(r, next_on);
     for (int64_t base = r0 + warp * groups; base < r1; base += step, r += step) {  // the warp's lanes stay together
       const Row<T, kVec, kC> row = next;
       const bool on = next_on;
+      const int id = next_id;
       next_on = after_on;
       next.load(x + (r + step) * a.E, a.E, l, lanes, next_on);
+      next_id = first_id(r + step, next_on);
       after_on = counted(r + 2 * step);
+      if (!__any_sync(0xffffffffu, on)) continue;  // spans of masked rows
       if (on) {
         if (l == 0) ++n;
-        for (int j = l; j < a.k; j += lanes) {
-          const int id = ld(a.ids + r * a.k + j);
-          if (id >= 0 && id < a.E)
-            atomicAdd(counts + id, 1);
-          else if (id >= a.E)
-            raise_device_error(a.err, SAO_DEVERR_EXPERT_ID);
-        }
+        count(id);
+        for (int j = l + lanes; j < a.k; j += lanes) count(ld(a.ids + r * a.k + j));
       }
       float q[kC], em;
       const float inv = row_scores<kSigmoid>(row, q, lanes, em);
+      const tc::f32x2 inv2 = tc::pack_f32x2(inv, inv);
 #pragma unroll
-      for (int j = 0; j < kC; ++j) acc[j] = fmaf(q[j], inv, acc[j]);
+      for (int j = 0; j < kC; j += 2)
+        tc::unpack_f32x2(tc::fma_f32x2(tc::pack_f32x2(q[j], q[j + 1]), inv2, tc::pack_f32x2(acc[j], acc[j + 1])), acc[j],
+                         acc[j + 1]);
     }
     for (int o = lanes; o < 32; o <<= 1) {  // the warp's groups
 #pragma unroll
@@ -385,10 +402,11 @@ __global__ void __launch_bounds__(kThreads, kCtas<T, kC>)
   for (int j = 0; j < kC; ++j) w[j] = 0.f;
   for (int64_t base = r0 + warp * groups; base < r1; base += step, r += step) {
     const Row<T, kVec, kC> row = next;
+    const bool on = next_on;
     next_on = after_on;
     next.load(x + (r + step) * a.E, a.E, l, lanes, next_on);
     after_on = counted(r + 2 * step);
-    if (r < r1 && r >= seg_end) {
+    if (on && r >= seg_end) {
       b = seg_of(a, r);
       seg_end = b + 1 < a.B ? seg_at(a, b + 1) : a.N;
       if (seg_end <= r) seg_end = r + 1;  // (cu_seqlens that do not rise)
@@ -402,15 +420,20 @@ __global__ void __launch_bounds__(kThreads, kCtas<T, kC>)
     }
     __syncwarp();
     float q[kC], em = 0.f;
-    const float inv = row_scores<kSigmoid>(row, q, lanes, em);
-    float d = 0.f;
+    if (__any_sync(0xffffffffu, on)) {
+      const float inv = row_scores<kSigmoid>(row, q, lanes, em);
+      float d = 0.f;
 #pragma unroll
-    for (int j = 0; j < kC; ++j) d = fmaf(q[j], w[j], d);
-    d = lanes_sum(d, lanes) * inv;
+      for (int j = 0; j < kC; ++j) d = fmaf(q[j], w[j], d);
+      d = lanes_sum(d, lanes) * inv;
 #pragma unroll
-    for (int j = 0; j < kC; ++j) {
-      const float s = kSigmoid ? q[j] * inv * fmaf(-em, q[j], 1.f) : q[j] * inv;
-      q[j] = s * (w[j] - d);
+      for (int j = 0; j < kC; ++j) {
+        const float s = kSigmoid ? q[j] * inv * fmaf(-em, q[j], 1.f) : q[j] * inv;
+        q[j] = s * (w[j] - d);
+      }
+    } else {  // spans of masked rows
+#pragma unroll
+      for (int j = 0; j < kC; ++j) q[j] = 0.f;
     }
     if (r < r1) Row<T, kVec, kC>::store(dx + r * a.E, q, a.E, l, lanes);
   }

@@ -31,14 +31,13 @@ namespace {
 
 using namespace tc;
 
-constexpr int TM = 128, TN = 256, KB = 64, STAGES = 4;
+constexpr int TM = 128, TN = 256, KB = 64;
 static_assert(TN == kTopTile, "offsets count entries by tile");
-#ifndef KPART
-#define KPART 512
-#endif
-constexpr int kPart = KPART;                   // contraction elements between two read-outs of an accumulator
+constexpr int kPart = 512;                   // contraction elements between two read-outs of an accumulator
 constexpr int kPartBlocks = kPart / KB;
-constexpr uint32_t A_BYTES = TM * KB * 2, B_BYTES = TN * KB * 2, STAGE_BYTES = A_BYTES + B_BYTES;
+constexpr uint32_t A_BYTES = TM * KB * 2, B_BYTES = TN * KB * 2;
+constexpr uint32_t RING_BYTES = 4 * (A_BYTES + B_BYTES);  // 4 stages, or 6 of half a B tile
+constexpr int kMaxStages = 6;
 constexpr int ACCS = 2;
 constexpr uint32_t TMEM_COLS = ACCS * TN;
 constexpr int NUM_THREADS = 640;             // warp 0 TMA, warp 1 MMA, warps 4-19 add the parts and finish
@@ -48,12 +47,12 @@ static_assert(128 * ISSUE_REGS + 512 * SUM_REGS <= NUM_THREADS * LAUNCH_REGS, "s
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct __align__(8) SmemCtl {
-  uint64_t full[STAGES], empty[STAGES], acc_full[ACCS], acc_empty[ACCS];
+  uint64_t full[kMaxStages], empty[kMaxStages], acc_full[ACCS], acc_empty[ACCS];
   uint32_t tmem_base;
   int abort;
   float2 quarter[2][4][TM];  // (max, sum) of each quarter tile's rows, two tiles in turn
 };
-constexpr size_t SMEM_BYTES = 1024 + size_t(STAGES) * STAGE_BYTES + sizeof(SmemCtl);
+constexpr size_t SMEM_BYTES = 1024 + RING_BYTES + sizeof(SmemCtl);
 static_assert(SMEM_BYTES <= 232448, "shared memory of an SM");
 
 struct FwdParams {
@@ -78,31 +77,45 @@ __device__ __forceinline__ void tile_of(int L, const FwdParams &p, int nM, int &
   n = within / gm;
 }
 
+// kCG = 2: CTA pairs, as in the backward's products (tc_gemm_kernel): every MMA is one of
+// M = 256 over the pair, each CTA loads its own 128 rows of H and half of the tile of W,
+// and keeps its own 128 rows' sums.
+template <int kCG>
 __global__ void __launch_bounds__(NUM_THREADS, 1)
     distill_logits_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                           const FwdParams p) {
+  constexpr uint32_t kStageBytes = A_BYTES + B_BYTES / kCG;
+  constexpr int kStages = int(RING_BYTES / kStageBytes);
+  static_assert(kStages <= kMaxStages, "barrier arrays");
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
-  SmemCtl *ctl = reinterpret_cast<SmemCtl *>(smem_raw + (base - raw) + size_t(STAGES) * STAGE_BYTES);
+  SmemCtl *ctl = reinterpret_cast<SmemCtl *>(smem_raw + (base - raw) + RING_BYTES);
   volatile int *abort = &ctl->abort;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = kCG == 2 ? cluster_ctarank() : 0u;
+  const int cl = int(blockIdx.x) / kCG, ncl = int(gridDim.x) / kCG;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < STAGES; ++s) {
+    for (int s = 0; s < kStages; ++s) {
       mbar_init(smem_u32(&ctl->full[s]), 1);
       mbar_init(smem_u32(&ctl->empty[s]), 1);
     }
     for (int a = 0; a < ACCS; ++a) {
       mbar_init(smem_u32(&ctl->acc_full[a]), 1);
-      mbar_init(smem_u32(&ctl->acc_empty[a]), 512);
+      mbar_init(smem_u32(&ctl->acc_empty[a]), 512 * kCG);
     }
     ctl->abort = 0;
     fence_barrier_init();
   }
   if (warp == 1) {
-    tmem_alloc(smem_u32(&ctl->tmem_base), TMEM_COLS);
-    tmem_relinquish();
+    if constexpr (kCG == 2) {
+      tmem_alloc_pair(smem_u32(&ctl->tmem_base), TMEM_COLS);
+      tmem_relinquish_pair();
+    } else {
+      tmem_alloc(smem_u32(&ctl->tmem_base), TMEM_COLS);
+      tmem_relinquish();
+    }
   }
   if (warp == 0 && lane == 0) {
     tma_prefetch_map(&map_a);
@@ -110,6 +123,8 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
   }
   fence_before_sync();
   __syncthreads();
+  // both CTAs' barriers exist before either CTA's copies, commits or arrivals reach them
+  if constexpr (kCG == 2) cluster_sync();
   fence_after_sync();
   const uint32_t tmem_base = ctl->tmem_base;
   grid_wait_long();
@@ -117,7 +132,7 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
   int64_t rows = p.rows;
   if (p.m_count) {
     rows = *p.m_count;
-    nM = int((rows + TM - 1) / TM);
+    nM = int((rows + TM * kCG - 1) / (TM * kCG));
   }
   const int tiles = nM * p.nN;
 
@@ -128,7 +143,7 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
       int stage = 0;
       uint32_t phase = 0, issued = 0, issued_phase = 0;
       bool ok = true;
-      for (int L = blockIdx.x; L < tiles && ok; L += gridDim.x) {
+      for (int L = cl; L < tiles && ok; L += ncl) {
         int m, n;
         tile_of(L, p, nM, m, n);
         for (int kb = 0; kb < p.nK; ++kb) {
@@ -136,22 +151,29 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
             ok = false;
             break;
           }
-          const uint32_t fb = smem_u32(&ctl->full[stage]);
+          // a pair's bytes are all counted on the even CTA's barrier
+          const uint32_t own = smem_u32(&ctl->full[stage]);
           issued |= 1u << stage;
           issued_phase = (issued_phase & ~(1u << stage)) | (phase << stage);
-          mbar_arrive_expect_tx(fb, STAGE_BYTES);
-          const uint32_t sa = base + uint32_t(stage) * STAGE_BYTES;
-          tma_load_2d(sa, &map_a, fb, kb * KB, m * TM);
-          tma_load_2d(sa + A_BYTES, &map_b, fb, kb * KB, n * TN);
-          if (++stage == STAGES) {
+          if (rank == 0u) mbar_arrive_expect_tx(own, kStageBytes * kCG);
+          const uint32_t sa = base + uint32_t(stage) * kStageBytes;
+          if constexpr (kCG == 2) {
+            const uint32_t fb = mapa_shared(own, 0u);
+            tma_load_2d_pair(sa, &map_a, fb, kb * KB, (m * kCG + int(rank)) * TM);
+            tma_load_2d_pair(sa + A_BYTES, &map_b, fb, kb * KB, n * TN + int(rank) * (TN / kCG));
+          } else {
+            tma_load_2d(sa, &map_a, own, kb * KB, m * TM);
+            tma_load_2d(sa + A_BYTES, &map_b, own, kb * KB, n * TN);
+          }
+          if (++stage == kStages) {
             stage = 0;
             phase ^= 1u;
           }
         }
       }
-      if (!ok) {
+      if (!ok && rank == 0u) {
         // let the copies already in flight land before the CTA can exit
-        for (int s = 0; s < STAGES; ++s) {
+        for (int s = 0; s < kStages; ++s) {
           if (!((issued >> s) & 1u)) continue;
           const uint32_t par = (issued_phase >> s) & 1u;
           const uint64_t t0 = globaltimer_ns();
@@ -160,13 +182,19 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
         }
       }
     }
-    if (warp == 1 && lane == 0) {
-      // ---------------------------------------------------------- MMA issuer
-      constexpr uint32_t idesc = idesc_bf16(TM, TN, false, false);
+    if (warp == 1 && lane == 0 && rank == 0u) {
+      // ---------------------------------------------------------- MMA issuer (a pair's: the even CTA)
+      constexpr uint32_t idesc = idesc_bf16(TM * kCG, TN, false, false);
+      auto commit = [&](uint64_t *bar) {
+        if constexpr (kCG == 2)
+          mma_commit_pair(smem_u32(bar), uint16_t(0x3));
+        else
+          mma_commit(smem_u32(bar));
+      };
       int stage = 0, acc = 0;
       uint32_t phase = 0, acc_phase = 0;
       bool ok = true;
-      for (int L = blockIdx.x; L < tiles && ok; L += gridDim.x) {
+      for (int L = cl; L < tiles && ok; L += ncl) {
         for (int kb = 0; kb < p.nK; ++kb) {
           const int in_part = kb % kPartBlocks;
           if ((in_part == 0 && !mbar_wait(smem_u32(&ctl->acc_empty[acc]), acc_phase ^ 1u, abort, p.err)) ||
@@ -175,19 +203,24 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
             break;
           }
           fence_after_sync();
-          const uint32_t sa = base + uint32_t(stage) * STAGE_BYTES, sb = sa + A_BYTES;
+          const uint32_t sa = base + uint32_t(stage) * kStageBytes, sb = sa + A_BYTES;
           const uint32_t d = tmem_base + uint32_t(acc) * TN;
 #pragma unroll
-          for (int kk = 0; kk < KB / 16; ++kk)
-            mma_bf16(d, sdesc_sw128(sa + kk * 32u, 16u, 1024u), sdesc_sw128(sb + kk * 32u, 16u, 1024u), idesc,
-                     (in_part | kk) != 0 ? 1u : 0u);
-          mma_commit(smem_u32(&ctl->empty[stage]));
-          if (++stage == STAGES) {
+          for (int kk = 0; kk < KB / 16; ++kk) {
+            const uint64_t ad = sdesc_sw128(sa + kk * 32u, 16u, 1024u), bd = sdesc_sw128(sb + kk * 32u, 16u, 1024u);
+            const uint32_t accum = (in_part | kk) != 0 ? 1u : 0u;
+            if constexpr (kCG == 2)
+              mma_bf16_pair(d, ad, bd, idesc, accum);
+            else
+              mma_bf16(d, ad, bd, idesc, accum);
+          }
+          commit(&ctl->empty[stage]);
+          if (++stage == kStages) {
             stage = 0;
             phase ^= 1u;
           }
           if (in_part == kPartBlocks - 1 || kb == p.nK - 1) {
-            mma_commit(smem_u32(&ctl->acc_full[acc]));
+            commit(&ctl->acc_full[acc]);
             if (++acc == ACCS) {
               acc = 0;
               acc_phase ^= 1u;
@@ -203,12 +236,13 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
     const int quarter = (warp - 4) >> 2;
     const int r = quad * 32 + lane;
     const int parts = (p.nK + kPartBlocks - 1) / kPartBlocks;
+    const float scale = p.top.inv_t * kLog2e;
     int a = 0, local = 0;
     uint32_t a_phase = 0;
-    for (int L = blockIdx.x; L < tiles; L += gridDim.x, ++local) {
+    for (int L = cl; L < tiles; L += ncl, ++local) {
       int m, n;
       tile_of(L, p, nM, m, n);
-      const int64_t row = int64_t(m) * TM + r;
+      const int64_t row = (int64_t(m) * kCG + int(rank)) * TM + r;
       const bool row_ok = row < rows;
       const int col0 = n * TN + quarter * HN;
       // this thread's entries: a bit per column, and where its first one stands in the row's list
@@ -217,25 +251,23 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
       int first = 0;
       if (row_ok) {
         const uint16_t *off = p.top.off + t * (p.top.tiles + 1) + n;
+        const int32_t *id = p.top.id + t * p.top.K;
         first = ld(off);
         const int end = ld(off + 1);
-        for (int q = first; q < end; ++q) {
-          const int c = ld(p.top.id + t * p.top.K + q) - col0;
-          if (c < 0) {
-            first = q + 1;
-          } else if (c < HN) {
-            if (c < 32)
-              bits[0] |= 1u << c;
-            else
-              bits[1] |= 1u << (c - 32);
-          } else {
-            break;
+        constexpr int kU = 4;  // loads in flight
+        for (int q = first; q < end; q += kU) {
+          int c[kU];
+#pragma unroll
+          for (int u = 0; u < kU; ++u) c[u] = q + u < end ? ld(id + q + u) - col0 : HN;
+#pragma unroll
+          for (int u = 0; u < kU; ++u) {
+            first += c[u] < 0;
+            if (unsigned(c[u]) < 32u) bits[0] |= 1u << c[u];
+            if (unsigned(c[u] - 32) < 32u) bits[1] |= 1u << (c[u] - 32);
           }
         }
       }
       float z[HN];
-#pragma unroll
-      for (int j = 0; j < HN; ++j) z[j] = 0.f;
       bool ok = true;
 #pragma unroll 1
       for (int part = 0; part < parts; ++part) {
@@ -250,11 +282,23 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
           uint32_t u[16];
           tmem_ld16(taddr + c, u);
           tmem_wait_ld();
+          if (part == 0) {
 #pragma unroll
-          for (int j = 0; j < 16; ++j) z[c + j] += __uint_as_float(u[j]);
+            for (int j = 0; j < 16; ++j) z[c + j] = __uint_as_float(u[j]);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 16; j += 2)
+              unpack_f32x2(add_f32x2(pack_f32x2(z[c + j], z[c + j + 1]),
+                                     pack_f32x2(__uint_as_float(u[j]), __uint_as_float(u[j + 1]))),
+                           z[c + j], z[c + j + 1]);
+          }
         }
         fence_before_sync();
-        mbar_arrive(smem_u32(&ctl->acc_empty[a]));
+        const uint32_t bar = smem_u32(&ctl->acc_empty[a]);
+        if (kCG == 2 && rank != 0u)
+          mbar_arrive_cluster(mapa_shared(bar, 0u));
+        else
+          mbar_arrive(bar);
         if (++a == ACCS) {
           a = 0;
           a_phase ^= 1u;
@@ -262,32 +306,38 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
       }
       // the four warps of a row exchange their quarters below: they go on together or not at all
       if (!named_barrier_and(1 + quad, 128, ok)) break;
-      const int valid = p.vocab - col0;  // <= 0: no column of a ragged last tile
-#pragma unroll
-      for (int j = 0; j < HN; ++j) z[j] *= p.top.inv_t;
       if (__any_sync(0xffffffffu, (bits[0] | bits[1]) != 0u)) {
         float *dst = p.top.z + t * p.top.K + first;
 #pragma unroll
         for (int j = 0; j < HN; ++j)
           if ((bits[j / 32] >> (j % 32)) & 1u) {
-            *dst++ = z[j];
+            *dst++ = z[j] * p.top.inv_t;
             z[j] = -INFINITY;
           }
       }
+      const int valid = p.vocab - col0;  // <= 0: no column of a ragged last tile
       if (valid < HN) {
 #pragma unroll
         for (int j = 0; j < HN; ++j) z[j] = j < valid ? z[j] : -INFINITY;
       }
-      float mx = z[0];
+      float m4[4] = {z[0], z[1], z[2], z[3]};
 #pragma unroll
-      for (int j = 1; j < HN; ++j) mx = fmaxf(mx, z[j]);
+      for (int j = 4; j < HN; ++j) m4[j & 3] = fmaxf(m4[j & 3], z[j]);
+      const float mx = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
       float s = 0.f;
       if (mx != -INFINITY) {
-        // the difference first: as fma(z, log2e, -mx log2e) its rounding is that of the larger product
-        float s4[4] = {0.f, 0.f, 0.f, 0.f};
+        // the difference first: as fma(z, scale, -mx scale) its rounding is that of the larger product
+        const f32x2 neg = pack_f32x2(-mx, -mx), scale2 = pack_f32x2(scale, scale);
+        f32x2 s2[2] = {0, 0};
 #pragma unroll
-        for (int j = 0; j < HN; ++j) s4[j & 3] += ex2_approx((z[j] - mx) * kLog2e);
-        s = (s4[0] + s4[1]) + (s4[2] + s4[3]);
+        for (int j = 0; j < HN; j += 2) {
+          float t0, t1;
+          unpack_f32x2(mul_f32x2(add_f32x2(pack_f32x2(z[j], z[j + 1]), neg), scale2), t0, t1);
+          s2[(j >> 1) & 1] = add_f32x2(s2[(j >> 1) & 1], pack_f32x2(ex2_approx(t0), ex2_approx(t1)));
+        }
+        float s1;
+        unpack_f32x2(add_f32x2(s2[0], s2[1]), s, s1);
+        s += s1;
       }
       float2(*sh)[TM] = ctl->quarter[local & 1];
       sh[quarter][r] = make_float2(mx, s);
@@ -300,18 +350,65 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
         float ss = 0.f;
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-          if (v[k].x != -INFINITY) ss = fmaf(v[k].y, ex2_approx((v[k].x - mm) * kLog2e), ss);
-        p.part[int64_t(n) * p.rows + row] = make_float2(mm, ss);
+          if (v[k].x != -INFINITY) ss = fmaf(v[k].y, ex2_approx((v[k].x - mm) * scale), ss);
+        p.part[int64_t(n) * p.rows + row] = make_float2(mm * p.top.inv_t, ss);
       }
     }
   }
 
   fence_before_sync();
   __syncthreads();
+  // neither CTA of a pair frees its TMEM or exits while the other may still reach its shared memory
+  if constexpr (kCG == 2) cluster_sync();
   if (warp == 1) {
     fence_after_sync();
-    tmem_dealloc(tmem_base, TMEM_COLS);
+    if constexpr (kCG == 2)
+      tmem_dealloc_pair(tmem_base, TMEM_COLS);
+    else
+      tmem_dealloc(tmem_base, TMEM_COLS);
   }
+}
+
+template <int kCG>
+sao_status launch_logits(const CUtensorMap &ma, const CUtensorMap &mb, const FwdParams &p, cudaStream_t s) {
+  auto kern = distill_logits_kernel<kCG>;
+  struct SetUp {
+    cudaError_t err;
+    int workers;  // CTAs, or CTA pairs, that fit on the device at once
+  };
+  DeviceInfo di;
+  SAO_TRY(device_info(&di));
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = 2;
+  at[0].val.clusterDim.y = 1;
+  at[0].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(2);
+  cfg.blockDim = dim3(NUM_THREADS);
+  cfg.dynamicSmemBytes = SMEM_BYTES;
+  cfg.stream = s;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  static PerDevice<SetUp> set_up;
+  const SetUp up = set_up.get(di.device, [&] {
+    SetUp u{cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, int(SMEM_BYTES)), di.sm_count};
+    if (u.err == cudaSuccess && kCG == 2) u.err = cudaOccupancyMaxActiveClusters(&u.workers, kern, &cfg);
+    return u;
+  });
+  if (up.err != cudaSuccess) return fail(SAO_ERR_CUDA, "kernel set-up: %s", cudaGetErrorString(up.err));
+  if (up.workers < 1) return fail(SAO_ERR_UNSUPPORTED, "no CTA pair of the logits kernel fits on this device");
+  const int64_t tiles = int64_t(p.nM) * p.nN;
+  const int grid = tiles < up.workers ? int(tiles) : up.workers;
+  int slot = launch_begin("distill_logits", s);
+  if constexpr (kCG == 2) {
+    cfg.gridDim = dim3(unsigned(2 * grid));
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, ma, mb, p);
+    if (e != cudaSuccess) return fail(SAO_ERR_CUDA, "cudaLaunchKernelEx (distill_logits): %s", cudaGetErrorString(e));
+  } else {
+    pdl(kern, grid, NUM_THREADS, SMEM_BYTES, s)(ma, mb, p);
+  }
+  return launch_end(slot, s);
 }
 
 }  // namespace
@@ -328,11 +425,12 @@ sao_status tc_distill_fwd(const void *H, const void *W, const uint8_t *row_mask,
   if (row_mask) SAO_TRY(compact_rows(row_mask, nullptr, N, static_cast<const __nv_bfloat16 *>(H), h, &cr, c, s));
   float2 *part = c.take<float2>(size_t(nvt) * size_t(N));
   if (!c.ok()) return fail(SAO_ERR_WORKSPACE, "workspace too small for the distillation forward");
+  const int cg = cta_group();
   CUtensorMap ma, mb;
   SAO_TRY(make_map(&ma, row_mask ? cr.Hc : H, uint64_t(h), uint64_t(row_mask ? cr.cap : N), uint64_t(h), KB, TM));
-  SAO_TRY(make_map(&mb, W, uint64_t(h), uint64_t(V), uint64_t(h), KB, TN));
+  SAO_TRY(make_map(&mb, W, uint64_t(h), uint64_t(V), uint64_t(h), KB, TN / cg));
   FwdParams p{};
-  p.nM = int((N + TM - 1) / TM);
+  p.nM = int((N + TM * cg - 1) / (TM * cg));
   p.nN = nvt;
   p.nK = (h + KB - 1) / KB;
   p.group_m = 64;  // as the log-prob forward: 32 MB of H stay in L2 while W streams
@@ -345,18 +443,7 @@ sao_status tc_distill_fwd(const void *H, const void *W, const uint8_t *row_mask,
     p.m_count = cr.count;
     p.row_idx = cr.idx;
   }
-  DeviceInfo di;
-  SAO_TRY(device_info(&di));
-  static PerDevice<cudaError_t> set_up;
-  const cudaError_t e = set_up.get(di.device, [] {
-    return cudaFuncSetAttribute(distill_logits_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(SMEM_BYTES));
-  });
-  if (e != cudaSuccess) return fail(SAO_ERR_CUDA, "kernel set-up: %s", cudaGetErrorString(e));
-  const int64_t tiles = int64_t(p.nM) * p.nN;
-  const int grid = tiles < di.sm_count ? int(tiles) : di.sm_count;
-  int slot = launch_begin("distill_logits", s);
-  pdl(distill_logits_kernel, grid, NUM_THREADS, SMEM_BYTES, s)(ma, mb, p);
-  SAO_TRY(launch_end(slot, s));
+  SAO_TRY(cg == 2 ? launch_logits<2>(ma, mb, p, s) : launch_logits<1>(ma, mb, p, s));
   return distill_finish(top, f, part, nvt, row_mask ? cr.pos : nullptr, N, s);
 }
 

@@ -248,6 +248,21 @@ def test_in_chunks_of_the_vocabulary(dtype):
     close(cut, ref, c)
 
 
+@pytest.mark.parametrize("N", [40, 300, 1500])
+def test_cta_pairs(N):
+    c = _case(N, 1096, 3000, 40, "bf16", seed=15)
+    c["mask"] = (np.arange(N) % 7 != 3).astype(np.uint8)
+    c["G"] *= c["mask"]
+    ref = want(c)
+    sao.sao_set_cta_pairs(True)
+    try:
+        close(run(c), ref, c)
+        got = run(c, dw="f32")
+    finally:
+        sao.sao_set_cta_pairs(False)
+    close(got, ref, c, dw_tol=2.0 ** -8)
+
+
 @pytest.mark.parametrize("N", [90, 1500, 4000])
 def test_bf16_head_with_an_fp32_dW(N):
     c = _case(N, 136, 700, 11, "bf16", seed=8)
