@@ -103,7 +103,7 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
     }
     for (int a = 0; a < ACCS; ++a) {
       mbar_init(smem_u32(&ctl->acc_full[a]), 1);
-      mbar_init(smem_u32(&ctl->acc_empty[a]), 512 * kCG);
+      mbar_init(smem_u32(&ctl->acc_empty[a]), 16 * kCG);
     }
     ctl->abort = 0;
     fence_barrier_init();
@@ -293,12 +293,16 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
                            z[c + j], z[c + j + 1]);
           }
         }
+        // one arrival a warp: 512 of them a part, serialised in shared memory, held up the operands' reads
         fence_before_sync();
-        const uint32_t bar = smem_u32(&ctl->acc_empty[a]);
-        if (kCG == 2 && rank != 0u)
-          mbar_arrive_cluster(mapa_shared(bar, 0u));
-        else
-          mbar_arrive(bar);
+        __syncwarp();
+        if (lane == 0) {
+          const uint32_t bar = smem_u32(&ctl->acc_empty[a]);
+          if (kCG == 2 && rank != 0u)
+            mbar_arrive_cluster(mapa_shared(bar, 0u));
+          else
+            mbar_arrive(bar);
+        }
         if (++a == ACCS) {
           a = 0;
           a_phase ^= 1u;
@@ -306,13 +310,16 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
       }
       // the four warps of a row exchange their quarters below: they go on together or not at all
       if (!named_barrier_and(1 + quad, 128, ok)) break;
-      if (__any_sync(0xffffffffu, (bits[0] | bits[1]) != 0u)) {
-        float *dst = p.top.z + t * p.top.K + first;
+      float *dst = p.top.z + t * p.top.K + first;
 #pragma unroll
-        for (int j = 0; j < HN; ++j)
-          if ((bits[j / 32] >> (j % 32)) & 1u) {
-            *dst++ = z[j] * p.top.inv_t;
-            z[j] = -INFINITY;
+      for (int c = 0; c < HN; c += 16) {
+        const uint32_t some = bits[c / 32] >> (c % 32) & 0xffffu;
+        if (!__any_sync(0xffffffffu, some != 0u)) continue;
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          if ((some >> j) & 1u) {
+            *dst++ = z[c + j] * p.top.inv_t;
+            z[c + j] = -INFINITY;
           }
       }
       const int valid = p.vocab - col0;  // <= 0: no column of a ragged last tile
