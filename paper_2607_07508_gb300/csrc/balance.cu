@@ -20,6 +20,7 @@
 #include <type_traits>
 
 #include "balance.cuh"
+#include "per_device.h"
 #include "sao_common.cuh"
 #include "sao_internal.h"
 #include "tc_ptx.cuh"
@@ -27,7 +28,34 @@
 namespace sao {
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
+// A lane takes kC columns of a row, in loads of kVec columns (16 bytes, or one column).
+// Rows on their way lie in shared memory (asynchronous copies of 4 bytes or more), for
+// single bf16 columns in registers.
+template <class T, int kVec>
+constexpr bool kAsync = kVec * sizeof(T) >= 4;
+// Threads of a CTA, one to an SM: as many as the registers for the columns' scores and
+// sums, and for the words that stay in them, allow. One CTA, not several: its partials are a
+// launch's whole scratch, and the reduction reads them all.
+constexpr int threads_of(bool async, int columns) {
+  const int n = 65536 / ((async ? 2 : 4) * columns + 56) / 64 * 64;
+  return n > 1024 ? 1024 : n;
+}
+template <class T, int kVec, int kC>
+constexpr int kThreads = threads_of(kAsync<T, kVec>, kC);
+// Rows that a thread has on their way.
+constexpr int depth_of(bool async, int size, int columns) {
+  const int n = (112 << 10) / (threads_of(async, columns) * columns * size);
+  return !async ? 2 : n < 2 ? 2 : n > 6 ? 6 : n;
+}
+template <class T, int kVec, int kC>
+constexpr int kDepthOf = depth_of(kAsync<T, kVec>, int(sizeof(T)), kC);
+// Bytes of their slots, and of the expert ids' (kIds a row and thread).
+constexpr int kIds = 2;
+template <class T, int kVec, int kC>
+constexpr int kRing = kAsync<T, kVec> ? kThreads<T, kVec, kC> * kC * int(sizeof(T)) * kDepthOf<T, kVec, kC> : 0;
+template <class T, int kVec, int kC>
+constexpr int kIdRing = kThreads<T, kVec, kC> * kIds * 4 * kDepthOf<T, kVec, kC>;
+
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct BalanceArgs {
@@ -62,38 +90,12 @@ __device__ __forceinline__ int seg_of(const BalanceArgs &a, int64_t r) {
   return lo;
 }
 
-// How a row lies over `lanes` (a power of two) consecutive lanes, kC columns each: kVec
-// columns (16 bytes, or one) per load, lane l holding loads l, l + lanes, ... Columns
-// past E, and all of a row that is not counted, read as -inf: they have no score.
+// A row's words in one lane: load v is columns (l + v lanes) kVec .. + kVec.
 template <class T, int kVec, int kC>
 struct Row {
   static constexpr int kLoads = kC / kVec;
   static constexpr int kWords = kVec == 1 ? kLoads : kLoads * 4;
   uint32_t raw[kWords];
-  __device__ __forceinline__ void load(const T *row, int E, int l, int lanes, bool live) {
-#pragma unroll
-    for (int v = 0; v < kLoads; ++v) {
-      const int c = (l + v * lanes) * kVec;
-      if constexpr (kVec == 1) {
-        constexpr uint32_t none = sizeof(T) == 2 ? 0xff80u : 0xff800000u;  // -inf
-        raw[v] = none;
-        if (live && c < E) {
-          if constexpr (sizeof(T) == 2)
-            raw[v] = ld(reinterpret_cast<const uint16_t *>(row) + c);
-          else
-            raw[v] = ld(reinterpret_cast<const uint32_t *>(row) + c);
-        }
-      } else {
-        constexpr uint32_t none = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;
-        uint4 x = make_uint4(none, none, none, none);
-        if (live && c < E) x = ld(reinterpret_cast<const uint4 *>(row + c));
-        raw[4 * v] = x.x;
-        raw[4 * v + 1] = x.y;
-        raw[4 * v + 2] = x.z;
-        raw[4 * v + 3] = x.w;
-      }
-    }
-  }
   __device__ __forceinline__ float at(int j) const {
     if constexpr (sizeof(T) == 4) return __uint_as_float(raw[j]);
     if constexpr (kVec == 1) return __uint_as_float(raw[j] << 16);
@@ -127,55 +129,251 @@ struct Row {
   }
 };
 
+// The rows of a warp: first, first + step, ... (of its first lane group) below end.
+struct Rows {
+  int64_t first, end;
+  int step;
+};
+// Of [r0, r1) within a CTA.
+__device__ __forceinline__ Rows cta_rows(int64_t r0, int64_t r1, int warp, int warps, int groups) {
+  return Rows{r0 + warp * groups, r1, warps * groups};
+}
+// Of the whole batch, the CTAs side by side: spans of masked rows fall on all of them (a
+// contiguous part each left SMs idle for a sixth of the time).
+__device__ __forceinline__ Rows grid_rows(const BalanceArgs &a, int warp, int warps, int groups) {
+  return Rows{(int64_t(warp) * gridDim.x + blockIdx.x) * groups, a.N, warps * groups * int(gridDim.x)};
+}
+
+// 4 or 16 bytes into shared memory, asynchronously.
+template <int kBytes>
+__device__ __forceinline__ void copy_async(uint32_t dst, const void *src) {
+  if constexpr (kBytes == 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+
+// The rows first, first + step, ... that a group of lanes goes through, those ahead
+// already on their way into slots of the thread's own (no barrier). Rows that are not
+// counted are not read (their words are anything), and columns past E read as -inf: they
+// have no score. What a row needs is asked for kDepth rows before, its expert ids too, and
+// the mask 32 rows at a time: with one row ahead, or a byte of the mask read per row, the
+// kernels waited for memory half of their time (2^20 x 160 bf16 forward 93-128 us).
+template <class T, int kVec, int kC>
+struct Stream {
+  static constexpr bool kSlots = kAsync<T, kVec>;
+  static constexpr int kDepth = kDepthOf<T, kVec, kC>, kLoads = kC / kVec;
+  static constexpr int kBytes = kVec * int(sizeof(T));
+  static constexpr uint32_t kPitch = kThreads<T, kVec, kC> * uint32_t(kBytes);  // from a load's slots to the next one's
+  const T *src;         // this lane's first column of the row kDepth steps ahead
+  const int32_t *ids;   // this lane's first id of that row, or null
+  const uint8_t *mask;  // of the warp's first row 64 steps after the last refill, or null
+  int left;             // rows from the warp's first row of this step to the end
+  int step, E, k, l, lanes, cur = 0, seen = 0;
+  uint64_t on_bits;     // bit d: the row d steps ahead is counted
+  uint32_t slots, id_slots;  // shared-memory addresses of this thread's first ones
+  Row<T, kVec, kC> reg[kSlots ? 1 : kDepth];
+
+  // Bit i of the result: this group's row i steps on is counted, `from` the warp's first row.
+  __device__ __forceinline__ uint32_t counted32(const uint8_t *from, int rows) const {
+    const int groups = 32 / lanes, lane = threadIdx.x & 31, mine = lane / lanes;
+    uint32_t bits = 0;
+    for (int g = 0; g < groups; ++g) {
+      const int64_t at = int64_t(lane) * step + g;
+      const uint32_t b = __ballot_sync(0xffffffffu, at < rows && (from == nullptr || ld(from + at) != 0));
+      if (g == mine) bits = b;
+    }
+    return bits;
+  }
+  // Rows left after `steps` more (0 or less: none).
+  __device__ __forceinline__ int past(int steps) const {
+    const int64_t n = left - int64_t(steps) * step;
+    return n > 0 ? int(n) : 0;
+  }
+  __device__ __forceinline__ void fetch(int slot, bool live) {
+    if (live) {
+      if constexpr (kSlots) {
+        const uint32_t dst = slots + uint32_t(slot * kLoads) * kPitch;
+#pragma unroll
+        for (int v = 0; v < kLoads; ++v)
+          if ((l + v * lanes) * kVec < E) copy_async<kBytes>(dst + v * kPitch, src + v * lanes * kVec);
+      }
+      if (ids) {
+#pragma unroll
+        for (int i = 0; i < kIds; ++i)
+          if (l + i * lanes < k)
+            copy_async<4>(id_slots + uint32_t(slot * kIds + i) * (kThreads<T, kVec, kC> * 4u), ids + i * lanes);
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    if constexpr (!kSlots) {
+      constexpr uint32_t none = 0xff80u;  // -inf
+#pragma unroll
+      for (int v = 0; v < kLoads; ++v) {
+        uint32_t w = none;
+        if (live && l + v * lanes < E) w = ld(reinterpret_cast<const uint16_t *>(src) + v * lanes);
+        reg[kDepth - 1].raw[v] = w;
+      }
+    }
+  }
+  // `lane_ids`: expert ids [N, k], or null.
+  __device__ __forceinline__ Stream(const BalanceArgs &a, const Rows &rows, int lane, int group, const int32_t *lane_ids,
+                                    const void *ring, const void *id_ring)
+      : left(int(rows.end > rows.first ? rows.end - rows.first : 0)), step(rows.step), E(a.E), k(a.k), l(lane),
+        lanes(group) {
+    const int64_t warp_first = rows.first, first = warp_first + (threadIdx.x & 31) / group;
+    src = static_cast<const T *>(a.x) + first * a.E + lane * kVec;
+    ids = lane_ids ? lane_ids + first * a.k + lane : nullptr;
+    mask = a.mask ? a.mask + warp_first : nullptr;
+    on_bits = counted32(mask, left) |
+              uint64_t(counted32(mask ? mask + 32 * int64_t(step) : nullptr, past(32))) << 32;
+    if (mask) mask += 64 * int64_t(step);
+    id_slots = tc::smem_u32(id_ring) + threadIdx.x * 4u;
+    slots = 0;
+    if constexpr (kSlots) {
+      slots = tc::smem_u32(ring) + threadIdx.x * uint32_t(kBytes);
+      constexpr uint32_t none = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;
+#pragma unroll
+      for (int v = 0; v < kLoads; ++v)
+        if ((l + v * lanes) * kVec >= E)
+          for (int d = 0; d < kDepth; ++d)
+#pragma unroll
+            for (int w = 0; w < kBytes; w += 4)
+              asm volatile("st.shared.b32 [%0], %1;" ::"r"(slots + uint32_t(d * kLoads + v) * kPitch + w), "r"(none)
+                           : "memory");
+    }
+#pragma unroll
+    for (int d = 0; d < kDepth; ++d) {
+      if constexpr (!kSlots)
+        if (d > 0) reg[d - 1] = reg[kDepth - 1];
+      fetch(d, on_bits >> d & 1u);
+      src += int64_t(step) * E;
+      if (ids) ids += int64_t(step) * k;
+    }
+  }
+  __device__ __forceinline__ bool on() const { return on_bits & 1u; }
+  __device__ __forceinline__ void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory"); }
+  // This row's words (again, until advance()).
+  __device__ __forceinline__ Row<T, kVec, kC> row() const {
+    if constexpr (kSlots) {
+      Row<T, kVec, kC> x;
+      const uint32_t at = slots + uint32_t(cur * kLoads) * kPitch;
+#pragma unroll
+      for (int v = 0; v < kLoads; ++v) {
+        if constexpr (kBytes == 16)
+          asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                       : "=r"(x.raw[4 * v]), "=r"(x.raw[4 * v + 1]), "=r"(x.raw[4 * v + 2]), "=r"(x.raw[4 * v + 3])
+                       : "r"(at + v * kPitch)
+                       : "memory");
+        else
+          asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x.raw[v]) : "r"(at + v * kPitch) : "memory");
+      }
+      return x;
+    } else {
+      return reg[0];
+    }
+  }
+  // Expert id l + i lanes of this row (i < kIds; below k only).
+  __device__ __forceinline__ int id(int i) const {
+    int v;
+    asm volatile("ld.shared.b32 %0, [%1];"
+                 : "=r"(v)
+                 : "r"(id_slots + uint32_t(cur * kIds + i) * (kThreads<T, kVec, kC> * 4u))
+                 : "memory");
+    return v;
+  }
+  // To the next row; the words and ids of this one have been used.
+  __device__ __forceinline__ void advance() {
+    if constexpr (!kSlots) {
+#pragma unroll
+      for (int d = 1; d < kDepth; ++d) reg[d - 1] = reg[d];
+    }
+    fetch(cur, on_bits >> kDepth & 1u);
+    src += int64_t(step) * E;
+    if (ids) ids += int64_t(step) * k;
+    on_bits >>= 1;
+    left = past(1);
+    if (++cur == kDepth) cur = 0;
+    if (++seen == 32) {
+      seen = 0;
+      on_bits |= uint64_t(counted32(mask, past(32))) << 32;
+      if (mask) mask += 32 * int64_t(step);
+    }
+  }
+};
+
 __device__ __forceinline__ float lanes_max(float v, int lanes) {
-  for (int o = 1; o < lanes; o <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1)
+    if (o < lanes) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
   return v;
 }
 __device__ __forceinline__ float lanes_sum(float v, int lanes) {
-  for (int o = 1; o < lanes; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1)
+    if (o < lanes) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
 
+__device__ __forceinline__ float rcp_approx(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// q = e^(x - m), or e^-m sigmoid(x) = 1 / (e^m + e^(m - x)), and their sum over the row.
+// kShift: m is given; else it is 0. (The difference is taken before it is scaled, so an
+// exponent is off by 2^-24 of itself.)
+template <bool kSigmoid, bool kShift, class R, int kC>
+__device__ __forceinline__ float scores(const R &x, float (&q)[kC], int lanes, float m, float em) {
+  constexpr float kScale = kSigmoid ? -kLog2e : kLog2e;
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int j = 0; j < kC; ++j) {
+    const float v = x.at(j);
+    q[j] = tc::ex2_approx((kShift ? v - m : v) * kScale);
+    if constexpr (kSigmoid) q[j] = rcp_approx(em + q[j]);
+    s[j & 3] += q[j];
+  }
+  return lanes_sum((s[0] + s[1]) + (s[2] + s[3]), lanes);
+}
+
 // A row's scores q, up to a factor that the normalisation takes out, and 1 / their sum
-// (0 for a row of -inf alone, which has no probabilities). Softmax: e^(x - max). Sigmoid:
-// e^-m sigmoid(x) = 1 / (e^m + e^(m - x)) with m = min(max, 0): sigmoid(x) itself, but
-// for rows far below 0, whose sigmoids vanish. em: e^m. (The difference is taken before
-// it is scaled, so an exponent is off by 2^-24 of itself.)
-template <bool kSigmoid, class R, int kC>
-__device__ __forceinline__ float row_scores(const R &x, float (&q)[kC], int lanes, float &em) {
-  float m4[4];
+// (0 for a row of -inf alone, which has no probabilities); em: e^m of that factor, 1
+// mostly. Rows whose sum without a shift is near 1 need none: their largest logit is
+// within 12 of 0, so exponents lose no more than with the largest subtracted. The
+// search for it and its exchanges between lanes were a third of the instructions, and
+// those bound the kernels. A warp with another row takes m = the largest logit, for sigmoids
+// only where it is below 0 (the sigmoids themselves would vanish with it).
+template <bool kSigmoid, class S, int kC>
+__device__ __forceinline__ float row_scores(const S &stream, float (&q)[kC], float &em) {
+  const int lanes = stream.lanes;
+  em = 1.f;
+  float s = scores<kSigmoid, false>(stream.row(), q, lanes, 0.f, em);
+  const bool fine = kSigmoid ? s > 0x1p-10f : s > 0x1p-10f && s < 0x1p17f;
+  if (!__all_sync(0xffffffffu, fine || !stream.on())) {
+    const auto x = stream.row();
+    float m = x.at(0);
 #pragma unroll
-  for (int j = 0; j < kC; ++j) m4[j & 3] = j < 4 ? x.at(j) : fmaxf(m4[j & 3], x.at(j));
-  float m = lanes_max(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])), lanes);
-  if (m == -INFINITY) m = 0.f;
-  if constexpr (kSigmoid) {
-    m = fminf(m, 0.f);
-    em = tc::ex2_approx(m * kLog2e);
-  }
-  // two columns per fp32 operation
-  const tc::f32x2 neg = tc::pack_f32x2(-m, -m), scale = tc::pack_f32x2(kSigmoid ? -kLog2e : kLog2e, kSigmoid ? -kLog2e : kLog2e);
-  tc::f32x2 s2[2] = {0, 0};
-#pragma unroll
-  for (int j = 0; j < kC; j += 2) {
-    float t0, t1;
-    tc::unpack_f32x2(tc::mul_f32x2(tc::add_f32x2(tc::pack_f32x2(x.at(j), x.at(j + 1)), neg), scale), t0, t1);
-    q[j] = tc::ex2_approx(t0);
-    q[j + 1] = tc::ex2_approx(t1);
+    for (int j = 1; j < kC; ++j) m = fmaxf(m, x.at(j));
+    m = lanes_max(m, lanes);
+    if (m == -INFINITY) m = 0.f;
     if constexpr (kSigmoid) {
-      q[j] = __fdividef(1.f, em + q[j]);
-      q[j + 1] = __fdividef(1.f, em + q[j + 1]);
+      m = fminf(m, 0.f);
+      em = tc::ex2_approx(m * kLog2e);
     }
-    s2[j / 2 & 1] = tc::add_f32x2(s2[j / 2 & 1], tc::pack_f32x2(q[j], q[j + 1]));
+    s = scores<kSigmoid, true>(x, q, lanes, m, em);
   }
-  float s, s1;
-  tc::unpack_f32x2(tc::add_f32x2(s2[0], s2[1]), s, s1);
-  s = lanes_sum(s + s1, lanes);
-  return s == 0.f ? 0.f : 1.f / s;
+  return s == 0.f ? 0.f : rcp_approx(s);
 }
 
 // Runs f(segment, first row, row after the last) for the segments of chunk c (all threads).
 template <class F>
 __device__ __forceinline__ void for_segments(const BalanceArgs &a, int c, F f) {
+  if (a.cu == nullptr) {
+    f(0, 0, a.N);
+    return;
+  }
   int64_t r = int64_t(c) * a.chunk;
   const int64_t end = r + a.chunk < a.N ? r + a.chunk : a.N;
   for (int b = seg_of(a, r); b < a.B && r < end; ++b) {
@@ -187,66 +385,55 @@ __device__ __forceinline__ void for_segments(const BalanceArgs &a, int c, F f) {
   }
 }
 
-// CTAs that an SM holds: as many registers as a lane's columns, the next row's and their sums take.
-template <class T, int kC>
-constexpr int kCtas = kC <= 8 ? 4 : (kC <= 16 || (kC <= 24 && sizeof(T) == 2)) ? 3 : 2;
-
 // Each group of `lanes` lanes takes a row at a time, the next one's logits in flight,
 // and keeps the sums of its columns in registers. One pass over the logits: bound by
 // reading them.
 template <class T, int kVec, int kC, bool kSigmoid>
-__global__ void __launch_bounds__(kThreads, kCtas<T, kC>)
+__global__ void __launch_bounds__(kThreads<T, kVec, kC>)
     balance_partial_kernel(const BalanceArgs a, int lanes, float *psum, int *pcount, int *prows, unsigned int *ticket) {
-  extern __shared__ float sums[];  // [kWarps][E], then the counts [E]
+  constexpr int kBlock = kThreads<T, kVec, kC>, kWarps = kBlock / 32;
+  extern __shared__ uint4 smem[];  // the stream's slots, sums [kWarps][E], counts [E]
   __shared__ int n_rows[kWarps];
   grid_wait();
   if (blockIdx.x == 0 && threadIdx.x == 0) *ticket = 0;
+  const void *id_ring = smem + kRing<T, kVec, kC> / 16;
+  float *sums = reinterpret_cast<float *>(smem + (kRing<T, kVec, kC> + kIdRing<T, kVec, kC>) / 16);
   int *counts = reinterpret_cast<int *>(sums + kWarps * a.E);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int groups = 32 / lanes, l = lane & (lanes - 1), step = kWarps * groups;
-  const T *x = static_cast<const T *>(a.x);
+  const int groups = 32 / lanes, l = lane & (lanes - 1);
   for_segments(a, blockIdx.x, [&](int b, int64_t r0, int64_t r1) {
-    for (int e = threadIdx.x; e < a.E; e += kThreads) counts[e] = 0;
+    for (int e = threadIdx.x; e < a.E; e += kBlock) counts[e] = 0;
     __syncthreads();
     float acc[kC];
 #pragma unroll
     for (int j = 0; j < kC; ++j) acc[j] = 0.f;
     int n = 0;
-    auto counted = [&](int64_t r) { return r < r1 && (a.mask == nullptr || ld(a.mask + r) != 0); };
-    int64_t r = r0 + warp * groups + lane / lanes;
-    Row<T, kVec, kC> next;
-    bool next_on = counted(r);
-    next.load(x + r * a.E, a.E, l, lanes, next_on);
-    bool after_on = counted(r + step);
-    auto first_id = [&](int64_t row, bool on) { return on && l < a.k ? ld(a.ids + row * a.k + l) : -1; };
     auto count = [&](int id) {
-      if (id >= 0 && id < a.E)
+      if (unsigned(id) < unsigned(a.E))
         atomicAdd(counts + id, 1);
-      else if (id >= a.E)
+      else if (id >= 0)
         raise_device_error(a.err, SAO_DEVERR_EXPERT_ID);
     };
-    int next_id = first_id(r, next_on);
-    for (int64_t base = r0 + warp * groups; base < r1; base += step, r += step) {  // the warp's lanes stay together
-      const Row<T, kVec, kC> row = next;
-      const bool on = next_on;
-      const int id = next_id;
-      next_on = after_on;
-      next.load(x + (r + step) * a.E, a.E, l, lanes, next_on);
-      next_id = first_id(r + step, next_on);
-      after_on = counted(r + 2 * step);
-      if (!__any_sync(0xffffffffu, on)) continue;  // spans of masked rows
-      if (on) {
-        if (l == 0) ++n;
-        count(id);
-        for (int j = l + lanes; j < a.k; j += lanes) count(ld(a.ids + r * a.k + j));
-      }
-      float q[kC], em;
-      const float inv = row_scores<kSigmoid>(row, q, lanes, em);
-      const tc::f32x2 inv2 = tc::pack_f32x2(inv, inv);
+    const Rows rows = a.cu ? cta_rows(r0, r1, warp, kWarps, groups) : grid_rows(a, warp, kWarps, groups);
+    Stream<T, kVec, kC> x(a, rows, l, lanes, a.ids, smem, id_ring);
+    for (int64_t r = rows.first + lane / lanes; x.left > 0; r += rows.step) {  // the warp's lanes stay together
+      x.wait();
+      const bool on = x.on();
+      if (__any_sync(0xffffffffu, on)) {  // (not in spans of masked rows)
+        float q[kC], em;
+        const float inv = row_scores<kSigmoid>(x, q, em);
+        if (on) {
+          if (l == 0) ++n;
 #pragma unroll
-      for (int j = 0; j < kC; j += 2)
-        tc::unpack_f32x2(tc::fma_f32x2(tc::pack_f32x2(q[j], q[j + 1]), inv2, tc::pack_f32x2(acc[j], acc[j + 1])), acc[j],
-                         acc[j + 1]);
+          for (int i = 0; i < kIds; ++i)
+            if (l + i * lanes < a.k) count(x.id(i));
+          for (int j = l + kIds * lanes; j < a.k; j += lanes) count(ld(a.ids + r * a.k + j));
+#pragma unroll
+          for (int j = 0; j < kC; ++j) acc[j] = fmaf(q[j], inv, acc[j]);
+        }
+        __syncwarp();
+      }
+      x.advance();
     }
     for (int o = lanes; o < 32; o <<= 1) {  // the warp's groups
 #pragma unroll
@@ -263,7 +450,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<T, kC>)
     if (lane == 0) n_rows[warp] = n;
     __syncthreads();
     const int64_t slot = int64_t(blockIdx.x) + b;
-    for (int e = threadIdx.x; e < a.E; e += kThreads) {
+    for (int e = threadIdx.x; e < a.E; e += kBlock) {
       float v = 0.f;
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) v += sums[w * a.E + e];
@@ -279,16 +466,16 @@ __global__ void __launch_bounds__(kThreads, kCtas<T, kC>)
   });
 }
 
-// CTA (b, 32 columns): adds the segment's partials, kSlices warps side by side;
-// the last CTA adds the products of all of them.
+// CTA (b, 32 columns): adds the segment's partials, kSlices warps side by side; the
+// last CTA adds the products of all of them. Bound by the latency of its few rounds of
+// loads. (The sums are of positive numbers, in a fixed order, in fp32; fp64, on which
+// GB300 has few units, took longer than the loads.)
 template <int kSlices>
 __global__ void __launch_bounds__(32 * kSlices)
     balance_reduce_kernel(const BalanceArgs a, const float *psum, const int *pcount, const int *prows, float *loss,
-                          int64_t *counts, float *prob_sums, int64_t *rows, double *terms, unsigned int *ticket) {
-  __shared__ float sh_sum[kSlices][32];
-  __shared__ long long sh_count[kSlices][32];
-  __shared__ long long sh_rows[kSlices];
-  __shared__ double sh_term[kSlices];
+                          int64_t *counts, float *prob_sums, int64_t *rows, float *terms, unsigned int *ticket) {
+  __shared__ float sh_sum[kSlices][32], sh_term[kSlices];
+  __shared__ long long sh_count[kSlices][32], sh_rows[kSlices];
   __shared__ int sh_used[kSlices];
   __shared__ bool last;
   grid_wait();
@@ -300,52 +487,69 @@ __global__ void __launch_bounds__(32 * kSlices)
   long long n = 0, nr = 0;
   if (r1 > r0) {
     const int c0 = int(r0 / a.chunk), c1 = int((r1 - 1) / a.chunk);
-#pragma unroll 4
-    for (int c = c0 + slice; c <= c1; c += kSlices) {
-      const int64_t slot = int64_t(c) + b;
-      if (e < a.E) {
-        s += ld(psum + slot * a.E + e);
-        n += ld(pcount + slot * a.E + e);
+    constexpr int kU = 4;  // partials in flight
+    for (int c = c0 + slice; c <= c1; c += kU * kSlices) {
+      float ps[kU];
+      int pn[kU], pr[kU];
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        const int64_t slot = int64_t(c) + u * kSlices + b;
+        const bool in = c + u * kSlices <= c1;
+        ps[u] = in && e < a.E ? ld(psum + slot * a.E + e) : 0.f;
+        pn[u] = in && e < a.E ? ld(pcount + slot * a.E + e) : 0;
+        pr[u] = in ? ld(prows + slot) : 0;
       }
-      nr += ld(prows + slot);
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        s += ps[u];
+        n += pn[u];
+        nr += pr[u];
+      }
     }
   }
   sh_sum[slice][lane] = s;
   sh_count[slice][lane] = n;
   if (lane == 0) sh_rows[slice] = nr;
   __syncthreads();
+  const bool alone = gridDim.x == 1;
   if (slice == 0) {
     s = 0.f;
     n = nr = 0;
+#pragma unroll
     for (int k = 0; k < kSlices; ++k) {
       s += sh_sum[k][lane];
       n += sh_count[k][lane];
       nr += sh_rows[k];
     }
-    double term = 0.0;
+    float term = 0.f;
     if (e < a.E) {
       prob_sums[int64_t(b) * a.E + e] = s;
       counts[int64_t(b) * a.E + e] = n;
-      term = nr > 0 ? double(s) * double(n) * (double(a.E) / (double(a.k) * double(nr) * double(nr))) : 0.0;
+      if (nr > 0) term = s * (float(n) * (float(a.E) / (float(a.k) * float(nr))) / float(nr));
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) term += __shfl_xor_sync(0xffffffffu, term, o);
     if (lane == 0) {
-      terms[blockIdx.x] = term;
       if (g == 0) rows[b] = nr;
       // checked mode: cu_seqlens runs from 0 to N and never falls
       if (a.cu && g == 0) {
         const int64_t u = ld(a.cu + b), v = ld(a.cu + b + 1);
         if (u > v || (b == 0 && u != 0) || (b == a.B - 1 && v != a.N)) raise_device_error(a.err, SAO_DEVERR_CU_SEQLENS);
       }
-      __threadfence();
-      last = atomicAdd(ticket, 1u) == gridDim.x - 1;
+      if (alone) {
+        loss[0] = term;
+      } else {
+        terms[blockIdx.x] = term;
+        __threadfence();
+        last = atomicAdd(ticket, 1u) == gridDim.x - 1;
+      }
     }
   }
+  if (alone) return;
   __syncthreads();
   if (!last) return;
   __threadfence();
-  double t = 0.0;
+  float t = 0.f;
   int used = 0;
   for (int64_t i = threadIdx.x; i < gridDim.x; i += 32 * kSlices) t += __ldcg(terms + i);
   for (int i = threadIdx.x; i < a.B; i += 32 * kSlices) used += __ldcg(rows + i) > 0;
@@ -358,13 +562,13 @@ __global__ void __launch_bounds__(32 * kSlices)
   }
   __syncthreads();
   if (threadIdx.x == 0) {
-    t = 0.0;
+    t = 0.f;
     used = 0;
     for (int k = 0; k < kSlices; ++k) {
       t += sh_term[k];
       used += sh_used[k];
     }
-    loss[0] = used ? float(t / double(used)) : 0.f;
+    loss[0] = used ? t / float(used) : 0.f;
   }
 }
 
@@ -372,42 +576,37 @@ __global__ void __launch_bounds__(32 * kSlices)
 // stay in registers until the segment ends. One pass: bound by reading the logits and
 // writing their gradient.
 template <class T, int kVec, int kC, bool kSigmoid>
-__global__ void __launch_bounds__(kThreads, kCtas<T, kC>)
+__global__ void __launch_bounds__(kThreads<T, kVec, kC>)
     balance_grad_kernel(const BalanceArgs a, int lanes, const int64_t *counts, const int64_t *rows,
                         const float *grad_loss, T *dx) {
+  constexpr int kBlock = kThreads<T, kVec, kC>, kWarps = kBlock / 32;
   __shared__ int sh_used[kWarps];
   grid_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   int used = 0;
-  for (int i = threadIdx.x; i < a.B; i += kThreads) used += ld(rows + i) > 0;
+  for (int i = threadIdx.x; i < a.B; i += kBlock) used += ld(rows + i) > 0;
   used = __reduce_add_sync(0xffffffffu, used);
   if (lane == 0) sh_used[warp] = used;
   __syncthreads();
   used = 0;
   for (int i = 0; i < kWarps; ++i) used += sh_used[i];
-  const T *x = static_cast<const T *>(a.x);
+  extern __shared__ uint4 smem[];  // the stream's slots
   const float g = ld(grad_loss);
-  const int groups = 32 / lanes, l = lane & (lanes - 1), step = kWarps * groups;
+  const int groups = 32 / lanes, l = lane & (lanes - 1);
   const int64_t r0 = int64_t(blockIdx.x) * a.chunk, r1 = r0 + a.chunk < a.N ? r0 + a.chunk : a.N;
-  auto counted = [&](int64_t r) { return r < r1 && (a.mask == nullptr || ld(a.mask + r) != 0); };
-  int64_t r = r0 + warp * groups + lane / lanes;
-  Row<T, kVec, kC> next;
-  bool next_on = counted(r);
-  next.load(x + r * a.E, a.E, l, lanes, next_on);
-  bool after_on = counted(r + step);
-  int b = -1;
-  int64_t seg_end = -1;  // of segment b: the weights are those of another one from there on
+  const Rows own = a.cu ? cta_rows(r0, r1, warp, kWarps, groups) : grid_rows(a, warp, kWarps, groups);
+  int64_t seg_end = -1;  // from this row on the weights are another segment's
   float w[kC];
 #pragma unroll
   for (int j = 0; j < kC; ++j) w[j] = 0.f;
-  for (int64_t base = r0 + warp * groups; base < r1; base += step, r += step) {
-    const Row<T, kVec, kC> row = next;
-    const bool on = next_on;
-    next_on = after_on;
-    next.load(x + (r + step) * a.E, a.E, l, lanes, next_on);
-    after_on = counted(r + 2 * step);
+  const int64_t first = own.first + lane / lanes;
+  Stream<T, kVec, kC> x(a, own, l, lanes, nullptr, smem, smem);
+  T *out = dx + first * a.E;
+  const int64_t out_step = int64_t(own.step) * a.E;
+  for (int64_t r = first; x.left > 0; r += own.step) {
+    const bool on = x.on();
     if (on && r >= seg_end) {
-      b = seg_of(a, r);
+      const int b = seg_of(a, r);
       seg_end = b + 1 < a.B ? seg_at(a, b + 1) : a.N;
       if (seg_end <= r) seg_end = r + 1;  // (cu_seqlens that do not rise)
       const float n = float(ld(rows + b));
@@ -418,24 +617,30 @@ __global__ void __launch_bounds__(kThreads, kCtas<T, kC>)
         w[j] = c < a.E ? f * float(ld(counts + int64_t(b) * a.E + c)) : 0.f;
       }
     }
+    x.wait();
     __syncwarp();
     float q[kC], em = 0.f;
     if (__any_sync(0xffffffffu, on)) {
-      const float inv = row_scores<kSigmoid>(row, q, lanes, em);
-      float d = 0.f;
+      const float inv = row_scores<kSigmoid>(x, q, em);
+      float d4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int j = 0; j < kC; ++j) d = fmaf(q[j], w[j], d);
-      d = lanes_sum(d, lanes) * inv;
+      for (int j = 0; j < kC; ++j) d4[j & 3] = fmaf(q[j], w[j], d4[j & 3]);
+      const float d = lanes_sum((d4[0] + d4[1]) + (d4[2] + d4[3]), lanes) * inv;
+      // q inv (w - d), with the two factors of the row taken into one multiply-add
+      const float nd = -d * inv;
 #pragma unroll
       for (int j = 0; j < kC; ++j) {
-        const float s = kSigmoid ? q[j] * inv * fmaf(-em, q[j], 1.f) : q[j] * inv;
-        q[j] = s * (w[j] - d);
+        const float slope = kSigmoid ? q[j] * fmaf(-em, q[j], 1.f) : q[j];
+        q[j] = slope * fmaf(w[j], inv, nd);
       }
-    } else {  // spans of masked rows
+    }
+    if (!on) {
 #pragma unroll
       for (int j = 0; j < kC; ++j) q[j] = 0.f;
     }
-    if (r < r1) Row<T, kVec, kC>::store(dx + r * a.E, q, a.E, l, lanes);
+    if (r < own.end) Row<T, kVec, kC>::store(out, q, a.E, l, lanes);
+    x.advance();
+    out += out_step;
   }
 }
 
@@ -445,23 +650,22 @@ struct Layout {
   bool vec;
 };
 // Vector loads where every row starts on 16 bytes. Of the layouts the one with the
-// least work: a lane's columns at about 7 instructions each, the exchanges between
-// lanes and 24 more, times the lanes (160 bf16 logits: 8 lanes x 24 columns, not
-// 16 x 16, of which 96 would be idle).
+// fewest instructions: about 5 for each of a lane's columns, 130 for all else that a
+// row takes, times the lanes; of 8 to 24 columns (32 or 40, with fewer warps to hide latencies,
+// were no faster for 128 to 256 experts) unless only 32 fit, and for single bf16 columns,
+// whose words stay in registers, of 8 (98,301 x 63: 44 us against 51 with 16).
 Layout layout(const void *x, const void *dx, sao_dtype dt, int E) {
   const int size = dt == SAO_BF16 ? 2 : 4, per = 16 / size;
   Layout best{0, 0, E % per == 0 && aligned16(x) && aligned16(dx)};
+  const int vec = best.vec ? per : 1, most = vec * size >= 4 ? 24 : 8;
   int least = 0;
   for (int c = 8; c <= 32; c += 8) {
-    const int vec = best.vec ? per : 1, loads = c / vec, units = E / vec;
-    int lanes = 1, log = 0;
-    while (lanes * loads < units) {
-      lanes <<= 1;
-      ++log;
-    }
+    const int loads = c / vec, units = E / vec;
+    int lanes = 1;
+    while (lanes * loads < units) lanes <<= 1;
     if (lanes > 32) continue;
-    const int cost = lanes * (7 * c + 4 * log + 24);
-    if (best.columns == 0 || (c < 32 && cost < least)) {  // 32 columns: where no other fits
+    const int cost = lanes * (5 * c + 130);
+    if (best.columns == 0 || (c <= most && cost < least)) {
       best.columns = c;
       best.lanes = lanes;
       least = cost;
@@ -487,34 +691,45 @@ void with_layout(const Layout &l, int score, F f) {
   score == SAO_SCORE_SIGMOID ? loads(std::true_type{}) : loads(std::false_type{});
 }
 
-// Rows per CTA: three CTAs on each of 152 SMs, at least one row for every lane group of
-// the CTA's with the fewest lanes. From N and E alone: the sums' order, and so their
-// bits, are those of any device and alignment.
-int chunk_rows(int64_t N, int E) {
-  const int64_t c = (N + 455) / 456, least = E <= 16 ? 256 : 32;
-  return int(c < least ? least : c);
+// Rows per CTA: one on each of 152 SMs, or 64 rows. From N alone: the sums' order does
+// not depend on the device.
+int chunk_rows(int64_t N) {
+  const int64_t c = (N + 151) / 152;
+  return int(c < 64 ? 64 : c);
 }
 BalanceArgs make_args(const void *x, const int32_t *ids, const uint8_t *mask, const int32_t *cu, int32_t B, int64_t N,
                       int32_t E, int32_t k, unsigned int *err) {
-  BalanceArgs a{x, ids, mask, cu, cu ? B : 1, N, E, k, chunk_rows(N, E), 0, err};
+  BalanceArgs a{x, ids, mask, cu, cu ? B : 1, N, E, k, chunk_rows(N), 0, err};
   a.chunks = int((N + a.chunk - 1) / a.chunk);
   return a;
+}
+
+// Lets the kernel have an SM's shared memory (once per device).
+template <auto kKernel>
+sao_status allow_smem() {
+  DeviceInfo di;
+  SAO_TRY(device_info(&di));
+  static PerDevice<cudaError_t> set_up;
+  const cudaError_t e = set_up.get(
+      di.device, [] { return cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 225 << 10); });
+  if (e != cudaSuccess) return fail(SAO_ERR_CUDA, "kernel set-up: %s", cudaGetErrorString(e));
+  return SAO_OK;
 }
 
 struct Scratch {
   float *psum;
   int *pcount, *prows;
-  double *terms;
+  float *terms;
   unsigned int *ticket;
 };
 Scratch take(Carver &c, int64_t N, int32_t E, int32_t B) {
-  const int64_t chunk = chunk_rows(N, E);
+  const int64_t chunk = chunk_rows(N);
   const size_t slots = size_t((N + chunk - 1) / chunk) + size_t(B);
   Scratch s;
   s.psum = c.take<float>(slots * size_t(E));
   s.pcount = c.take<int>(slots * size_t(E));
   s.prows = c.take<int>(slots);
-  s.terms = c.take<double>(size_t(B) * size_t((E + 31) / 32));
+  s.terms = c.take<float>(size_t(B) * size_t((E + 31) / 32));
   s.ticket = c.take<unsigned int>(1);
   return s;
 }
@@ -537,17 +752,25 @@ sao_status balance_fwd_launch(const void *x, sao_dtype dt, const int32_t *ids, c
   if (!c.ok()) return fail(SAO_ERR_WORKSPACE, "workspace too small for the balance loss");
   const Layout lay = layout(x, x, dt, E);
   int slot = launch_begin("balance_partial", s);
+  sao_status st = SAO_OK;
   auto partial = [&](auto t, auto vec, auto columns, auto sig) {
-    pdl(balance_partial_kernel<decltype(t), vec.value, columns.value, sig.value>, unsigned(a.chunks), kThreads,
-        size_t(E) * (kWarps + 1) * sizeof(float), s)(a, lay.lanes, w.psum, w.pcount, w.prows, w.ticket);
+    using T = decltype(t);
+    constexpr int kBlock = kThreads<T, vec.value, columns.value>;
+    auto kern = balance_partial_kernel<T, vec.value, columns.value, sig.value>;
+    const size_t smem = kRing<T, vec.value, columns.value> + kIdRing<T, vec.value, columns.value> +
+                        size_t(E) * (kBlock / 32 + 1) * sizeof(float);
+    st = allow_smem<balance_partial_kernel<T, vec.value, columns.value, sig.value>>();
+    if (st == SAO_OK)
+      pdl(kern, unsigned(a.chunks), kBlock, smem, s)(a, lay.lanes, w.psum, w.pcount, w.prows, w.ticket);
   };
   dt == SAO_BF16 ? with_layout<__nv_bfloat16>(lay, score, partial) : with_layout<float>(lay, score, partial);
+  SAO_TRY(st);
   SAO_TRY(launch_end(slot, s));
-  // a batch's partials, hundreds in few CTAs: 32 warps to each; many trajectories: 8
+  // a batch's partials, up to 152 in few CTAs: 16 warps to each; many trajectories: 8
   const unsigned grid = unsigned(a.B) * unsigned((E + 31) / 32);
   slot = launch_begin("balance_reduce", s);
-  auto reduce = grid <= 152 ? balance_reduce_kernel<32> : balance_reduce_kernel<8>;
-  pdl(reduce, grid, grid <= 152 ? 1024 : 256, 0, s)(a, w.psum, w.pcount, w.prows, loss, counts, prob_sums, rows,
+  auto reduce = grid <= 152 ? balance_reduce_kernel<16> : balance_reduce_kernel<8>;
+  pdl(reduce, grid, grid <= 152 ? 512 : 256, 0, s)(a, w.psum, w.pcount, w.prows, loss, counts, prob_sums, rows,
                                                     w.terms, w.ticket);
   return launch_end(slot, s);
 }
@@ -558,12 +781,17 @@ sao_status balance_bwd_launch(const void *x, sao_dtype dt, const uint8_t *mask, 
   const BalanceArgs a = make_args(x, nullptr, mask, cu, B, N, E, k, err);
   const Layout lay = layout(x, dx, dt, E);
   int slot = launch_begin("balance_grad", s);
+  sao_status st = SAO_OK;
   auto grad = [&](auto t, auto vec, auto columns, auto sig) {
     using T = decltype(t);
-    pdl(balance_grad_kernel<T, vec.value, columns.value, sig.value>, unsigned(a.chunks), kThreads, 0, s)(
-        a, lay.lanes, counts, rows, grad_loss, static_cast<T *>(dx));
+    auto kern = balance_grad_kernel<T, vec.value, columns.value, sig.value>;
+    st = allow_smem<balance_grad_kernel<T, vec.value, columns.value, sig.value>>();
+    if (st == SAO_OK)
+      pdl(kern, unsigned(a.chunks), kThreads<T, vec.value, columns.value>, size_t(kRing<T, vec.value, columns.value>), s)(
+          a, lay.lanes, counts, rows, grad_loss, static_cast<T *>(dx));
   };
   dt == SAO_BF16 ? with_layout<__nv_bfloat16>(lay, score, grad) : with_layout<float>(lay, score, grad);
+  SAO_TRY(st);
   return launch_end(slot, s);
 }
 
