@@ -38,9 +38,11 @@ __device__ __forceinline__ float teacher_logit(const void *a, sao_dtype adt, int
 // of V or more, or one id twice, is marked and raises SAO_DEVERR_TOP_ID.
 __global__ void __launch_bounds__(32 * kSortWarps)
     distill_sort_kernel(const int32_t *ids, const uint8_t *row_mask, int64_t N, int K, int kp, int V, int tiles,
-                        int32_t *sid, uint16_t *slot, uint16_t *off, int32_t *entries, unsigned int *err) {
+                        int32_t *sid, uint16_t *slot, uint16_t *off, int32_t *entries, unsigned int *range,
+                        unsigned int *err) {
   extern __shared__ uint64_t sort_smem[];
   grid_wait();
+  if (blockIdx.x == 0 && threadIdx.x < kRangeWords) range[threadIdx.x] = 0u;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t t = int64_t(blockIdx.x) * kSortWarps + warp;
   if (t >= N) return;
@@ -221,8 +223,9 @@ template <int kSub>
 __global__ void __launch_bounds__(256)
     distill_rows_kernel(const int32_t *ids, const void *a, sao_dtype adt, const float *teacher_lse, const float *lse,
                         const float *lse_rest, const float *z_top, const float *grad, int64_t N, int K, float inv_t,
-                        uint8_t *mask, float *g_rest, float *rest, float *dz_top) {
+                        uint8_t *mask, float *g_rest, float *rest, float *dz_top, unsigned int *range) {
   grid_wait();
+  if (blockIdx.x == 0 && threadIdx.x < kRangeWords) range[threadIdx.x] = 0u;
   const int64_t tid = int64_t(blockIdx.x) * blockDim.x + threadIdx.x;
   const int64_t row = tid / kSub;
   const int sub = int(tid % kSub);
@@ -349,6 +352,7 @@ struct FwdArrays {
   int32_t *sid, *entries;
   uint16_t *slot, *off;
   float *z;
+  unsigned int *range;
 };
 FwdArrays take_fwd(Carver &c, int64_t N, int32_t V, int32_t K) {
   const size_t nk = size_t(N) * size_t(K), tiles = (size_t(V) + kTopTile - 1) / kTopTile;
@@ -358,11 +362,13 @@ FwdArrays take_fwd(Carver &c, int64_t N, int32_t V, int32_t K) {
   f.slot = c.take<uint16_t>(nk);
   f.off = c.take<uint16_t>(size_t(N) * (tiles + 1));
   f.z = c.take<float>(nk);
+  f.range = c.take<unsigned int>(kRangeWords);
   return f;
 }
 struct BwdArrays {
   uint8_t *mask;
   float *g, *rest, *dz_top;
+  unsigned int *range;
 };
 BwdArrays take_bwd(Carver &c, int64_t N, int32_t K) {
   BwdArrays b;
@@ -370,6 +376,7 @@ BwdArrays take_bwd(Carver &c, int64_t N, int32_t K) {
   b.g = c.take<float>(size_t(N));
   b.rest = c.take<float>(size_t(N));
   b.dz_top = c.take<float>(size_t(N) * size_t(K));
+  b.range = c.take<unsigned int>(kRangeWords);
   return b;
 }
 
@@ -437,9 +444,9 @@ sao_status distill_fwd_launch(const void *H, const void *W, sao_dtype dt, const 
   int slot = launch_begin("distill_sort", s);
   pdl(distill_sort_kernel, unsigned((N + kSortWarps - 1) / kSortWarps), 32 * kSortWarps,
       size_t(kSortWarps) * kp * sizeof(uint64_t), s)(ids, row_mask, N, K, kp, V, tiles, w.sid, w.slot, w.off,
-                                                     w.entries, err);
+                                                     w.entries, w.range, err);
   SAO_TRY(launch_end(slot, s));
-  const TopRef top{w.sid, w.off, w.z, K, tiles, 1.f / temperature};
+  const TopRef top{w.sid, w.off, w.z, K, tiles, 1.f / temperature, w.range};
   const TopFinish f{a, adt, teacher_lse, w.slot, w.entries, row_mask, loss, lse, lse_rest, z_top, V};
   if (dt == SAO_BF16) return tc_distill_fwd(H, W, row_mask, N, h, V, top, f, err, c, s);
   return f32_distill_fwd(static_cast<const float *>(H), static_cast<const float *>(W), row_mask, N, h, V, top, f, err,
@@ -458,9 +465,9 @@ sao_status distill_bwd_launch(const void *H, const void *W, sao_dtype dt, const 
   const int sub = row_threads(N);
   int slot = launch_begin("distill_rows", s);
   pdl(sub == 32 ? distill_rows_kernel<32> : distill_rows_kernel<8>, unsigned((N * sub + 255) / 256), 256, 0, s)(
-      ids, a, adt, teacher_lse, lse, lse_rest, z_top, grad, N, K, inv_t, w.mask, w.g, w.rest, w.dz_top);
+      ids, a, adt, teacher_lse, lse, lse_rest, z_top, grad, N, K, inv_t, w.mask, w.g, w.rest, w.dz_top, w.range);
   SAO_TRY(launch_end(slot, s));
-  const TopGrad t{w.mask, w.g, w.rest, w.dz_top, ids, K, inv_t};
+  const TopGrad t{w.mask, w.g, w.rest, w.dz_top, ids, K, inv_t, w.range};
   if (dt == SAO_BF16) return tc_distill_bwd(H, W, t, N, h, V, dH, dW, dw_dt, accumulate, err, c, s);
   return f32_distill_bwd(static_cast<const float *>(H), static_cast<const float *>(W), t, N, h, V,
                          static_cast<float *>(dH), static_cast<float *>(dW), accumulate, err, c, s);

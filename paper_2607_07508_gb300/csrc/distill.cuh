@@ -25,6 +25,7 @@ struct TopRef {
   float *z;             // [N][K] out, in the order of id
   int K, tiles;
   float inv_t;          // 1 / temperature
+  unsigned int *range;  // fp32 heads: classes of the operands, cleared
 };
 
 // The backward's view of the rows: dZ[t, v] = g[t] exp(z[t, v] / T - rest[t]) on the
@@ -36,7 +37,9 @@ struct TopGrad {
   const int32_t *ids;    // [N][K], the caller's order; < 0: no entry
   int K;
   float inv_t;
+  unsigned int *range;   // fp32 heads: classes of the operands, cleared
 };
+constexpr int kRangeWords = 3;
 
 // A bf16 head of up to this many rows keeps its dZ as two bf16 pieces, the second one's
 // rows kFewRows after the first's in the same 128-row tile, with a copy of H's row, so

@@ -67,6 +67,7 @@ constexpr int ACCS = 2;                      // accumulators of 256 TMEM columns
 constexpr uint32_t TMEM_COLS = ACCS * TN;
 constexpr size_t SMEM_BYTES = 1024 + size_t(STAGES) * STAGE_BYTES + 256;
 static_assert(SMEM_BYTES <= 232448, "shared memory of an SM");
+constexpr float kLog2e = 1.4426950408889634f;
 constexpr int NUM_THREADS = 640;             // warp 0 TMA, warp 1 MMA, warps 4-19 accumulate and finish
 constexpr int HN = TN / 4;                   // columns per accumulating warp: four warps (128 rows) per quarter
 // Registers: the kernel starts with 96 a thread (61,440 for its 20 warps); the
@@ -75,6 +76,7 @@ constexpr int LAUNCH_REGS = 96, ISSUE_REGS = 40, SUM_REGS = 104;
 static_assert(128 * ISSUE_REGS + 512 * SUM_REGS <= NUM_THREADS * LAUNCH_REGS, "split within the launch's registers");
 constexpr unsigned SAFE_CLASSES = 2;  // 2^26 x 2^100, 2^62 x 2^62: products up to 2^126
 enum Operand : int { kOpH = 0, kOpW = 1, kOpDZ = 2, kOperands = 3 };
+static_assert(kOperands == kRangeWords, "classes cleared by the distillation's row kernels");
 constexpr int64_t MAX_ROWS = int64_t(65535) * 64;
 
 // kTopLogits, kTopDLogits: the two of a teacher's top logits (distill.cu)
@@ -504,7 +506,7 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
     }
     for (int a = 0; a < ACCS; ++a) {
       mbar_init(smem_u32(&ctl->acc_full[a]), 1);
-      mbar_init(smem_u32(&ctl->acc_empty[a]), 512);
+      mbar_init(smem_u32(&ctl->acc_empty[a]), 16);
     }
     fence_barrier_init();
   }
@@ -686,7 +688,8 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
           }
         }
         fence_before_sync();
-        mbar_arrive(smem_u32(&ctl->acc_empty[a]));
+        __syncwarp();  // one arrival a warp
+        if (lane == 0) mbar_arrive(smem_u32(&ctl->acc_empty[a]));
         if (++a == ACCS) {
           a = 0;
           a_phase ^= 1u;
@@ -744,7 +747,12 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
 #pragma unroll
         for (int j = 1; j < HN; ++j) mx = fmaxf(mx, z[j]);
         float s[4] = {0.f, 0.f, 0.f, 0.f};
-        if (kKind == kLogits || mx != -INFINITY) {  // (the entries may be all of the quarter tile)
+        if constexpr (kKind == kTopLogits) {
+          if (mx != -INFINITY) {  // (the entries may be all of the quarter tile)
+#pragma unroll
+            for (int j = 0; j < HN; ++j) s[j & 3] += ex2_approx((z[j] - mx) * kLog2e);
+          }
+        } else {
 #pragma unroll
           for (int j = 0; j < HN; ++j) s[j & 3] += expf(z[j] - mx);
         }
@@ -761,8 +769,8 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
         float most = 0.f;
 #pragma unroll
         for (int j = 0; j < HN; ++j) {
-          if constexpr (kKind == kTopDLogits)
-            z[j] = g != 0.f ? g * expf(z[j] * p.inv_t - l) : 0.f;
+          if constexpr (kKind == kTopDLogits)  // (an exponent of t off by 2^-24 t, as expf's argument is)
+            z[j] = g != 0.f ? g * ex2_approx(fmaf(z[j], p.inv_t, -l) * kLog2e) : 0.f;
           else
             z[j] = g != 0.f ? g * ((j == yy ? 1.f : 0.f) - expf(z[j] - l)) : 0.f;
           most = larger(most, z[j]);
@@ -995,9 +1003,9 @@ sao_status f32_logits(const float *H, const float *W, const int32_t *y, const To
   if (N > MAX_ROWS) return fail(SAO_ERR_SHAPE, "fp32 path supports at most %lld tokens", (long long)MAX_ROWS);
   const F32Plan q = f32_plan(N, h, V);
   const int nvt = (V + HN - 1) / HN;  // partials: quarter tiles that hold a column
-  unsigned int *range = c.take<unsigned int>(kOperands);
+  unsigned int *range = top ? top->range : c.take<unsigned int>(kOperands);
   RowList list{};
-  SAO_TRY(clear_scratch(range, kOperands * sizeof(unsigned int), s));
+  if (!top) SAO_TRY(clear_scratch(range, kOperands * sizeof(unsigned int), s));
   // Rows left out save nothing while all of them fit in one wave of 152 tiles, and listing
   // them is two launches (200 rows of h = 96, V = 1000: 19.3 us with the list, 14.5
   // without); the merge then skips them.
@@ -1074,9 +1082,9 @@ sao_status f32_backward(const float *H, const float *W, const int32_t *y, const 
                         unsigned int *err, Carver &c, cudaStream_t s) {
   if (N > MAX_ROWS || (int64_t(h) + 63) / 64 > 65535) return fail(SAO_ERR_SHAPE, "fp32 path size limit exceeded");
   const F32Plan q = f32_plan(N, h, V);
-  unsigned int *range = c.take<unsigned int>(kOperands);
+  unsigned int *range = top ? top->range : c.take<unsigned int>(kOperands);
   RowList list{};
-  SAO_TRY(clear_scratch(range, kOperands * sizeof(unsigned int), s));
+  if (!top) SAO_TRY(clear_scratch(range, kOperands * sizeof(unsigned int), s));
   SAO_TRY(list_rows(top ? top->mask : nullptr, G, N, &list, c, s));
   __nv_bfloat16 *hpl = c.take<__nv_bfloat16>(size_t(PL) * size_t(q.cap) * size_t(q.hp));
   __nv_bfloat16 *wpl = c.take<__nv_bfloat16>(size_t(PL) * size_t(q.vc_bwd) * size_t(q.hp));

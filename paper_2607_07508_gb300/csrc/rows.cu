@@ -251,10 +251,12 @@ sao_status list_rows(const uint8_t *mask, const float *g, int64_t N, RowList *ou
   out->pos = c.take<int>(size_t(N));
   out->count = count;
   if (!c.ok()) return fail(SAO_ERR_WORKSPACE, "workspace too small for row compaction");
+  if (nblocks > 1) {  // (one block's rows are counted as they are listed)
+    int slot = launch_begin("compact_rows", s);
+    pdl(compact_count_kernel, unsigned(nblocks), kScanThreads, 0, s)(mask, g, N, block);
+    SAO_TRY(launch_end(slot, s));
+  }
   int slot = launch_begin("compact_rows", s);
-  pdl(compact_count_kernel, unsigned(nblocks), kScanThreads, 0, s)(mask, g, N, block);
-  SAO_TRY(launch_end(slot, s));
-  slot = launch_begin("compact_rows", s);
   const bool scan = nblocks > kAddBlocks;
   if (scan) {
     pdl(compact_scan_kernel, 1, 1024, 0, s)(block, int(nblocks), count);
