@@ -77,15 +77,17 @@ __device__ __forceinline__ int64_t seg_at(const BalanceArgs &a, int b) {
   const int64_t v = ld(a.cu + b);
   return v < 0 ? 0 : v > a.N ? a.N : v;
 }
-// The segment that holds row r: the last one that starts at or before it.
+// The segment that holds row r, the last one that starts at or before it (whole warps; 32
+// starts a round, where a search by halves would wait for memory five times).
 __device__ __forceinline__ int seg_of(const BalanceArgs &a, int64_t r) {
-  int lo = 0, hi = a.B - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (seg_at(a, mid) <= r)
-      lo = mid;
-    else
-      hi = mid - 1;
+  const int lane = threadIdx.x & 31;
+  int lo = 0;
+  for (int n = a.B; n > 1;) {  // it is one of lo .. lo + n - 1
+    const int stride = (n + 31) / 32, at = lane * stride;
+    const unsigned after = ~__ballot_sync(0xffffffffu, at < n && (at == 0 || seg_at(a, lo + at) <= r));
+    const int k = after == 0u ? 31 : __ffs(after) - 2;  // the last lane of the leading ones that start before
+    lo += k * stride;
+    n = n - k * stride < stride ? n - k * stride : stride;
   }
   return lo;
 }
@@ -595,6 +597,7 @@ __global__ void __launch_bounds__(kThreads<T, kVec, kC>)
   const int groups = 32 / lanes, l = lane & (lanes - 1);
   const int64_t r0 = int64_t(blockIdx.x) * a.chunk, r1 = r0 + a.chunk < a.N ? r0 + a.chunk : a.N;
   const Rows own = a.cu ? cta_rows(r0, r1, warp, kWarps, groups) : grid_rows(a, warp, kWarps, groups);
+  int b = seg_of(a, own.first < a.N ? own.first : a.N - 1);
   int64_t seg_end = -1;  // from this row on the weights are another segment's
   float w[kC];
 #pragma unroll
@@ -606,9 +609,8 @@ __global__ void __launch_bounds__(kThreads<T, kVec, kC>)
   for (int64_t r = first; x.left > 0; r += own.step) {
     const bool on = x.on();
     if (on && r >= seg_end) {
-      const int b = seg_of(a, r);
+      while (b + 1 < a.B && seg_at(a, b + 1) <= r) ++b;
       seg_end = b + 1 < a.B ? seg_at(a, b + 1) : a.N;
-      if (seg_end <= r) seg_end = r + 1;  // (cu_seqlens that do not rise)
       const float n = float(ld(rows + b));
       const float f = n > 0.f ? g * float(a.E) / (float(a.k) * n * n * float(used)) : 0.f;
 #pragma unroll
