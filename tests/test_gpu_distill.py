@@ -140,6 +140,39 @@ def test_against_fp64(N, h, V, K, rest, dtype):
     assert np.abs(got["z_top"] - np.where(valid, ref["z_top"], 0)).max() <= bound(c) + 2 * U * np.abs(ref["z_top"]).max()
 
 
+@pytest.mark.parametrize("N,h,V,K", [(1, 8, 9, 4), (1, 2048, 5003, 20), (1, 2056, 700, 33), (1, 6144, 900, 7), (1, 6152, 900, 7),
+                                     (2, 1000, 2500, 300), (2, 4096, 311, 64), (3, 2048, 2000, 50), (4, 520, 80000, 1024),
+                                     (4, 2056, 300, 12), (2, 16, 400000, 100)])
+def test_few_rows(N, h, V, K):
+    """One or two rows of a bf16 head go through W in one pass: sums in fp32 throughout, dZ unrounded."""
+    for rest in (False, True):
+        g = torch.Generator().manual_seed(h)
+        c = _case(N, h, min(V, 50000), K, seed=V, rest=False, scale=0.02)
+        c["W"] = (torch.randn(V, h, generator=g) * 0.02).bfloat16()
+        r = np.random.Generator(np.random.PCG64(V))
+        ids = np.stack([r.permutation(V)[:K] for _ in range(N)]).astype(np.int32)
+        c["ids"] = np.where(c["ids"] >= 0, ids, -1).astype(np.int32)
+        if rest:
+            with_rest(c, r)
+        c["G"] = r.normal(size=N).astype(np.float32)
+        if N > 1:
+            c["mask"] = np.ones(N, np.uint8)
+            c["mask"][1], c["G"][1] = 0, 0
+            c["H"][1] = float("nan")
+        else:
+            c["T"] = 0.7
+            if rest:
+                with_rest(c, r)
+        clean = {**c, "H": torch.nan_to_num(c["H"])}
+        ref = want(clean)
+        close(run(c), ref, clean)
+        if h * V < 1 << 23:
+            close(run(c, dw="f32"), ref, clean, dw_tol=1e-5 if h <= (6144 if N == 1 else 2048 if N == 2 else 0) else 2.0 ** -8)
+            prev = torch.randn(V, h) * 0.01
+            got = run(c, prev=prev)
+            assert np.linalg.norm(got["dW"] - prev.double().numpy() - ref["dW"]) <= 2.0 ** -8 * np.linalg.norm(ref["dW"])
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("V,K", [(5, 5), (256, 256), (300, 300), (1100, 1024)])
 def test_entries_that_fill_tiles_or_the_vocabulary(V, K, dtype):
