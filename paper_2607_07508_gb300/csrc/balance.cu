@@ -49,12 +49,12 @@ constexpr int depth_of(bool async, int size, int columns) {
 }
 template <class T, int kVec, int kC>
 constexpr int kDepthOf = depth_of(kAsync<T, kVec>, int(sizeof(T)), kC);
-// Bytes of their slots, and of the expert ids' (kIds a row and thread).
+// Bytes of a thread's slots, and of its expert ids' (kIds a row).
 constexpr int kIds = 2;
 template <class T, int kVec, int kC>
-constexpr int kRing = kAsync<T, kVec> ? kThreads<T, kVec, kC> * kC * int(sizeof(T)) * kDepthOf<T, kVec, kC> : 0;
+constexpr int kRing = kAsync<T, kVec> ? kC * int(sizeof(T)) * kDepthOf<T, kVec, kC> : 0;
 template <class T, int kVec, int kC>
-constexpr int kIdRing = kThreads<T, kVec, kC> * kIds * 4 * kDepthOf<T, kVec, kC>;
+constexpr int kIdRing = kIds * 4 * kDepthOf<T, kVec, kC>;
 
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -166,7 +166,7 @@ struct Stream {
   static constexpr bool kSlots = kAsync<T, kVec>;
   static constexpr int kDepth = kDepthOf<T, kVec, kC>, kLoads = kC / kVec;
   static constexpr int kBytes = kVec * int(sizeof(T));
-  static constexpr uint32_t kPitch = kThreads<T, kVec, kC> * uint32_t(kBytes);  // from a load's slots to the next one's
+  __device__ __forceinline__ uint32_t pitch() const { return blockDim.x * uint32_t(kBytes); }  // from a load's slots to the next one's
   const T *src;         // this lane's first column of the row kDepth steps ahead
   const int32_t *ids;   // this lane's first id of that row, or null
   const uint8_t *mask;  // of the warp's first row 64 steps after the last refill, or null
@@ -195,16 +195,16 @@ struct Stream {
   __device__ __forceinline__ void fetch(int slot, bool live) {
     if (live) {
       if constexpr (kSlots) {
-        const uint32_t dst = slots + uint32_t(slot * kLoads) * kPitch;
+        const uint32_t dst = slots + uint32_t(slot * kLoads) * pitch();
 #pragma unroll
         for (int v = 0; v < kLoads; ++v)
-          if ((l + v * lanes) * kVec < E) copy_async<kBytes>(dst + v * kPitch, src + v * lanes * kVec);
+          if ((l + v * lanes) * kVec < E) copy_async<kBytes>(dst + v * pitch(), src + v * lanes * kVec);
       }
       if (ids) {
 #pragma unroll
         for (int i = 0; i < kIds; ++i)
           if (l + i * lanes < k)
-            copy_async<4>(id_slots + uint32_t(slot * kIds + i) * (kThreads<T, kVec, kC> * 4u), ids + i * lanes);
+            copy_async<4>(id_slots + uint32_t(slot * kIds + i) * (blockDim.x * 4u), ids + i * lanes);
       }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
@@ -241,7 +241,7 @@ struct Stream {
           for (int d = 0; d < kDepth; ++d)
 #pragma unroll
             for (int w = 0; w < kBytes; w += 4)
-              asm volatile("st.shared.b32 [%0], %1;" ::"r"(slots + uint32_t(d * kLoads + v) * kPitch + w), "r"(none)
+              asm volatile("st.shared.b32 [%0], %1;" ::"r"(slots + uint32_t(d * kLoads + v) * pitch() + w), "r"(none)
                            : "memory");
     }
 #pragma unroll
@@ -259,16 +259,16 @@ struct Stream {
   __device__ __forceinline__ Row<T, kVec, kC> row() const {
     if constexpr (kSlots) {
       Row<T, kVec, kC> x;
-      const uint32_t at = slots + uint32_t(cur * kLoads) * kPitch;
+      const uint32_t at = slots + uint32_t(cur * kLoads) * pitch();
 #pragma unroll
       for (int v = 0; v < kLoads; ++v) {
         if constexpr (kBytes == 16)
           asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
                        : "=r"(x.raw[4 * v]), "=r"(x.raw[4 * v + 1]), "=r"(x.raw[4 * v + 2]), "=r"(x.raw[4 * v + 3])
-                       : "r"(at + v * kPitch)
+                       : "r"(at + v * pitch())
                        : "memory");
         else
-          asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x.raw[v]) : "r"(at + v * kPitch) : "memory");
+          asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x.raw[v]) : "r"(at + v * pitch()) : "memory");
       }
       return x;
     } else {
@@ -280,7 +280,7 @@ struct Stream {
     int v;
     asm volatile("ld.shared.b32 %0, [%1];"
                  : "=r"(v)
-                 : "r"(id_slots + uint32_t(cur * kIds + i) * (kThreads<T, kVec, kC> * 4u))
+                 : "r"(id_slots + uint32_t(cur * kIds + i) * (blockDim.x * 4u))
                  : "memory");
     return v;
   }
@@ -393,18 +393,18 @@ __device__ __forceinline__ void for_segments(const BalanceArgs &a, int c, F f) {
 template <class T, int kVec, int kC, bool kSigmoid>
 __global__ void __launch_bounds__(kThreads<T, kVec, kC>)
     balance_partial_kernel(const BalanceArgs a, int lanes, float *psum, int *pcount, int *prows, unsigned int *ticket) {
-  constexpr int kBlock = kThreads<T, kVec, kC>, kWarps = kBlock / 32;
-  extern __shared__ uint4 smem[];  // the stream's slots, sums [kWarps][E], counts [E]
-  __shared__ int n_rows[kWarps];
+  extern __shared__ uint4 smem[];  // the stream's slots, ids', sums [warps][E], counts [E]
+  __shared__ int n_rows[32];
+  const int block = blockDim.x, warps = block >> 5;
   grid_wait();
   if (blockIdx.x == 0 && threadIdx.x == 0) *ticket = 0;
-  const void *id_ring = smem + kRing<T, kVec, kC> / 16;
-  float *sums = reinterpret_cast<float *>(smem + (kRing<T, kVec, kC> + kIdRing<T, kVec, kC>) / 16);
-  int *counts = reinterpret_cast<int *>(sums + kWarps * a.E);
+  const uint4 *id_ring = smem + block * kRing<T, kVec, kC> / 16;
+  float *sums = reinterpret_cast<float *>(const_cast<uint4 *>(id_ring) + block * kIdRing<T, kVec, kC> / 16);
+  int *counts = reinterpret_cast<int *>(sums + warps * a.E);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int groups = 32 / lanes, l = lane & (lanes - 1);
   for_segments(a, blockIdx.x, [&](int b, int64_t r0, int64_t r1) {
-    for (int e = threadIdx.x; e < a.E; e += kBlock) counts[e] = 0;
+    for (int e = threadIdx.x; e < a.E; e += block) counts[e] = 0;
     __syncthreads();
     float acc[kC];
 #pragma unroll
@@ -416,7 +416,7 @@ __global__ void __launch_bounds__(kThreads<T, kVec, kC>)
       else if (id >= 0)
         raise_device_error(a.err, SAO_DEVERR_EXPERT_ID);
     };
-    const Rows rows = a.cu ? cta_rows(r0, r1, warp, kWarps, groups) : grid_rows(a, warp, kWarps, groups);
+    const Rows rows = a.cu ? cta_rows(r0, r1, warp, warps, groups) : grid_rows(a, warp, warps, groups);
     Stream<T, kVec, kC> x(a, rows, l, lanes, a.ids, smem, id_ring);
     for (int64_t r = rows.first + lane / lanes; x.left > 0; r += rows.step) {  // the warp's lanes stay together
       x.wait();
@@ -452,16 +452,16 @@ __global__ void __launch_bounds__(kThreads<T, kVec, kC>)
     if (lane == 0) n_rows[warp] = n;
     __syncthreads();
     const int64_t slot = int64_t(blockIdx.x) + b;
-    for (int e = threadIdx.x; e < a.E; e += kBlock) {
+    for (int e = threadIdx.x; e < a.E; e += block) {
       float v = 0.f;
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) v += sums[w * a.E + e];
+#pragma unroll 4
+      for (int w = 0; w < warps; ++w) v += sums[w * a.E + e];
       psum[slot * a.E + e] = v;
       pcount[slot * a.E + e] = counts[e];
     }
     if (threadIdx.x == 0) {
       int t = 0;
-      for (int w = 0; w < kWarps; ++w) t += n_rows[w];
+      for (int w = 0; w < warps; ++w) t += n_rows[w];
       prows[slot] = t;
     }
     __syncthreads();
@@ -581,22 +581,22 @@ template <class T, int kVec, int kC, bool kSigmoid>
 __global__ void __launch_bounds__(kThreads<T, kVec, kC>)
     balance_grad_kernel(const BalanceArgs a, int lanes, const int64_t *counts, const int64_t *rows,
                         const float *grad_loss, T *dx) {
-  constexpr int kBlock = kThreads<T, kVec, kC>, kWarps = kBlock / 32;
-  __shared__ int sh_used[kWarps];
+  const int block = blockDim.x, warps = block >> 5;
+  __shared__ int sh_used[32];
   grid_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   int used = 0;
-  for (int i = threadIdx.x; i < a.B; i += kBlock) used += ld(rows + i) > 0;
+  for (int i = threadIdx.x; i < a.B; i += block) used += ld(rows + i) > 0;
   used = __reduce_add_sync(0xffffffffu, used);
   if (lane == 0) sh_used[warp] = used;
   __syncthreads();
   used = 0;
-  for (int i = 0; i < kWarps; ++i) used += sh_used[i];
+  for (int i = 0; i < warps; ++i) used += sh_used[i];
   extern __shared__ uint4 smem[];  // the stream's slots
   const float g = ld(grad_loss);
   const int groups = 32 / lanes, l = lane & (lanes - 1);
   const int64_t r0 = int64_t(blockIdx.x) * a.chunk, r1 = r0 + a.chunk < a.N ? r0 + a.chunk : a.N;
-  const Rows own = a.cu ? cta_rows(r0, r1, warp, kWarps, groups) : grid_rows(a, warp, kWarps, groups);
+  const Rows own = a.cu ? cta_rows(r0, r1, warp, warps, groups) : grid_rows(a, warp, warps, groups);
   int b = seg_of(a, own.first < a.N ? own.first : a.N - 1);
   int64_t seg_end = -1;  // from this row on the weights are another segment's
   float w[kC];
@@ -706,6 +706,14 @@ BalanceArgs make_args(const void *x, const int32_t *ids, const uint8_t *mask, co
   return a;
 }
 
+// Threads of a launch: no more warps than a CTA has rows for. (All of them, and their slots' shared
+// memory, made a launch of a few rows 4 us longer.)
+int block_of(int most, int chunk, int lanes) {
+  const int groups = 32 / lanes, warps = (chunk + groups - 1) / groups;
+  return warps * 32 < most ? warps * 32 : most;
+}
+constexpr size_t kPlainSmem = 40u << 10;  // dynamic shared memory that any kernel may have
+
 // Lets the kernel have an SM's shared memory (once per device).
 template <auto kKernel>
 sao_status allow_smem() {
@@ -757,13 +765,12 @@ sao_status balance_fwd_launch(const void *x, sao_dtype dt, const int32_t *ids, c
   sao_status st = SAO_OK;
   auto partial = [&](auto t, auto vec, auto columns, auto sig) {
     using T = decltype(t);
-    constexpr int kBlock = kThreads<T, vec.value, columns.value>;
     auto kern = balance_partial_kernel<T, vec.value, columns.value, sig.value>;
-    const size_t smem = kRing<T, vec.value, columns.value> + kIdRing<T, vec.value, columns.value> +
-                        size_t(E) * (kBlock / 32 + 1) * sizeof(float);
-    st = allow_smem<balance_partial_kernel<T, vec.value, columns.value, sig.value>>();
-    if (st == SAO_OK)
-      pdl(kern, unsigned(a.chunks), kBlock, smem, s)(a, lay.lanes, w.psum, w.pcount, w.prows, w.ticket);
+    const int block = block_of(kThreads<T, vec.value, columns.value>, a.chunk, lay.lanes);
+    const size_t smem = size_t(block) * (kRing<T, vec.value, columns.value> + kIdRing<T, vec.value, columns.value>) +
+                        size_t(E) * (block / 32 + 1) * sizeof(float);
+    if (smem > kPlainSmem) st = allow_smem<balance_partial_kernel<T, vec.value, columns.value, sig.value>>();
+    if (st == SAO_OK) pdl(kern, unsigned(a.chunks), block, smem, s)(a, lay.lanes, w.psum, w.pcount, w.prows, w.ticket);
   };
   dt == SAO_BF16 ? with_layout<__nv_bfloat16>(lay, score, partial) : with_layout<float>(lay, score, partial);
   SAO_TRY(st);
@@ -787,10 +794,11 @@ sao_status balance_bwd_launch(const void *x, sao_dtype dt, const uint8_t *mask, 
   auto grad = [&](auto t, auto vec, auto columns, auto sig) {
     using T = decltype(t);
     auto kern = balance_grad_kernel<T, vec.value, columns.value, sig.value>;
-    st = allow_smem<balance_grad_kernel<T, vec.value, columns.value, sig.value>>();
+    const int block = block_of(kThreads<T, vec.value, columns.value>, a.chunk, lay.lanes);
+    const size_t smem = size_t(block) * kRing<T, vec.value, columns.value>;
+    if (smem > kPlainSmem) st = allow_smem<balance_grad_kernel<T, vec.value, columns.value, sig.value>>();
     if (st == SAO_OK)
-      pdl(kern, unsigned(a.chunks), kThreads<T, vec.value, columns.value>, size_t(kRing<T, vec.value, columns.value>), s)(
-          a, lay.lanes, counts, rows, grad_loss, static_cast<T *>(dx));
+      pdl(kern, unsigned(a.chunks), block, smem, s)(a, lay.lanes, counts, rows, grad_loss, static_cast<T *>(dx));
   };
   dt == SAO_BF16 ? with_layout<__nv_bfloat16>(lay, score, grad) : with_layout<float>(lay, score, grad);
   SAO_TRY(st);
