@@ -170,8 +170,10 @@ struct Stream {
   const T *src;         // this lane's first column of the row kDepth steps ahead
   const int32_t *ids;   // this lane's first id of that row, or null
   const uint8_t *mask;  // of the warp's first row 64 steps after the last refill, or null
+  int64_t src_step, ids_step;
   int left;             // rows from the warp's first row of this step to the end
-  int step, E, k, l, lanes, cur = 0, seen = 0;
+  int step, k, l, lanes, cur = 0, seen = 0;
+  int loads;            // this lane's loads that are in the row
   uint64_t on_bits;     // bit d: the row d steps ahead is counted
   uint32_t slots, id_slots;  // shared-memory addresses of this thread's first ones
   Row<T, kVec, kC> reg[kSlots ? 1 : kDepth];
@@ -198,7 +200,7 @@ struct Stream {
         const uint32_t dst = slots + uint32_t(slot * kLoads) * pitch();
 #pragma unroll
         for (int v = 0; v < kLoads; ++v)
-          if ((l + v * lanes) * kVec < E) copy_async<kBytes>(dst + v * pitch(), src + v * lanes * kVec);
+          if (v < loads) copy_async<kBytes>(dst + v * pitch(), src + v * lanes * kVec);
       }
       if (ids) {
 #pragma unroll
@@ -213,7 +215,7 @@ struct Stream {
 #pragma unroll
       for (int v = 0; v < kLoads; ++v) {
         uint32_t w = none;
-        if (live && l + v * lanes < E) w = ld(reinterpret_cast<const uint16_t *>(src) + v * lanes);
+        if (live && v < loads) w = ld(reinterpret_cast<const uint16_t *>(src) + v * lanes);
         reg[kDepth - 1].raw[v] = w;
       }
     }
@@ -221,10 +223,12 @@ struct Stream {
   // `lane_ids`: expert ids [N, k], or null.
   __device__ __forceinline__ Stream(const BalanceArgs &a, const Rows &rows, int lane, int group, const int32_t *lane_ids,
                                     const void *ring, const void *id_ring)
-      : left(int(rows.end > rows.first ? rows.end - rows.first : 0)), step(rows.step), E(a.E), k(a.k), l(lane),
-        lanes(group) {
+      : left(int(rows.end > rows.first ? rows.end - rows.first : 0)), step(rows.step), k(a.k), l(lane),
+        lanes(group), loads((a.E / kVec - lane + group - 1) / group) {
     const int64_t warp_first = rows.first, first = warp_first + (threadIdx.x & 31) / group;
     src = static_cast<const T *>(a.x) + first * a.E + lane * kVec;
+    src_step = int64_t(step) * a.E;
+    ids_step = int64_t(step) * a.k;
     ids = lane_ids ? lane_ids + first * a.k + lane : nullptr;
     mask = a.mask ? a.mask + warp_first : nullptr;
     on_bits = counted32(mask, left) |
@@ -237,7 +241,7 @@ struct Stream {
       constexpr uint32_t none = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;
 #pragma unroll
       for (int v = 0; v < kLoads; ++v)
-        if ((l + v * lanes) * kVec >= E)
+        if (v >= loads)
           for (int d = 0; d < kDepth; ++d)
 #pragma unroll
             for (int w = 0; w < kBytes; w += 4)
@@ -249,8 +253,8 @@ struct Stream {
       if constexpr (!kSlots)
         if (d > 0) reg[d - 1] = reg[kDepth - 1];
       fetch(d, on_bits >> d & 1u);
-      src += int64_t(step) * E;
-      if (ids) ids += int64_t(step) * k;
+      src += src_step;
+      if (ids) ids += ids_step;
     }
   }
   __device__ __forceinline__ bool on() const { return on_bits & 1u; }
@@ -291,10 +295,10 @@ struct Stream {
       for (int d = 1; d < kDepth; ++d) reg[d - 1] = reg[d];
     }
     fetch(cur, on_bits >> kDepth & 1u);
-    src += int64_t(step) * E;
-    if (ids) ids += int64_t(step) * k;
+    src += src_step;
+    if (ids) ids += ids_step;
     on_bits >>= 1;
-    left = past(1);
+    left = left > step ? left - step : 0;
     if (++cur == kDepth) cur = 0;
     if (++seen == 32) {
       seen = 0;
@@ -693,22 +697,27 @@ void with_layout(const Layout &l, int score, F f) {
   score == SAO_SCORE_SIGMOID ? loads(std::true_type{}) : loads(std::false_type{});
 }
 
-// Rows per CTA: one on each of 152 SMs, or 64 rows. From N alone: the sums' order does
-// not depend on the device.
-int chunk_rows(int64_t N) {
-  const int64_t c = (N + 151) / 152;
+// CTAs on each of 152 SMs. One for a batch, whose rows they share evenly. Four, of a quarter of the
+// threads, where trajectories are balanced by themselves: a CTA that meets the end of
+// one adds up its sums twice, and the others of its SM work on (65,536 x 256 in 16
+// trajectories 47 -> 42 us, 98,301 x 63 in 96 42 -> 37; a batch of 65,536 x 128 30 -> 37).
+int ctas_of(bool segments) { return segments ? 4 : 1; }
+// Rows per CTA, at least 64. From N alone: the sums' order does not depend on the device.
+int chunk_rows(int64_t N, bool segments) {
+  const int64_t ctas = 152 * ctas_of(segments), c = (N + ctas - 1) / ctas;
   return int(c < 64 ? 64 : c);
 }
 BalanceArgs make_args(const void *x, const int32_t *ids, const uint8_t *mask, const int32_t *cu, int32_t B, int64_t N,
                       int32_t E, int32_t k, unsigned int *err) {
-  BalanceArgs a{x, ids, mask, cu, cu ? B : 1, N, E, k, chunk_rows(N), 0, err};
+  BalanceArgs a{x, ids, mask, cu, cu ? B : 1, N, E, k, chunk_rows(N, cu != nullptr), 0, err};
   a.chunks = int((N + a.chunk - 1) / a.chunk);
   return a;
 }
 
 // Threads of a launch: no more warps than a CTA has rows for. (All of them, and their slots' shared
 // memory, made a launch of a few rows 4 us longer.)
-int block_of(int most, int chunk, int lanes) {
+int block_of(int most, int chunk, int lanes, bool segments) {
+  most = most / ctas_of(segments) / 32 * 32;
   const int groups = 32 / lanes, warps = (chunk + groups - 1) / groups;
   return warps * 32 < most ? warps * 32 : most;
 }
@@ -733,7 +742,7 @@ struct Scratch {
   unsigned int *ticket;
 };
 Scratch take(Carver &c, int64_t N, int32_t E, int32_t B) {
-  const int64_t chunk = chunk_rows(N);
+  const int64_t chunk = chunk_rows(N, true);  // (a batch takes fewer)
   const size_t slots = size_t((N + chunk - 1) / chunk) + size_t(B);
   Scratch s;
   s.psum = c.take<float>(slots * size_t(E));
@@ -766,7 +775,7 @@ sao_status balance_fwd_launch(const void *x, sao_dtype dt, const int32_t *ids, c
   auto partial = [&](auto t, auto vec, auto columns, auto sig) {
     using T = decltype(t);
     auto kern = balance_partial_kernel<T, vec.value, columns.value, sig.value>;
-    const int block = block_of(kThreads<T, vec.value, columns.value>, a.chunk, lay.lanes);
+    const int block = block_of(kThreads<T, vec.value, columns.value>, a.chunk, lay.lanes, a.cu != nullptr);
     const size_t smem = size_t(block) * (kRing<T, vec.value, columns.value> + kIdRing<T, vec.value, columns.value>) +
                         size_t(E) * (block / 32 + 1) * sizeof(float);
     if (smem > kPlainSmem) st = allow_smem<balance_partial_kernel<T, vec.value, columns.value, sig.value>>();
@@ -794,7 +803,7 @@ sao_status balance_bwd_launch(const void *x, sao_dtype dt, const uint8_t *mask, 
   auto grad = [&](auto t, auto vec, auto columns, auto sig) {
     using T = decltype(t);
     auto kern = balance_grad_kernel<T, vec.value, columns.value, sig.value>;
-    const int block = block_of(kThreads<T, vec.value, columns.value>, a.chunk, lay.lanes);
+    const int block = block_of(kThreads<T, vec.value, columns.value>, a.chunk, lay.lanes, a.cu != nullptr);
     const size_t smem = size_t(block) * kRing<T, vec.value, columns.value>;
     if (smem > kPlainSmem) st = allow_smem<balance_grad_kernel<T, vec.value, columns.value, sig.value>>();
     if (st == SAO_OK)
