@@ -462,8 +462,9 @@ SAO_API sao_status sao_value_loss(const float *values, const float *ret, const u
  * loss 0 and no gradient. A row with an id out of range or there twice has loss
  * NaN (and SAO_DEVERR_TOP_ID). lse_rest is NaN on the rows that take no gradient:
  * masked ones, and those whose loss is not finite or has nothing to learn from.
- * bf16 logits are added up in fp32 every 256 elements of h (the tensor cores'
- * own sums truncate): lse within 3e-7 of itself at h = 2,048.
+ * bf16 H and W are 16-byte aligned. Their logits' sums leave the tensor cores,
+ * which truncate as they add, every 512 elements of h and go on in fp32: lse is
+ * within 5e-7 of itself up to h = 6,144.
  * The workspace of both calls: sao_distill_workspace_bytes.
  */
 SAO_API size_t sao_distill_workspace_bytes(int64_t N, int32_t h, int32_t V, int32_t K, sao_dtype dt);
@@ -483,8 +484,9 @@ SAO_API sao_status sao_distill_loss_fwd(const void *H, const void *W, sao_dtype 
  *   dW [V, h] dw_dt       SAO_F32, overwritten or (accumulate_dW != 0) added to,
  *                         so that it adds to another loss's dW; or for a bf16 head
  *                         SAO_BF16, overwritten only (a sum over calls needs fp32)
- * For a bf16 head dZ is rounded to bf16 once before the two products (as in
- * sao_token_logprobs_bwd): 2^-9 of each of its elements.
+ * A bf16 head's dH and dW are 16-byte aligned. Its dZ is rounded to bf16 once
+ * before the two products (as in sao_token_logprobs_bwd): 2^-9 of each of its
+ * elements, 2^-17 up to 64 rows, not at all for one row.
  */
 SAO_API sao_status sao_distill_loss_bwd(const void *H, const void *W, sao_dtype dt, const int32_t *top_ids,
                                         const void *top_logits, sao_dtype top_dt, const float *teacher_lse,

@@ -156,9 +156,9 @@ __device__ __forceinline__ void copy_async(uint32_t dst, const void *src) {
 }
 
 // The rows first, first + step, ... that a group of lanes goes through, those ahead
-// already on their way into slots of the thread's own (no barrier). Rows that are not
-// counted are not read (their words are anything), and columns past E read as -inf: they
-// have no score. What a row needs is asked for kDepth rows before, its expert ids too, and
+// already on their way into slots of the thread's own (no barrier). The words of rows that
+// are not counted are anything (but for the first few rows they are not read), and
+// columns past E read as -inf: they have no score. What a row needs is asked for kDepth rows before, its expert ids too, and
 // the mask 32 rows at a time: with one row ahead, or a byte of the mask read per row, the
 // kernels waited for memory half of their time (2^20 x 160 bf16 forward 93-128 us).
 template <class T, int kVec, int kC>
@@ -230,10 +230,6 @@ struct Stream {
     src_step = int64_t(step) * a.E;
     ids_step = int64_t(step) * a.k;
     ids = lane_ids ? lane_ids + first * a.k + lane : nullptr;
-    mask = a.mask ? a.mask + warp_first : nullptr;
-    on_bits = counted32(mask, left) |
-              uint64_t(counted32(mask ? mask + 32 * int64_t(step) : nullptr, past(32))) << 32;
-    if (mask) mask += 64 * int64_t(step);
     id_slots = tc::smem_u32(id_ring) + threadIdx.x * 4u;
     slots = 0;
     if constexpr (kSlots) {
@@ -248,14 +244,20 @@ struct Stream {
               asm volatile("st.shared.b32 [%0], %1;" ::"r"(slots + uint32_t(d * kLoads + v) * pitch() + w), "r"(none)
                            : "memory");
     }
+    // the first rows, counted or not: the mask is on its way as well
+    const int mine = (threadIdx.x & 31) / group;
 #pragma unroll
     for (int d = 0; d < kDepth; ++d) {
       if constexpr (!kSlots)
         if (d > 0) reg[d - 1] = reg[kDepth - 1];
-      fetch(d, on_bits >> d & 1u);
+      fetch(d, mine < past(d));
       src += src_step;
       if (ids) ids += ids_step;
     }
+    mask = a.mask ? a.mask + warp_first : nullptr;
+    on_bits = counted32(mask, left) |
+              uint64_t(counted32(mask ? mask + 32 * int64_t(step) : nullptr, past(32))) << 32;
+    if (mask) mask += 64 * int64_t(step);
   }
   __device__ __forceinline__ bool on() const { return on_bits & 1u; }
   __device__ __forceinline__ void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory"); }
@@ -589,25 +591,28 @@ __global__ void __launch_bounds__(kThreads<T, kVec, kC>)
   __shared__ int sh_used[32];
   grid_wait();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  int used = 0;
-  for (int i = threadIdx.x; i < a.B; i += block) used += ld(rows + i) > 0;
-  used = __reduce_add_sync(0xffffffffu, used);
-  if (lane == 0) sh_used[warp] = used;
-  __syncthreads();
-  used = 0;
-  for (int i = 0; i < warps; ++i) used += sh_used[i];
   extern __shared__ uint4 smem[];  // the stream's slots
-  const float g = ld(grad_loss);
   const int groups = 32 / lanes, l = lane & (lanes - 1);
   const int64_t r0 = int64_t(blockIdx.x) * a.chunk, r1 = r0 + a.chunk < a.N ? r0 + a.chunk : a.N;
   const Rows own = a.cu ? cta_rows(r0, r1, warp, warps, groups) : grid_rows(a, warp, warps, groups);
+  Stream<T, kVec, kC> x(a, own, l, lanes, nullptr, smem, smem);
+  const float g = ld(grad_loss);
+  int used = 1;  // segments with a counted row
+  if (a.B > 1) {
+    used = 0;
+    for (int i = threadIdx.x; i < a.B; i += block) used += ld(rows + i) > 0;
+    used = __reduce_add_sync(0xffffffffu, used);
+    if (lane == 0) sh_used[warp] = used;
+    __syncthreads();
+    used = 0;
+    for (int i = 0; i < warps; ++i) used += sh_used[i];
+  }
   int b = seg_of(a, own.first < a.N ? own.first : a.N - 1);
   int64_t seg_end = -1;  // from this row on the weights are another segment's
   float w[kC];
 #pragma unroll
   for (int j = 0; j < kC; ++j) w[j] = 0.f;
   const int64_t first = own.first + lane / lanes;
-  Stream<T, kVec, kC> x(a, own, l, lanes, nullptr, smem, smem);
   T *out = dx + first * a.E;
   const int64_t out_step = int64_t(own.step) * a.E;
   for (int64_t r = first; x.left > 0; r += own.step) {

@@ -3,15 +3,20 @@
 // the row's entries, the entries' logits kept.
 //
 // The tensor core truncates as it adds to its accumulator. Over a contraction of 2,048
-// that moved a logit of 12 by 2.6e-5, always towards zero, and the loss by 1e-5 of
-// itself, some ten times what fp32 FMAs lose. So the accumulator is emptied every
-// kPart elements of the contraction and the parts are added in fp32 registers: a part's
-// accumulator is smaller by the number of parts, and so is what truncation takes.
-// Sixteen warps hold a 128x256 tile as 64 sums a thread.
+// that moved a logit of 12 by 2.6e-5, always towards zero, and the losses by 2.7e-6 of
+// themselves (7.2e-6 at h = 6,144), three to five times what fp32 FMAs lose. So the
+// accumulator is emptied every kPart elements of the contraction and the parts are added
+// in fp32 registers: a part's accumulator is smaller by the number of parts, and so is
+// what truncation takes. Sixteen warps hold a 128x256 tile as 64 sums a thread. Losses
+// off by (h = 2,048) and time of 12,288 rows on the moe head: parts of 256 3.6e-7, 5.83
+// ms; 512 6.7e-7, 5.68; 1,024 1.3e-6, 5.35; one part 2.7e-6, 5.41 (fp32 FMAs 9.2e-7).
 //
 // A row's entries are sorted by id, and off[] counts them by tile, so a thread finds
 // those of its 64 columns while the tile's products run. Per tile 128 x 256 x h
-// multiply-adds against 128 x 256 exponentials: bound by the tensor cores from h = 512 on.
+// multiply-adds against 128 x 256 exponentials: bound by the tensor cores, and those by
+// the power cap: 12,288 rows, K = 1 4.66 ms, 1.64 PFLOP/s (of 1.89 in a burst, 1.69
+// sustained); K = 128 5.13 ms, the entries' columns taken out of two thirds of the
+// 16-column pieces. 388 rows 202 us, 24,576 rows of h = 1,024, V = 32,000 1.02 ms.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cudaTypedefs.h>

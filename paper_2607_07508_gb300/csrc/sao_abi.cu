@@ -496,6 +496,8 @@ sao_status sao_distill_loss_fwd(const void *H, const void *W, sao_dtype dt, cons
   if (N == 0) return SAO_OK;
   if (!H || !W || !top_ids || !top_logits || !loss || !lse || !lse_rest || !z_top)
     return fail(SAO_ERR_INVALID_ARG, "NULL array argument");
+  if (dt == SAO_BF16 && (!aligned16(H) || !aligned16(W)))
+    return fail(SAO_ERR_INVALID_ARG, "H and W of a bf16 head must be 16-byte aligned");
   SAO_TRY(check_tc_device(dt));
   Ws w;
   SAO_TRY(take_ws(ws, ws_bytes, distill_ws_bytes(N, h, V, K, dt), &w));
@@ -525,8 +527,8 @@ sao_status sao_distill_loss_bwd(const void *H, const void *W, sao_dtype dt, cons
   }
   if (!H || !top_ids || !top_logits || !lse || !lse_rest || !z_top || !grad_loss || !dH)
     return fail(SAO_ERR_INVALID_ARG, "NULL array argument");
-  if (dt == SAO_BF16 && (!aligned16(dH) || !aligned16(dW)))
-    return fail(SAO_ERR_INVALID_ARG, "dH and dW of a bf16 head must be 16-byte aligned");
+  if (dt == SAO_BF16 && (!aligned16(H) || !aligned16(W) || !aligned16(dH) || !aligned16(dW)))
+    return fail(SAO_ERR_INVALID_ARG, "H, W, dH and dW of a bf16 head must be 16-byte aligned");
   SAO_TRY(check_tc_device(dt));
   Ws w;
   SAO_TRY(take_ws(ws, ws_bytes, distill_ws_bytes(N, h, V, K, dt), &w));

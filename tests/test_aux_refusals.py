@@ -35,6 +35,8 @@ def test_distill_refusals(lib):
         assert _dfwd(lib, T=T) == INVALID and _dbwd(lib, T=T) == INVALID
     for null in ("H", "W", "ids", "a", "loss", "z", "ws"):
         assert _dfwd(lib, **{null: None}) == INVALID, null
+    assert _dfwd(lib, dt=BF16, H=18) == INVALID and _dfwd(lib, dt=BF16, W=24) == INVALID
+    assert "16-byte" in lib.sao_last_error_string().decode()
     assert _dfwd(lib, ws=128) == INVALID and _dfwd(lib, wsb=256) == WORKSPACE
     assert _dfwd(lib, N=0, H=None, loss=None, ws=None) == 0
     assert _dbwd(lib, dt=F32, dw_dt=BF16) == UNSUPPORTED and _dbwd(lib, dt=BF16, dw_dt=BF16, acc=1) == UNSUPPORTED

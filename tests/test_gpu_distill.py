@@ -1,8 +1,9 @@
 """Distillation from a teacher's top logits against fp64.
 
 Bounds, with u = 2^-24 and S the largest sum_k |H_tk W_vk| / T. A logit of a bf16
-head: products exact, sums of 256 elements truncated 16 times at 2u each, the
-parts added in fp32: (32 + h / 256) u S. Of an fp32 head (see
+head: products exact, sums of up to 512 elements truncated 32 times, each time by up to
+2u of a partial sum that is half of the whole on average, the parts added in fp32:
+(32 + h / 256) u S. Of an fp32 head (see
 test_gpu_logprobs_f32.py): (8 + h / 32) u S. Both get the exponentials' and
 merges' share, 16 u (1 + |lse|); the loss is a weighted mean of differences of
 two such values, and its teacher's terms add 16 u (1 + |la|). Gradients in the
