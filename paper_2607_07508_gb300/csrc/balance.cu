@@ -393,12 +393,84 @@ __device__ __forceinline__ void for_segments(const BalanceArgs &a, int c, F f) {
   }
 }
 
+// Where one cluster's forward writes its results; loss null: partials for the reduction.
+struct BalanceOut {
+  float *loss, *prob_sums;
+  int64_t *counts, *rows;
+};
+
+constexpr int kCluster = 8;
+__device__ __forceinline__ void cluster_barrier() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// The same shared variable in the CTA of cluster rank `rank`.
+template <class T>
+__device__ __forceinline__ T *peer_shared(T *p, unsigned rank) {
+  uint64_t out;
+  asm("mapa.u64 %0, %1, %2;" : "=l"(out) : "l"(reinterpret_cast<uint64_t>(p)), "r"(rank));
+  return reinterpret_cast<T *>(out);
+}
+
+// The end of a forward by one cluster (kCluster CTAs, the whole batch): each CTA has its sums
+// and counts of every column, and its rows; CTA r adds those of columns r, r + 8, ...
+__device__ __forceinline__ void cluster_finish(const BalanceArgs &a, const BalanceOut &o, float *sums, int *counts,
+                                               int n) {
+  __shared__ int my_rows;
+  __shared__ float my_term, warp_term[32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (threadIdx.x == 0) my_rows = n;
+  cluster_barrier();
+  const int nr = __reduce_add_sync(0xffffffffu, lane < kCluster ? *peer_shared(&my_rows, lane) : 0);
+  const float f = nr > 0 ? float(a.E) / (float(a.k) * float(nr)) / float(nr) : 0.f;
+  float term = 0.f;
+  for (int e = int(blockIdx.x) + kCluster * int(threadIdx.x); e < a.E; e += kCluster * int(blockDim.x)) {
+    float ps[kCluster];
+    int pc[kCluster];
+#pragma unroll
+    for (int p = 0; p < kCluster; ++p) {
+      ps[p] = *peer_shared(sums + e, p);
+      pc[p] = *peer_shared(counts + e, p);
+    }
+    float v = 0.f;
+    int64_t c = 0;
+#pragma unroll
+    for (int p = 0; p < kCluster; ++p) {
+      v += ps[p];
+      c += pc[p];
+    }
+    o.prob_sums[e] = v;
+    o.counts[e] = c;
+    term += v * (float(c) * f);
+  }
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) term += __shfl_xor_sync(0xffffffffu, term, d);
+  if (lane == 0) warp_term[warp] = term;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    term = 0.f;
+    for (int w = 0; w < int(blockDim.x >> 5); ++w) term += warp_term[w];
+    my_term = term;
+  }
+  cluster_barrier();
+  if (blockIdx.x == 0 && warp == 0) {
+    term = lane < kCluster ? *peer_shared(&my_term, lane) : 0.f;
+#pragma unroll
+    for (int d = kCluster / 2; d > 0; d >>= 1) term += __shfl_xor_sync(0xffffffffu, term, d);
+    if (lane == 0) {
+      o.loss[0] = term;
+      o.rows[0] = nr;
+    }
+  }
+  cluster_barrier();  // no CTA leaves while its shared memory may still be read
+}
+
 // Each group of `lanes` lanes takes a row at a time, the next one's logits in flight,
 // and keeps the sums of its columns in registers. One pass over the logits: bound by
 // reading them.
 template <class T, int kVec, int kC, bool kSigmoid>
 __global__ void __launch_bounds__(kThreads<T, kVec, kC>)
-    balance_partial_kernel(const BalanceArgs a, int lanes, float *psum, int *pcount, int *prows, unsigned int *ticket) {
+    balance_partial_kernel(const BalanceArgs a, int lanes, const BalanceOut out, float *psum, int *pcount, int *prows,
+                           unsigned int *ticket) {
   extern __shared__ uint4 smem[];  // the stream's slots, ids', sums [warps][E], counts [E]
   __shared__ int n_rows[32];
   const int block = blockDim.x, warps = block >> 5;
@@ -462,14 +534,21 @@ __global__ void __launch_bounds__(kThreads<T, kVec, kC>)
       float v = 0.f;
 #pragma unroll 4
       for (int w = 0; w < warps; ++w) v += sums[w * a.E + e];
-      psum[slot * a.E + e] = v;
-      pcount[slot * a.E + e] = counts[e];
+      if (out.loss) {
+        sums[e] = v;
+      } else {
+        psum[slot * a.E + e] = v;
+        pcount[slot * a.E + e] = counts[e];
+      }
     }
-    if (threadIdx.x == 0) {
-      int t = 0;
+    int t = 0;
+    if (threadIdx.x == 0)
       for (int w = 0; w < warps; ++w) t += n_rows[w];
-      prows[slot] = t;
+    if (out.loss) {
+      cluster_finish(a, out, sums, counts, t);
+      return;
     }
+    if (threadIdx.x == 0) prows[slot] = t;
     __syncthreads();
   });
 }
@@ -728,6 +807,12 @@ int block_of(int most, int chunk, int lanes, bool segments) {
 }
 constexpr size_t kPlainSmem = 40u << 10;  // dynamic shared memory that any kernel may have
 
+// Small batches by one cluster, in one launch (another one is 2 us of the host's time, and
+// with the reduction's own latency 2 to 4 of the GPU's). Forward on the GPU alone, us,
+// cluster / two launches: 256 x 60 4.9 / 8.6, 1,024 x 128 8.4 / 8.8, 4,096 x 8 8.3 / 6.4,
+// 4,096 x 60 10.7 / 8.0; a forward and backward of 2,304 x 8, bound by the host, 14.3 / 16.6.
+bool one_cluster(int64_t N, int32_t E) { return N <= 4096 && N * E <= (1 << 17); }
+
 // Lets the kernel have an SM's shared memory (once per device).
 template <auto kKernel>
 sao_status allow_smem() {
@@ -775,20 +860,44 @@ sao_status balance_fwd_launch(const void *x, sao_dtype dt, const int32_t *ids, c
   const Scratch w = take(c, N, E, a.B);
   if (!c.ok()) return fail(SAO_ERR_WORKSPACE, "workspace too small for the balance loss");
   const Layout lay = layout(x, x, dt, E);
-  int slot = launch_begin("balance_partial", s);
+  const bool one = cu == nullptr && one_cluster(N, E);
+  const BalanceOut out = one ? BalanceOut{loss, prob_sums, counts, rows} : BalanceOut{};
+  int slot = launch_begin(one ? "balance_cluster" : "balance_partial", s);
   sao_status st = SAO_OK;
   auto partial = [&](auto t, auto vec, auto columns, auto sig) {
     using T = decltype(t);
     auto kern = balance_partial_kernel<T, vec.value, columns.value, sig.value>;
-    const int block = block_of(kThreads<T, vec.value, columns.value>, a.chunk, lay.lanes, a.cu != nullptr);
+    const int block =
+        block_of(kThreads<T, vec.value, columns.value>, one ? int((N + kCluster - 1) / kCluster) : a.chunk, lay.lanes,
+                 a.cu != nullptr);
     const size_t smem = size_t(block) * (kRing<T, vec.value, columns.value> + kIdRing<T, vec.value, columns.value>) +
                         size_t(E) * (block / 32 + 1) * sizeof(float);
     if (smem > kPlainSmem) st = allow_smem<balance_partial_kernel<T, vec.value, columns.value, sig.value>>();
-    if (st == SAO_OK) pdl(kern, unsigned(a.chunks), block, smem, s)(a, lay.lanes, w.psum, w.pcount, w.prows, w.ticket);
+    if (st != SAO_OK) return;
+    if (one) {
+      cudaLaunchAttribute at[2];
+      at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+      at[0].val.programmaticStreamSerializationAllowed = 1;
+      at[1].id = cudaLaunchAttributeClusterDimension;
+      at[1].val.clusterDim.x = kCluster;
+      at[1].val.clusterDim.y = 1;
+      at[1].val.clusterDim.z = 1;
+      cudaLaunchConfig_t cfg = {};
+      cfg.gridDim = dim3(kCluster);
+      cfg.blockDim = dim3(unsigned(block));
+      cfg.dynamicSmemBytes = smem;
+      cfg.stream = s;
+      cfg.attrs = at;
+      cfg.numAttrs = 2;
+      cudaLaunchKernelEx(&cfg, kern, a, lay.lanes, out, w.psum, w.pcount, w.prows, w.ticket);
+    } else {
+      pdl(kern, unsigned(a.chunks), block, smem, s)(a, lay.lanes, out, w.psum, w.pcount, w.prows, w.ticket);
+    }
   };
   dt == SAO_BF16 ? with_layout<__nv_bfloat16>(lay, score, partial) : with_layout<float>(lay, score, partial);
   SAO_TRY(st);
   SAO_TRY(launch_end(slot, s));
+  if (one) return SAO_OK;
   // a batch's partials, up to 152 in few CTAs: 16 warps to each; many trajectories: 8
   const unsigned grid = unsigned(a.B) * unsigned((E + 31) / 32);
   slot = launch_begin("balance_reduce", s);

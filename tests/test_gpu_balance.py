@@ -68,7 +68,7 @@ def close(got, ref, grad, bf16):
     assert (np.abs(got["dlogits"] - d) <= tol + (2.0 ** -8 * np.abs(d) if bf16 else 0) + 1e-37).all()
 
 
-SIZES = [(1, 1, 1), (1, 8, 2), (2, 7, 7), (31, 33, 3), (32, 64, 8), (257, 100, 4), (1000, 128, 8), (700, 160, 6),
+SIZES = [(4096, 32, 2), (4097, 32, 2), (1024, 128, 4), (1025, 128, 4), (1, 1, 1), (1, 8, 2), (2, 7, 7), (31, 33, 3), (32, 64, 8), (257, 100, 4), (1000, 128, 8), (700, 160, 6),
          (65, 256, 8), (40, 1000, 10), (33, 1024, 1), (5000, 8, 2), (20011, 16, 4)]
 
 
