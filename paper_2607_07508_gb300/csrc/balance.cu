@@ -29,10 +29,12 @@ namespace sao {
 namespace {
 
 // A lane takes kC columns of a row, in loads of kVec columns (16 bytes, or one column).
-// Rows on their way lie in shared memory (asynchronous copies of 4 bytes or more), for
-// single bf16 columns in registers.
-template <class T, int kVec>
-constexpr bool kAsync = kVec * sizeof(T) >= 4;
+// Rows on their way lie in shared memory (asynchronous copies), for single columns in registers
+// (fp32 98,301 x 63 in 96 trajectories, forward / backward: 18 / 16 us, by copies of 4 bytes
+// 20 / 25; 200,000 x 21 15 / 14, 19 / 33. Copying a warp's rows as one span of 16-byte pieces
+// and picking the columns out of it took 20 / 22 and 18 / 20.)
+template <int kVec>
+constexpr bool kAsync = kVec > 1;
 // Threads of a CTA, one to an SM: as many as the registers for the columns' scores and
 // sums, and for the words that stay in them, allow. One CTA, not several: its partials are a
 // launch's whole scratch, and the reduction reads them all.
@@ -41,18 +43,18 @@ constexpr int threads_of(bool async, int columns) {
   return n > 1024 ? 1024 : n;
 }
 template <class T, int kVec, int kC>
-constexpr int kThreads = threads_of(kAsync<T, kVec>, kC);
+constexpr int kThreads = threads_of(kAsync<kVec>, kC);
 // Rows that a thread has on their way.
 constexpr int depth_of(bool async, int size, int columns) {
   const int n = (112 << 10) / (threads_of(async, columns) * columns * size);
   return !async ? 2 : n < 2 ? 2 : n > 6 ? 6 : n;
 }
 template <class T, int kVec, int kC>
-constexpr int kDepthOf = depth_of(kAsync<T, kVec>, int(sizeof(T)), kC);
+constexpr int kDepthOf = depth_of(kAsync<kVec>, int(sizeof(T)), kC);
 // Bytes of a thread's slots, and of its expert ids' (kIds a row).
 constexpr int kIds = 2;
 template <class T, int kVec, int kC>
-constexpr int kRing = kAsync<T, kVec> ? kC * int(sizeof(T)) * kDepthOf<T, kVec, kC> : 0;
+constexpr int kRing = kAsync<kVec> ? kC * int(sizeof(T)) * kDepthOf<T, kVec, kC> : 0;
 template <class T, int kVec, int kC>
 constexpr int kIdRing = kIds * 4 * kDepthOf<T, kVec, kC>;
 
@@ -163,7 +165,7 @@ __device__ __forceinline__ void copy_async(uint32_t dst, const void *src) {
 // kernels waited for memory half of their time (2^20 x 160 bf16 forward 93-128 us).
 template <class T, int kVec, int kC>
 struct Stream {
-  static constexpr bool kSlots = kAsync<T, kVec>;
+  static constexpr bool kSlots = kAsync<kVec>;
   static constexpr int kDepth = kDepthOf<T, kVec, kC>, kLoads = kC / kVec;
   static constexpr int kBytes = kVec * int(sizeof(T));
   __device__ __forceinline__ uint32_t pitch() const { return blockDim.x * uint32_t(kBytes); }  // from a load's slots to the next one's
@@ -211,11 +213,12 @@ struct Stream {
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
     if constexpr (!kSlots) {
-      constexpr uint32_t none = 0xff80u;  // -inf
+      using Word = std::conditional_t<sizeof(T) == 4, uint32_t, uint16_t>;
+      constexpr uint32_t none = sizeof(T) == 4 ? 0xff800000u : 0xff80u;  // -inf
 #pragma unroll
       for (int v = 0; v < kLoads; ++v) {
         uint32_t w = none;
-        if (live && v < loads) w = ld(reinterpret_cast<const uint16_t *>(src) + v * lanes);
+        if (live && v < loads) w = ld(reinterpret_cast<const Word *>(src) + v * lanes);
         reg[kDepth - 1].raw[v] = w;
       }
     }
@@ -268,13 +271,10 @@ struct Stream {
       const uint32_t at = slots + uint32_t(cur * kLoads) * pitch();
 #pragma unroll
       for (int v = 0; v < kLoads; ++v) {
-        if constexpr (kBytes == 16)
-          asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                       : "=r"(x.raw[4 * v]), "=r"(x.raw[4 * v + 1]), "=r"(x.raw[4 * v + 2]), "=r"(x.raw[4 * v + 3])
-                       : "r"(at + v * pitch())
-                       : "memory");
-        else
-          asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x.raw[v]) : "r"(at + v * pitch()) : "memory");
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(x.raw[4 * v]), "=r"(x.raw[4 * v + 1]), "=r"(x.raw[4 * v + 2]), "=r"(x.raw[4 * v + 3])
+                     : "r"(at + v * pitch())
+                     : "memory");
       }
       return x;
     } else {
@@ -464,9 +464,10 @@ __device__ __forceinline__ void cluster_finish(const BalanceArgs &a, const Balan
   cluster_barrier();  // no CTA leaves while its shared memory may still be read
 }
 
-// Each group of `lanes` lanes takes a row at a time, the next one's logits in flight,
-// and keeps the sums of its columns in registers. One pass over the logits: bound by
-// reading them.
+// Each group of `lanes` lanes takes a row at a time, the next ones' logits in flight, and
+// keeps the sums of its columns in registers. One pass over the logits. 2^20 x 160 bf16:
+// (a quarter masked) 94 us, 3.0 TB/s, bound by instructions (2.9 a cycle and SM);
+// 2^20 x 128 fp32: 92 us, 5.8 TB/s.
 template <class T, int kVec, int kC, bool kSigmoid>
 __global__ void __launch_bounds__(kThreads<T, kVec, kC>)
     balance_partial_kernel(const BalanceArgs a, int lanes, const BalanceOut out, float *psum, int *pcount, int *prows,
@@ -554,8 +555,8 @@ __global__ void __launch_bounds__(kThreads<T, kVec, kC>)
 }
 
 // CTA (b, 32 columns): adds the segment's partials, kSlices warps side by side; the
-// last CTA adds the products of all of them. Bound by the latency of its few rounds of
-// loads. (The sums are of positive numbers, in a fixed order, in fp32; fp64, on which
+// last CTA adds the products of all of them. Bound by latency: a batch's 152 partials are
+// asked for at once (in three rounds a forward of 65,536 x 128 was 1 us longer). (The sums are of positive numbers, in a fixed order, in fp32; fp64, on which
 // GB300 has few units, took longer than the loads.)
 template <int kSlices>
 __global__ void __launch_bounds__(32 * kSlices)
@@ -574,7 +575,7 @@ __global__ void __launch_bounds__(32 * kSlices)
   long long n = 0, nr = 0;
   if (r1 > r0) {
     const int c0 = int(r0 / a.chunk), c1 = int((r1 - 1) / a.chunk);
-    constexpr int kU = 4;  // partials in flight
+    constexpr int kU = 10;  // partials in flight
     for (int c = c0 + slice; c <= c1; c += kU * kSlices) {
       float ps[kU];
       int pn[kU], pr[kU];
@@ -660,8 +661,9 @@ __global__ void __launch_bounds__(32 * kSlices)
 }
 
 // A group of `lanes` lanes per row, as in the forward; the segment's weights of its columns
-// stay in registers until the segment ends. One pass: bound by reading the logits and
-// writing their gradient.
+// stay in registers until the segment ends. One pass, bound by reading the logits and
+// writing their gradient: 2^20 x 160 bf16 108-115 us, 5.1-5.4 TB/s; 2^20 x 128 fp32 174 us,
+// 6.2 TB/s.
 template <class T, int kVec, int kC, bool kSigmoid>
 __global__ void __launch_bounds__(kThreads<T, kVec, kC>)
     balance_grad_kernel(const BalanceArgs a, int lanes, const int64_t *counts, const int64_t *rows,
@@ -742,12 +744,12 @@ struct Layout {
 // Vector loads where every row starts on 16 bytes. Of the layouts the one with the
 // fewest instructions: about 5 for each of a lane's columns, 130 for all else that a
 // row takes, times the lanes; of 8 to 24 columns (32 or 40, with fewer warps to hide latencies,
-// were no faster for 128 to 256 experts) unless only 32 fit, and for single bf16 columns,
-// whose words stay in registers, of 8 (98,301 x 63: 44 us against 51 with 16).
+// were no faster for 128 to 256 experts) unless only 32 fit, and for single columns,
+// whose words stay in registers, of 8 (98,301 x 63 bf16: 44 us against 51 with 16).
 Layout layout(const void *x, const void *dx, sao_dtype dt, int E) {
   const int size = dt == SAO_BF16 ? 2 : 4, per = 16 / size;
   Layout best{0, 0, E % per == 0 && aligned16(x) && aligned16(dx)};
-  const int vec = best.vec ? per : 1, most = vec * size >= 4 ? 24 : 8;
+  const int vec = best.vec ? per : 1, most = best.vec ? 24 : 8;
   int least = 0;
   for (int c = 8; c <= 32; c += 8) {
     const int loads = c / vec, units = E / vec;

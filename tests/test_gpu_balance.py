@@ -106,6 +106,33 @@ def test_alignment(dtype, offset):
     close(run(x, ids, "softmax", m, offset=offset), O.balance_loss(x, ids, "softmax", m), 1.0, dtype == "bf16")
 
 
+@pytest.mark.parametrize("at_x,at_dx", [(8, 8), (9, 9), (9, 8), (8, 11)])
+@pytest.mark.parametrize("N,E,segments", [(1, 1, False), (1, 2, False), (3, 63, False), (301, 60, False), (301, 63, True),
+                                          (65, 1, False), (6001, 21, False), (5003, 257, True), (5003, 511, False),
+                                          (40, 1023, True), (40, 1024, False)])
+def test_bf16_rows_that_share_words_with_their_neighbours(N, E, segments, at_x, at_dx):
+    """Rows that start and end inside 4-byte words, the logits inside a buffer of NaN, their gradient inside one that
+    keeps its other elements."""
+    lens = [N // 3, 0, N - N // 3] if segments else None
+    x, ids, m, cu = _case(N, E, min(E, 3), "bf16", seed=N + E, lens=lens, mask=N > 1)
+    flat = torch.full((N * E + 32,), float("nan"), dtype=torch.bfloat16, device="cuda")
+    out = torch.full((N * E + 32,), 7.0, dtype=torch.bfloat16, device="cuda")
+    xd, dx = flat[at_x:at_x + N * E].view(N, E), out[at_dx:at_dx + N * E].view(N, E)
+    xd.copy_(x)
+    B = len(lens) if segments else 1
+    idd, md = torch.from_numpy(ids).cuda(), None if m is None else torch.from_numpy(m).cuda()
+    cud = None if cu is None else torch.from_numpy(cu).cuda()
+    loss, sums, one = torch.empty(1, device="cuda"), torch.empty(B, E, device="cuda"), torch.ones(1, device="cuda")
+    counts, rows = torch.empty(B, E, dtype=torch.int64, device="cuda"), torch.empty(B, dtype=torch.int64, device="cuda")
+    ws = sao.balance_workspace(N, E, B)
+    sao.sao_balance_loss_fwd(xd, idd, 0, loss, counts, sums, rows, ws, row_mask=md, cu_seqlens=cud)
+    sao.sao_balance_loss_bwd(xd, ids.shape[1], 0, counts, rows, one, dx, ws, row_mask=md, cu_seqlens=cud)
+    got = {"loss": loss.item(), "counts": counts.cpu().numpy(), "sums": sums.double().cpu().numpy(),
+           "rows": rows.cpu().numpy(), "dlogits": dx.double().cpu().numpy()}
+    close(got, O.balance_loss(x, ids, "softmax", m, cu), 1.0, True)
+    assert (out[:at_dx] == 7).all() and (out[at_dx + N * E:] == 7).all()
+
+
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 @pytest.mark.parametrize("E", [12, 128])
 def test_masked_rows_dropped_choices_and_extreme_logits(E, score):
