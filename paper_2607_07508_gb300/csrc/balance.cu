@@ -181,6 +181,8 @@ struct Stream {
   Row<T, kVec, kC> reg[kSlots ? 1 : kDepth];
 
   // Bit i of the result: this group's row i steps on is counted, `from` the warp's first row.
+  // (Several groups' bytes asked for before the first is waited for saved 0.3 us of a short
+  // launch, but took registers: 2^20 x 160 bf16 backward 113 -> 127 us.)
   __device__ __forceinline__ uint32_t counted32(const uint8_t *from, int rows) const {
     const int groups = 32 / lanes, lane = threadIdx.x & 31, mine = lane / lanes;
     uint32_t bits = 0;
@@ -555,19 +557,21 @@ __global__ void __launch_bounds__(kThreads<T, kVec, kC>)
 }
 
 // CTA (b, 32 columns): adds the segment's partials, kSlices warps side by side; the
-// last CTA adds the products of all of them. Bound by latency: a batch's 152 partials are
+// CTAs of a batch of up to 256 experts are one cluster, whose first CTA adds their products
+// (2 us less than by the ticket); else the last CTA adds those of all. Bound by latency: a batch's 152 partials are
 // asked for at once (in three rounds a forward of 65,536 x 128 was 1 us longer). (The sums are of positive numbers, in a fixed order, in fp32; fp64, on which
 // GB300 has few units, took longer than the loads.)
 template <int kSlices>
 __global__ void __launch_bounds__(32 * kSlices)
-    balance_reduce_kernel(const BalanceArgs a, const float *psum, const int *pcount, const int *prows, float *loss,
-                          int64_t *counts, float *prob_sums, int64_t *rows, float *terms, unsigned int *ticket) {
+    balance_reduce_kernel(const BalanceArgs a, int cols, bool cluster, const float *psum, const int *pcount,
+                          const int *prows, float *loss, int64_t *counts, float *prob_sums, int64_t *rows, float *terms,
+                          unsigned int *ticket) {
   __shared__ float sh_sum[kSlices][32], sh_term[kSlices];
   __shared__ long long sh_count[kSlices][32], sh_rows[kSlices];
   __shared__ int sh_used[kSlices];
   __shared__ bool last;
+  __shared__ float my_term;
   grid_wait();
-  const int cols = (a.E + 31) / 32;
   const int b = blockIdx.x / cols, g = blockIdx.x % cols;
   const int slice = threadIdx.x >> 5, lane = threadIdx.x & 31, e = g * 32 + lane;
   const int64_t r0 = seg_at(a, b), r1 = seg_at(a, b + 1);
@@ -599,7 +603,6 @@ __global__ void __launch_bounds__(32 * kSlices)
   sh_count[slice][lane] = n;
   if (lane == 0) sh_rows[slice] = nr;
   __syncthreads();
-  const bool alone = gridDim.x == 1;
   if (slice == 0) {
     s = 0.f;
     n = nr = 0;
@@ -624,8 +627,8 @@ __global__ void __launch_bounds__(32 * kSlices)
         const int64_t u = ld(a.cu + b), v = ld(a.cu + b + 1);
         if (u > v || (b == 0 && u != 0) || (b == a.B - 1 && v != a.N)) raise_device_error(a.err, SAO_DEVERR_CU_SEQLENS);
       }
-      if (alone) {
-        loss[0] = term;
+      if (cluster) {
+        my_term = term;
       } else {
         terms[blockIdx.x] = term;
         __threadfence();
@@ -633,7 +636,17 @@ __global__ void __launch_bounds__(32 * kSlices)
       }
     }
   }
-  if (alone) return;
+  if (cluster) {
+    cluster_barrier();
+    if (blockIdx.x == 0 && slice == 0) {
+      float t = lane < cols ? *peer_shared(&my_term, lane) : 0.f;
+#pragma unroll
+      for (int o = kCluster / 2; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+      if (lane == 0) loss[0] = t;
+    }
+    cluster_barrier();  // no CTA leaves while its shared memory may still be read
+    return;
+  }
   __syncthreads();
   if (!last) return;
   __threadfence();
@@ -827,6 +840,26 @@ sao_status allow_smem() {
   return SAO_OK;
 }
 
+// A grid of one cluster, as a programmatic dependent launch.
+template <class K, class... A>
+void launch_cluster(K kern, int ctas, int block, size_t smem, cudaStream_t s, A... args) {
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = unsigned(ctas);
+  at[1].val.clusterDim.y = 1;
+  at[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(unsigned(ctas));
+  cfg.blockDim = dim3(unsigned(block));
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cfg.attrs = at;
+  cfg.numAttrs = 2;
+  cudaLaunchKernelEx(&cfg, kern, args...);
+}
+
 struct Scratch {
   float *psum;
   int *pcount, *prows;
@@ -877,21 +910,7 @@ sao_status balance_fwd_launch(const void *x, sao_dtype dt, const int32_t *ids, c
     if (smem > kPlainSmem) st = allow_smem<balance_partial_kernel<T, vec.value, columns.value, sig.value>>();
     if (st != SAO_OK) return;
     if (one) {
-      cudaLaunchAttribute at[2];
-      at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-      at[0].val.programmaticStreamSerializationAllowed = 1;
-      at[1].id = cudaLaunchAttributeClusterDimension;
-      at[1].val.clusterDim.x = kCluster;
-      at[1].val.clusterDim.y = 1;
-      at[1].val.clusterDim.z = 1;
-      cudaLaunchConfig_t cfg = {};
-      cfg.gridDim = dim3(kCluster);
-      cfg.blockDim = dim3(unsigned(block));
-      cfg.dynamicSmemBytes = smem;
-      cfg.stream = s;
-      cfg.attrs = at;
-      cfg.numAttrs = 2;
-      cudaLaunchKernelEx(&cfg, kern, a, lay.lanes, out, w.psum, w.pcount, w.prows, w.ticket);
+      launch_cluster(kern, kCluster, block, smem, s, a, lay.lanes, out, w.psum, w.pcount, w.prows, w.ticket);
     } else {
       pdl(kern, unsigned(a.chunks), block, smem, s)(a, lay.lanes, out, w.psum, w.pcount, w.prows, w.ticket);
     }
@@ -901,11 +920,19 @@ sao_status balance_fwd_launch(const void *x, sao_dtype dt, const int32_t *ids, c
   SAO_TRY(launch_end(slot, s));
   if (one) return SAO_OK;
   // a batch's partials, up to 152 in few CTAs: 16 warps to each; many trajectories: 8
-  const unsigned grid = unsigned(a.B) * unsigned((E + 31) / 32);
+  int cols = (E + 31) / 32;
+  const bool cluster = cu == nullptr && cols <= kCluster;
+  if (cluster)  // a power of two of CTAs: 1, 2, 4 or 8
+    while (cols & (cols - 1)) ++cols;
+  const unsigned grid = unsigned(a.B) * unsigned(cols);
   slot = launch_begin("balance_reduce", s);
   auto reduce = grid <= 152 ? balance_reduce_kernel<16> : balance_reduce_kernel<8>;
-  pdl(reduce, grid, grid <= 152 ? 512 : 256, 0, s)(a, w.psum, w.pcount, w.prows, loss, counts, prob_sums, rows,
-                                                    w.terms, w.ticket);
+  if (cluster)
+    launch_cluster(reduce, cols, 512, 0, s, a, cols, true, w.psum, w.pcount, w.prows, loss, counts, prob_sums, rows,
+                   w.terms, w.ticket);
+  else
+    pdl(reduce, grid, grid <= 152 ? 512 : 256, 0, s)(a, cols, false, w.psum, w.pcount, w.prows, loss, counts, prob_sums,
+                                                      rows, w.terms, w.ticket);
   return launch_end(slot, s);
 }
 
