@@ -486,7 +486,8 @@ SAO_API sao_status sao_distill_loss_fwd(const void *H, const void *W, sao_dtype 
  *                         SAO_BF16, overwritten only (a sum over calls needs fp32)
  * A bf16 head's dH and dW are 16-byte aligned. Its dZ is rounded to bf16 once
  * before the two products (as in sao_token_logprobs_bwd): 2^-9 of each of its
- * elements, 2^-17 up to 64 rows, not at all for one row.
+ * elements, 2^-17 up to 64 rows, not at all for one row of
+ * h <= 6,144 or two of h <= 2,048.
  */
 SAO_API sao_status sao_distill_loss_bwd(const void *H, const void *W, sao_dtype dt, const int32_t *top_ids,
                                         const void *top_logits, sao_dtype top_dt, const float *teacher_lse,

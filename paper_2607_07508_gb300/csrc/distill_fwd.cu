@@ -8,8 +8,9 @@
 // accumulator is emptied every kPart elements of the contraction and the parts are added
 // in fp32 registers: a part's accumulator is smaller by the number of parts, and so is
 // what truncation takes. Sixteen warps hold a 128x256 tile as 64 sums a thread. Losses
-// off by (h = 2,048) and time of 12,288 rows on the moe head: parts of 256 3.6e-7, 5.83
-// ms; 512 6.7e-7, 5.68; 1,024 1.3e-6, 5.35; one part 2.7e-6, 5.41 (fp32 FMAs 9.2e-7).
+// off by (h = 2,048) and time of 12,288 rows on the moe head, with warps that still polled:
+// parts of 256 3.6e-7, 5.83 ms; 512 6.7e-7, 5.68; 1,024 1.3e-6, 5.35; one part 2.7e-6, 5.41
+// (fp32 FMAs 9.2e-7).
 //
 // A row's entries are sorted by id, and off[] counts them by tile, so a thread finds
 // those of its 64 columns while the tile's products run. Per tile 128 x 256 x h

@@ -10,7 +10,8 @@
 // 256 threads holds kNV vectors of 8 columns of the rows, and of H; the kR x kN dot products are
 // added over the CTA (a reduce-scatter in each warp, then 8 partials each through shared
 // memory), and one thread per product finishes it. All sums in fp32, dZ in fp32: the
-// outputs are rounded once.
+// outputs are rounded once. One row of the moe head, V = 151,936, h = 2,048: forward 104 us
+// (622 MB, 6.0 TB/s), backward 209 us (1.24 GB, 5.9 TB/s), of 6.8 TB/s for a copy.
 #include <cuda_bf16.h>
 #include <math.h>
 #include <stdint.h>

@@ -30,8 +30,8 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 // A try suspends its warp for up to 4 us: at the default limit warps that wait for a long
-// product polled a billion times a millisecond, and under the power cap the tensor cores
-// paid for it (16 waiting warps a CTA, 12,288 x 151,936 x 2,048: 5.08 -> 4.66 ms).
+// product executed half a billion instructions a millisecond, and under the power cap the
+// tensor cores paid for them (16 waiting warps a CTA, 12,288 x 151,936 x 2,048: 5.08 -> 4.66 ms).
 __device__ __forceinline__ uint32_t mbar_try_wait(uint32_t bar, uint32_t parity) {
   uint32_t ok;
   asm volatile(
