@@ -487,7 +487,9 @@ SAO_API sao_status sao_distill_loss_fwd(const void *H, const void *W, sao_dtype 
  * A bf16 head's dH and dW are 16-byte aligned. Its dZ is rounded to bf16 once
  * before the two products (as in sao_token_logprobs_bwd): 2^-9 of each of its
  * elements, 2^-17 up to 64 rows, not at all for one row of
- * h <= 6,144 or two of h <= 2,048.
+ * h <= 6,144 or two of h <= 2,048. Few rows (those, and of an fp32 head up to
+ * eight of h <= 1,024, four of h <= 2,048, one of h <= 4,096) read W once in each
+ * direction.
  */
 SAO_API sao_status sao_distill_loss_bwd(const void *H, const void *W, sao_dtype dt, const int32_t *top_ids,
                                         const void *top_logits, sao_dtype top_dt, const float *teacher_lse,

@@ -426,7 +426,7 @@ size_t distill_ws_bytes(int64_t N, int32_t h, int32_t V, int32_t K, sao_dtype dt
   Carver f(nullptr, ~size_t(0)), b(nullptr, ~size_t(0));
   take_fwd(f, N, V, K);
   take_bwd(b, N, K);
-  const bool rows = dt == SAO_BF16 && gemv_takes(N, h);
+  const bool rows = gemv_takes(N, h, dt);
   const size_t head_f = rows             ? gemv_fwd_bytes(N, V)
                         : dt == SAO_BF16 ? tc_distill_fwd_bytes(N, h, V)
                                          : f32_ws_bytes(N, h, V);
@@ -453,7 +453,7 @@ sao_status distill_fwd_launch(const void *H, const void *W, sao_dtype dt, const 
   SAO_TRY(launch_end(slot, s));
   const TopRef top{w.sid, w.off, w.z, K, tiles, 1.f / temperature, w.range};
   const TopFinish f{a, adt, teacher_lse, w.slot, w.entries, row_mask, loss, lse, lse_rest, z_top, V};
-  if (dt == SAO_BF16 && gemv_takes(N, h)) return gemv_distill_fwd(H, W, row_mask, N, h, V, top, f, c, s);
+  if (gemv_takes(N, h, dt)) return gemv_distill_fwd(H, W, dt, row_mask, N, h, V, top, f, c, s);
   if (dt == SAO_BF16) return tc_distill_fwd(H, W, row_mask, N, h, V, top, f, err, c, s);
   return f32_distill_fwd(static_cast<const float *>(H), static_cast<const float *>(W), row_mask, N, h, V, top, f, err,
                          c, s);
@@ -474,8 +474,8 @@ sao_status distill_bwd_launch(const void *H, const void *W, sao_dtype dt, const 
       ids, a, adt, teacher_lse, lse, lse_rest, z_top, grad, N, K, inv_t, w.mask, w.g, w.rest, w.dz_top, w.range);
   SAO_TRY(launch_end(slot, s));
   const TopGrad t{w.mask, w.g, w.rest, w.dz_top, ids, K, inv_t, w.range};
-  if (dt == SAO_BF16 && gemv_takes(N, h))
-    return gemv_distill_bwd(H, W, t, N, h, V, dH, dW, dw_dt, accumulate, c, s);
+  if (gemv_takes(N, h, dt))
+    return gemv_distill_bwd(H, W, dt, t, N, h, V, dH, dW, dw_dt, accumulate, c, s);
   if (dt == SAO_BF16) return tc_distill_bwd(H, W, t, N, h, V, dH, dW, dw_dt, accumulate, err, c, s);
   return f32_distill_bwd(static_cast<const float *>(H), static_cast<const float *>(W), t, N, h, V,
                          static_cast<float *>(dH), static_cast<float *>(dW), accumulate, err, c, s);

@@ -93,14 +93,14 @@ sao_status f32_distill_fwd(const float *H, const float *W, const uint8_t *row_ma
 sao_status f32_distill_bwd(const float *H, const float *W, const TopGrad &t, int64_t N, int32_t h, int32_t V,
                            float *dH, float *dW, int accumulate, unsigned int *err, Carver &c, cudaStream_t s);
 
-// distill_rows.cu: one or two rows of a bf16 head, W read once by each direction.
-bool gemv_takes(int64_t N, int32_t h);
+// distill_rows.cu: a few rows on the fp32 units, W read once by each direction.
+bool gemv_takes(int64_t N, int32_t h, sao_dtype dt);
 size_t gemv_fwd_bytes(int64_t N, int32_t V);
 size_t gemv_bwd_bytes(int64_t N, int32_t h, int32_t V);
-sao_status gemv_distill_fwd(const void *H, const void *W, const uint8_t *row_mask, int64_t N, int32_t h, int32_t V,
-                            const TopRef &top, const TopFinish &f, Carver &c, cudaStream_t s);
-sao_status gemv_distill_bwd(const void *H, const void *W, const TopGrad &t, int64_t N, int32_t h, int32_t V, void *dH,
-                            void *dW, sao_dtype dw_dt, int accumulate, Carver &c, cudaStream_t s);
+sao_status gemv_distill_fwd(const void *H, const void *W, sao_dtype dt, const uint8_t *row_mask, int64_t N, int32_t h,
+                            int32_t V, const TopRef &top, const TopFinish &f, Carver &c, cudaStream_t s);
+sao_status gemv_distill_bwd(const void *H, const void *W, sao_dtype dt, const TopGrad &t, int64_t N, int32_t h,
+                            int32_t V, void *dH, void *dW, sao_dtype dw_dt, int accumulate, Carver &c, cudaStream_t s);
 
 // distill.cu, called by the C entry points
 size_t distill_ws_bytes(int64_t N, int32_t h, int32_t V, int32_t K, sao_dtype dt);

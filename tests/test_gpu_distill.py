@@ -174,6 +174,58 @@ def test_few_rows(N, h, V, K):
             assert np.linalg.norm(got["dW"] - prev.double().numpy() - ref["dW"]) <= 2.0 ** -8 * np.linalg.norm(ref["dW"])
 
 
+@pytest.mark.parametrize("N,h,V,K", [(1, 1, 9, 4), (1, 256, 4096, 8), (1, 515, 3001, 20), (1, 1024, 5003, 33), (1, 1025, 700, 5),
+                                     (1, 2048, 900, 7), (1, 2052, 900, 7), (1, 4096, 313, 64), (1, 4095, 313, 64),
+                                     (1, 4100, 300, 12), (2, 96, 2500, 300), (3, 1024, 20000, 1024), (4, 1023, 700, 11),
+                                     (4, 2047, 300, 9), (4, 2048, 500, 50), (5, 2048, 300, 9), (5, 40, 40000, 100),
+                                     (7, 515, 1000, 64), (8, 1024, 2000, 20), (8, 1022, 311, 3), (9, 1024, 700, 20)])
+def test_few_rows_of_an_fp32_head(N, h, V, K):
+    for rest in (False, True):
+        c = _case(N, h, V, K, "f32", seed=V + h, rest=False, scale=0.03)
+        r = np.random.Generator(np.random.PCG64(V))
+        c["T"] = 0.7 if N == 1 else 2.0
+        if rest:
+            with_rest(c, r)
+        c["G"] = r.normal(size=N).astype(np.float32)
+        if N > 1:
+            c["mask"] = np.ones(N, np.uint8)
+            c["mask"][1], c["G"][1] = 0, 0
+            c["H"][1] = float("nan")
+        clean = {**c, "H": torch.nan_to_num(c["H"])}
+        ref = want(clean)
+        close(run(c), ref, clean)
+        prev = torch.randn(V, h) * 0.01
+        got = run(c, prev=prev)
+        d = got["dW"] - prev.double().numpy() - ref["dW"]
+        assert np.linalg.norm(d) <= 1e-5 * np.linalg.norm(ref["dW"]) + 2 * U * np.linalg.norm(prev.double().numpy())
+
+
+@pytest.mark.parametrize("at", [1, 2, 4])
+def test_few_rows_inside_a_buffer(at):
+    """fp32 operands off 16-byte alignment, between elements that are not theirs."""
+    N, h, V, K = 3, 256, 700, 9
+    c = _case(N, h, V, K, "f32", seed=at, rest=False)
+    c["G"][:] = [0.5, -1.0, 2.0]
+    ref = want(c)
+
+    def inside(x, fill):
+        flat = torch.full((x.numel() + 8,), fill, device="cuda")
+        flat[at:at + x.numel()] = x.flatten().cuda()
+        return flat, flat[at:at + x.numel()].view(x.shape)
+
+    H, W = inside(c["H"], float("nan"))[1], inside(c["W"], float("nan"))[1]
+    (dh_buf, dH), (dw_buf, dW) = inside(torch.zeros(N, h), 7.0), inside(torch.zeros(V, h), 7.0)
+    ids, a, G = torch.from_numpy(c["ids"]).cuda(), c["a"].cuda(), torch.from_numpy(c["G"]).cuda()
+    o = {k: torch.empty(N, device="cuda") for k in ("loss", "lse", "lse_rest")}
+    z = torch.empty(N, K, device="cuda")
+    ws = sao.distill_workspace(N, h, V, K, torch.float32)
+    sao.sao_distill_loss_fwd(H, W, ids, a, 1.0, o["loss"], o["lse"], o["lse_rest"], z, ws)
+    sao.sao_distill_loss_bwd(H, W, ids, a, 1.0, o["lse"], o["lse_rest"], z, G, dH, dW, ws)
+    close({k: v.double().cpu().numpy() for k, v in {**o, "dH": dH, "dW": dW}.items()}, ref, c)
+    for buf, n in ((dh_buf, N * h), (dw_buf, V * h)):
+        assert (buf[:at] == 7).all() and (buf[at + n:] == 7).all()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("V,K", [(5, 5), (256, 256), (300, 300), (1100, 1024)])
 def test_entries_that_fill_tiles_or_the_vocabulary(V, K, dtype):
