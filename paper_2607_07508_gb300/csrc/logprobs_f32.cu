@@ -833,22 +833,26 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
 }
 
 // out[t][c] (+)= sum over the splits of part[split][row of t][c] (fixed order);
-// pos (nullable): token -> row, or -1 (zeros). A warp per token; rows of part
-// are 16-byte aligned.
+// pos (nullable): token -> row, or -1 (zeros). A warp per 128 columns of a token, eight
+// splits' loads in flight (a warp per token, each load waited for: 32 us more for a few rows
+// of 1,024 columns); rows of part are 16-byte aligned.
 __global__ void __launch_bounds__(256) f32_reduce_kernel(const float *part, int splits, int64_t split_stride,
                                                          int64_t ldp, const int *pos, int64_t rows, int h, float *out,
                                                          int accumulate) {
   grid_wait();
-  const int lane = threadIdx.x & 31;
+  const int lane = threadIdx.x & 31, pieces = (h + 127) / 128;
   const bool wide = (h & 3) == 0 && aligned16_dev(out);
-  for (int64_t t = int64_t(blockIdx.x) * 8 + (threadIdx.x >> 5); t < rows; t += int64_t(gridDim.x) * 8) {
+  for (int64_t w = int64_t(blockIdx.x) * 8 + (threadIdx.x >> 5); w < rows * pieces; w += int64_t(gridDim.x) * 8) {
+    const int64_t t = w / pieces;
+    const int c = int(w - t * pieces) * 128 + lane * 4;
     const int64_t i = pos ? int64_t(ld(pos + t)) : t;
     const float *src = part + i * ldp;
     float *dst = out + t * h;
-    for (int c = lane * 4; c < h; c += 128) {
+    if (c < h) {
       float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
       if (i >= 0) {
         s = __ldcs(reinterpret_cast<const float4 *>(src + c));
+#pragma unroll 8
         for (int k = 1; k < splits; ++k) {
           const float4 v = __ldcs(reinterpret_cast<const float4 *>(src + k * split_stride + c));
           s.x += v.x;
