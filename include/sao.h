@@ -485,8 +485,9 @@ SAO_API sao_status sao_distill_loss_fwd(const void *H, const void *W, sao_dtype 
  *                         so that it adds to another loss's dW; or for a bf16 head
  *                         SAO_BF16, overwritten only (a sum over calls needs fp32)
  * A bf16 head's dH and dW are 16-byte aligned. Its dZ is rounded to bf16 once
- * before the two products (as in sao_token_logprobs_bwd): 2^-9 of each of its
- * elements, 2^-17 up to 64 rows, not at all for one row of
+ * before the two products (as in sao_token_logprobs_bwd): 2^-8 of each of its
+ * elements, 2^-16 up to 64 rows and, up to 8,192, for the entries of the 32 rows
+ * that would lose most; not at all for one row of
  * h <= 6,144 or two of h <= 2,048. Few rows (those, and of an fp32 head up to
  * eight of h <= 1,024, four of h <= 2,048, one of h <= 4,096) read W once in each
  * direction.

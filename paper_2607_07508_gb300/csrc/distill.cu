@@ -223,9 +223,14 @@ template <int kSub>
 __global__ void __launch_bounds__(256)
     distill_rows_kernel(const int32_t *ids, const void *a, sao_dtype adt, const float *teacher_lse, const float *lse,
                         const float *lse_rest, const float *z_top, const float *grad, int64_t N, int K, float inv_t,
-                        uint8_t *mask, float *g_rest, float *rest, float *dz_top, unsigned int *range) {
+                        uint8_t *mask, float *g_rest, float *rest, float *dz_top, unsigned int *range, float *lost) {
   grid_wait();
   if (blockIdx.x == 0 && threadIdx.x < kRangeWords) range[threadIdx.x] = 0u;
+  if (lost != nullptr && blockIdx.x == 0 && threadIdx.x < kExtraRows) {
+    mask[N + threadIdx.x] = 1;
+    g_rest[N + threadIdx.x] = 0.f;
+    rest[N + threadIdx.x] = 0.f;
+  }
   const int64_t tid = int64_t(blockIdx.x) * blockDim.x + threadIdx.x;
   const int64_t row = tid / kSub;
   const int sub = int(tid % kSub);
@@ -243,21 +248,111 @@ __global__ void __launch_bounds__(256)
   }
   const float la = whole ? (on ? ld(teacher_lse + row) : 0.f) : teacher.log();
   const float l = on ? ld(lse + row) : 0.f, gt = g * inv_t;
-  float psum = 0.f;
+  float psum = 0.f, off = 0.f;  // off: what rounding the entries to bf16 takes
   for (int i = sub; i < n; i += kSub) {
     if (ld(ids + base + i) < 0) continue;
     const float p = expf(teacher_logit(a, adt, base + i) * inv_t - la);
     psum += p;
-    dz_top[base + i] = gt * (expf(ld(z_top + base + i) - l) - p);
+    const float d = gt * (expf(ld(z_top + base + i) - l) - p);
+    dz_top[base + i] = d;
+    off += fabsf(d - __bfloat162float(__float2bfloat16_rn(d)));
   }
   psum = sub_sum<kSub>(psum);
+  off = sub_sum<kSub>(off);
   if (!live || sub != 0) return;
+  if (lost != nullptr) lost[row] = off;
   mask[row] = on ? 1 : 0;
   if (!on) return;
   const bool none = lr == -INFINITY;  // the entries are all columns
   const float rho = whole && !none ? fmaxf(1.f - psum, 0.f) : 0.f;
   g_rest[row] = none ? 0.f : gt * (expf(lr - l) - rho);
   rest[row] = none ? 0.f : lr;
+}
+
+// The block's exclusive sums of v, and *total (every thread; `sh` of 33).
+__device__ __forceinline__ int block_before(int v, int *sh, int *total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int s = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int up = __shfl_up_sync(0xffffffffu, s, o);
+    if (lane >= o) s += up;
+  }
+  __syncthreads();
+  if (lane == 31) sh[warp] = s;
+  __syncthreads();
+  int before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < 32; ++w) {
+    if (w < warp) before += sh[w];
+    all += sh[w];
+  }
+  *total = all;
+  return before + s - v;
+}
+
+// extra[j]: the kExtraRows tokens with the largest lost[] (none with 0), one CTA. The least value that
+// is among them is found bit by bit, to 2^-11 of itself; where more tokens have it than
+// there is room for, the first ones. Bound by its barriers.
+__global__ void __launch_bounds__(1024) distill_extra_kernel(const float *lost, int N, int *extra) {
+  constexpr int kEach = int(kExtraMost / 1024), kLowBit = 12;
+  __shared__ int sh[32], counts[2][32];
+  grid_wait();
+  uint32_t key[kEach];
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int t = int(threadIdx.x) * kEach + i;
+    key[i] = t < N ? __float_as_uint(ld(lost + t)) : 0u;
+  }
+  auto among = [&](uint32_t low, uint32_t high) {  // keys in [low, high) of this thread
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) n += key[i] >= low && key[i] < high;
+    return n;
+  };
+  constexpr uint32_t kMost = 0x80000000u;
+  uint32_t least = 0u;
+  for (int bit = 30; bit >= kLowBit; --bit) {
+    const int n = __reduce_add_sync(0xffffffffu, among(least | 1u << bit, kMost));
+    if ((threadIdx.x & 31) == 0) counts[bit & 1][threadIdx.x >> 5] = n;
+    __syncthreads();
+    if (__reduce_add_sync(0xffffffffu, counts[bit & 1][threadIdx.x & 31]) >= kExtraRows) least |= 1u << bit;
+  }
+  if (threadIdx.x < kExtraRows) extra[threadIdx.x] = -1;
+  int taken = 0;
+  uint32_t low = least + (1u << kLowBit), high = kMost;
+#pragma unroll
+  for (int pass = 0; pass < 2; ++pass) {  // those above the least one, then those at it
+    int total, at = taken + block_before(among(low, high), sh, &total);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+      if (key[i] >= low && key[i] < high) {
+        if (at < kExtraRows) extra[at] = int(threadIdx.x) * kEach + i;
+        ++at;
+      }
+    taken += total;
+    high = low;
+    low = least > 0u ? least : 1u;
+  }
+}
+
+// CTA (j, 1,024 columns, part): acc[part][row of its token] += acc[part][extra row j].
+__global__ void __launch_bounds__(256) distill_fold_kernel(const TopGrad t, float *acc, const DhParts d, int h,
+                                                           const int *pos, const int *count) {
+  grid_wait();
+  const int token = ld(t.extra + blockIdx.x);
+  if (token < 0) return;
+  const int rows = *count, parts = d.cap_rows ? dh_parts(d, rows) : 1;
+  const int64_t to = ld(pos + token), from = ld(pos + t.tokens + blockIdx.x);
+  const int c = int(blockIdx.y * 256 + threadIdx.x) * 4;  // (h is a multiple of 8)
+  if (c >= h) return;
+  for (int k = blockIdx.z; k < parts; k += gridDim.z) {
+    float *part = acc + int64_t(k) * rows * h + c;
+    float4 x = *reinterpret_cast<const float4 *>(part + to * h);
+    const float4 y = *reinterpret_cast<const float4 *>(part + from * h);
+    x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
+    *reinterpret_cast<float4 *>(part + to * h) = x;
+  }
 }
 
 // A warp per compacted row.
@@ -269,8 +364,13 @@ __global__ void __launch_bounds__(256)
   grid_wait();
   const int64_t i = int64_t(blockIdx.x) * 8 + (threadIdx.x >> 5);
   if (i >= *count) return;
-  const int64_t t = ld(idx + i);
-  if (kPatch == kFewPieces && t < 0) return;
+  int64_t t = ld(idx + i);
+  bool second = kPatch == kFewPieces && i >= kFewRows;
+  if (kPatch == kOnePiece && g.extra != nullptr && t >= g.tokens) {
+    t = ld(g.extra + (t - g.tokens));
+    second = true;
+  }
+  if (t < 0) return;
   const int64_t base = t * g.K;
   float most = 0.f;
   for (int k = threadIdx.x & 31; k < g.K; k += 32) {
@@ -288,7 +388,7 @@ __global__ void __launch_bounds__(256)
       dst[2 * plane] = __float2bfloat16_rn(p2);
     } else {
       const __nv_bfloat16 b = __float2bfloat16_rn(d);
-      dst[0] = kPatch == kFewPieces && i >= kFewRows ? __float2bfloat16_rn(d - __bfloat162float(b)) : b;
+      dst[0] = second ? __float2bfloat16_rn(d - __bfloat162float(b)) : b;
     }
   }
   if constexpr (kPatch == kThreePlanes) raise_class(range, most);
@@ -367,14 +467,17 @@ FwdArrays take_fwd(Carver &c, int64_t N, int32_t V, int32_t K) {
 }
 struct BwdArrays {
   uint8_t *mask;
-  float *g, *rest, *dz_top;
+  float *g, *rest, *dz_top, *lost;
+  int *extra;
   unsigned int *range;
 };
 BwdArrays take_bwd(Carver &c, int64_t N, int32_t K) {
   BwdArrays b;
-  b.mask = c.take<uint8_t>(size_t(N));
-  b.g = c.take<float>(size_t(N));
-  b.rest = c.take<float>(size_t(N));
+  b.mask = c.take<uint8_t>(size_t(N + kExtraRows));
+  b.g = c.take<float>(size_t(N + kExtraRows));
+  b.rest = c.take<float>(size_t(N + kExtraRows));
+  b.lost = c.take<float>(size_t(N < kExtraMost ? N : kExtraMost));
+  b.extra = c.take<int>(kExtraRows);
   b.dz_top = c.take<float>(size_t(N) * size_t(K));
   b.range = c.take<unsigned int>(kRangeWords);
   return b;
@@ -409,6 +512,14 @@ sao_status distill_few_dH(const float *acc, const DhParts &parts, int32_t h, con
                           int64_t N, __nv_bfloat16 *dH, cudaStream_t s) {
   int slot = launch_begin("distill_few_dH", s);
   pdl(distill_few_dH_kernel, unsigned((N * h + 255) / 256), 256, 0, s)(acc, parts, h, pos, count, N, dH);
+  return launch_end(slot, s);
+}
+
+sao_status distill_fold_extra(const TopGrad &t, float *acc, const DhParts &parts, int32_t h, const int *pos,
+                              const int *count, cudaStream_t s) {
+  int slot = launch_begin("distill_fold", s);
+  const dim3 grid(unsigned(kExtraRows), unsigned((h + 1023) / 1024), parts.cap_rows ? 8u : 1u);
+  pdl(distill_fold_kernel, grid, 256, 0, s)(t, acc, parts, h, pos, count);
   return launch_end(slot, s);
 }
 
@@ -469,11 +580,18 @@ sao_status distill_bwd_launch(const void *H, const void *W, sao_dtype dt, const 
   if (!c.ok()) return fail(SAO_ERR_WORKSPACE, "workspace too small for the distillation backward");
   const float inv_t = 1.f / temperature;
   const int sub = row_threads(N);
+  const bool extra = dt == SAO_BF16 && extra_rows(N);
   int slot = launch_begin("distill_rows", s);
   pdl(sub == 32 ? distill_rows_kernel<32> : distill_rows_kernel<8>, unsigned((N * sub + 255) / 256), 256, 0, s)(
-      ids, a, adt, teacher_lse, lse, lse_rest, z_top, grad, N, K, inv_t, w.mask, w.g, w.rest, w.dz_top, w.range);
+      ids, a, adt, teacher_lse, lse, lse_rest, z_top, grad, N, K, inv_t, w.mask, w.g, w.rest, w.dz_top, w.range,
+      extra ? w.lost : nullptr);
   SAO_TRY(launch_end(slot, s));
-  const TopGrad t{w.mask, w.g, w.rest, w.dz_top, ids, K, inv_t, w.range};
+  if (extra) {
+    slot = launch_begin("distill_extra", s);
+    pdl(distill_extra_kernel, 1, 1024, 0, s)(w.lost, int(N), w.extra);
+    SAO_TRY(launch_end(slot, s));
+  }
+  const TopGrad t{w.mask, w.g, w.rest, w.dz_top, ids, K, inv_t, w.range, extra ? w.extra : nullptr, N};
   if (gemv_takes(N, h, dt))
     return gemv_distill_bwd(H, W, dt, t, N, h, V, dH, dW, dw_dt, accumulate, c, s);
   if (dt == SAO_BF16) return tc_distill_bwd(H, W, t, N, h, V, dH, dW, dw_dt, accumulate, err, c, s);

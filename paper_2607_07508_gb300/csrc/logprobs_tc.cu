@@ -1480,15 +1480,17 @@ sao_status bwd_recompute_block(const void *H, const void *W, const int32_t *y, c
   const int Vc = pl.vc;
   const bool few = top != nullptr && N <= kFewRows;  // dZ in two pieces, in 128 rows
   const bool multi = Vc < V;                      // several vocabulary chunks
-  const bool f32_dh = multi || pl.splits > 1 || few;  // dH through fp32 rows, rounded at the end
+  const bool extra = top != nullptr && top->extra != nullptr;  // kExtraRows more rows: second pieces
+  const bool f32_dh = multi || pl.splits > 1 || few || extra;  // dH through fp32 rows, rounded at the end
   // Rows whose incoming gradient is zero contribute nothing: compact the rest.
   CompactRows cr{};
   if (few)
     SAO_TRY(distill_few_rows(mask, N, static_cast<const __nv_bfloat16 *>(H), h, &cr, c, s));
   else
-    SAO_TRY(compact_rows(mask, mask ? nullptr : G, N, static_cast<const __nv_bfloat16 *>(H), h, &cr, c, s));
+    SAO_TRY(compact_rows(mask, mask ? nullptr : G, extra ? N + kExtraRows : N, static_cast<const __nv_bfloat16 *>(H), h,
+                         &cr, c, s, extra ? top->extra : nullptr, N));
   const int64_t tokens = N;
-  if (few) N = 2 * kFewRows;  // rows of the products from here on
+  N = few ? 2 * kFewRows : extra ? N + kExtraRows : N;  // rows of the products from here on
   __nv_bfloat16 *dz = c.take<__nv_bfloat16>(size_t(N) * size_t(Vc));
   const DhParts parts = dh_scratch(pl.splits, pl.rows, h, Vc < V ? Vc : V);
   float *dh_acc = f32_dh ? c.take<float>(size_t(pl.splits) * size_t(pl.rows) * size_t(h)) : nullptr;
@@ -1575,9 +1577,11 @@ sao_status bwd_recompute_block(const void *H, const void *W, const int32_t *y, c
     }
     if (few && last)
       SAO_TRY(distill_few_dH(dh_acc, parts, h, cr.pos, cr.count, tokens, static_cast<__nv_bfloat16 *>(dH), s));
-    else if (f32_dh && last)
-      SAO_TRY(scatter_rows_to_bf16(dh_acc, parts, h, nullptr, cr.pos, cr.idx, cr.count, N,
+    else if (f32_dh && last) {
+      if (extra) SAO_TRY(distill_fold_extra(*top, dh_acc, parts, h, cr.pos, cr.count, s));
+      SAO_TRY(scatter_rows_to_bf16(dh_acc, parts, h, nullptr, cr.pos, cr.idx, cr.count, tokens,
                                    static_cast<__nv_bfloat16 *>(dH), overwrite_dH, s));
+    }
   }
   return SAO_OK;
 }
@@ -1604,12 +1608,12 @@ sao_status bwd_recompute(const void *H, const void *W, const int32_t *y, const f
 }  // namespace
 
 // The plan takes one block of rows: a bf16 dW is written from its whole sum. Few rows
-// take 128 (see kFewRows).
+// take 128 (see kFewRows), more of them some extra ones (kExtraRows).
 namespace {
-int64_t distill_rows(int64_t N) { return N <= kFewRows ? 2 * kFewRows : N; }
+int64_t distill_rows(int64_t N) { return N <= kFewRows ? 2 * kFewRows : extra_rows(N) ? N + kExtraRows : N; }
 }  // namespace
 size_t tc_distill_bwd_bytes(int64_t N, int32_t h, int32_t V) {
-  return recompute_bytes(bwd_plan(distill_rows(N), h, V, true), h, V, N <= kFewRows);
+  return recompute_bytes(bwd_plan(distill_rows(N), h, V, true), h, V, N <= kExtraMost);
 }
 sao_status tc_distill_bwd(const void *H, const void *W, const TopGrad &t, int64_t N, int32_t h, int32_t V, void *dH,
                           void *dW, sao_dtype dw_dt, int accumulate, unsigned int *err, Carver &c, cudaStream_t s) {

@@ -150,7 +150,7 @@ __global__ void __launch_bounds__(kScanThreads) compact_scatter_kernel(const uin
 
 // H_c[i] = H[idx[i]] for i < count; rows [count, round_up(count, 128)) = 0.
 __global__ void gather_rows_kernel(const __nv_bfloat16 *H, int h, const int *idx, const int *count,
-                                   __nv_bfloat16 *Hc, int64_t rows_cap) {
+                                   __nv_bfloat16 *Hc, int64_t rows_cap, const int *extra, int64_t tokens) {
   grid_wait();
   const int n = *count;
   const int64_t pad = (int64_t(n) + 127) / 128 * 128;
@@ -160,7 +160,9 @@ __global__ void gather_rows_kernel(const __nv_bfloat16 *H, int h, const int *idx
     const int64_t i = e / vec;
     const int v = int(e - i * vec);
     uint4 val = make_uint4(0u, 0u, 0u, 0u);
-    if (i < n) val = reinterpret_cast<const uint4 *>(H + int64_t(idx[i]) * h)[v];
+    int64_t t = i < n ? idx[i] : -1;
+    if (extra != nullptr && t >= tokens) t = extra[t - tokens];
+    if (t >= 0) val = reinterpret_cast<const uint4 *>(H + t * h)[v];
     reinterpret_cast<uint4 *>(Hc + i * h)[v] = val;
   }
 }
@@ -269,7 +271,7 @@ sao_status list_rows(const uint8_t *mask, const float *g, int64_t N, RowList *ou
 }
 
 sao_status compact_rows(const uint8_t *mask, const float *g, int64_t N, const __nv_bfloat16 *H, int32_t h,
-                        CompactRows *out, Carver &c, cudaStream_t s) {
+                        CompactRows *out, Carver &c, cudaStream_t s, const int *extra, int64_t tokens) {
   const int64_t cap = (N + 127) / 128 * 128;
   SAO_TRY(list_rows(mask, g, N, out, c, s));
   out->Hc = c.take<__nv_bfloat16>(size_t(cap) * size_t(h));
@@ -278,7 +280,8 @@ sao_status compact_rows(const uint8_t *mask, const float *g, int64_t N, const __
   DeviceInfo di;
   SAO_TRY(device_info(&di));
   int slot = launch_begin("gather_rows", s);
-  pdl(gather_rows_kernel, unsigned(di.sm_count * 8), 256, 0, s)(H, h, out->idx, out->count, out->Hc, cap);
+  pdl(gather_rows_kernel, unsigned(di.sm_count * 8), 256, 0, s)(H, h, out->idx, out->count, out->Hc, cap, extra,
+                                                                   tokens);
   return launch_end(slot, s);
 }
 

@@ -26,9 +26,10 @@ size_t compact_ws_bytes(int64_t N, int32_t h);
 
 // Active rows are those with mask[t] != 0 (mask given) or g[t] != 0.
 sao_status list_rows(const uint8_t *mask, const float *g, int64_t N, RowList *out, Carver &c, cudaStream_t s);
-// The list, and the active rows of H gathered in its order.
+// The list, and the active rows of H gathered in its order. `extra`: H has `tokens` < N rows,
+// and the row of token t >= tokens is that of token extra[t - tokens] (-1: zeros).
 sao_status compact_rows(const uint8_t *mask, const float *g, int64_t N, const __nv_bfloat16 *H, int32_t h,
-                        CompactRows *out, Carver &c, cudaStream_t s);
+                        CompactRows *out, Carver &c, cudaStream_t s, const int *extra = nullptr, int64_t tokens = 0);
 
 // dH[t] = bf16(sum over the parts k of acc[(k * count + pos[t]) * h ..]) on the
 // active rows, times scale[pos[t]] where a scale is given (all_rows only); inactive
