@@ -5,7 +5,7 @@
 // The tensor core truncates as it adds to its accumulator. Over a contraction of 2,048
 // that moved a logit of 12 by 2.6e-5, always towards zero, and the losses by 2.7e-6 of
 // themselves (7.2e-6 at h = 6,144), three to five times what fp32 FMAs lose. So the
-// accumulator is emptied every kPart elements of the contraction and the parts are added
+// accumulator is emptied every 512 elements of the contraction (up to 128 rows: 128) and the parts are added
 // in fp32 registers: a part's accumulator is smaller by the number of parts, and so is
 // what truncation takes. Sixteen warps hold a 128x256 tile as 64 sums a thread. Losses
 // off by (h = 2,048) and time of 12,288 rows on the moe head, with warps that still polled:
@@ -39,8 +39,11 @@ using namespace tc;
 
 constexpr int TM = 128, TN = 256, KB = 64;
 static_assert(TN == kTopTile, "offsets count entries by tile");
-constexpr int kPart = 512;                   // contraction elements between two read-outs of an accumulator
-constexpr int kPartBlocks = kPart / KB;
+// Contraction elements between two read-outs of an accumulator. One tile of rows waits for the bytes of
+// W, so it is emptied four times as often: 3 to 64 rows of the moe head in the same 113-135
+// us, the losses off by 2e-7 instead of 5e-7 to 1e-6. (With two tiles 130 -> 145 us.)
+constexpr int kPart = 512, kFewPart = 128;
+constexpr int64_t kFewPartRows = 128;
 constexpr uint32_t A_BYTES = TM * KB * 2, B_BYTES = TN * KB * 2;
 constexpr uint32_t RING_BYTES = 4 * (A_BYTES + B_BYTES);  // 4 stages, or 6 of half a B tile
 constexpr int kMaxStages = 6;
@@ -63,6 +66,7 @@ static_assert(SMEM_BYTES <= 232448, "shared memory of an SM");
 
 struct FwdParams {
   int nM, nN, nK;      // tiles along M and N, 64-wide K blocks
+  int part_blocks;     // K blocks between two read-outs of an accumulator, a power of two
   int group_m;         // tile raster: group_m M tiles per group, M fastest inside
   int64_t rows;        // rows of H, and the stride of part
   int vocab;
@@ -202,7 +206,7 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
       bool ok = true;
       for (int L = cl; L < tiles && ok; L += ncl) {
         for (int kb = 0; kb < p.nK; ++kb) {
-          const int in_part = kb % kPartBlocks;
+          const int in_part = kb & (p.part_blocks - 1);
           if ((in_part == 0 && !mbar_wait(smem_u32(&ctl->acc_empty[acc]), acc_phase ^ 1u, abort, p.err)) ||
               !mbar_wait(smem_u32(&ctl->full[stage]), phase, abort, p.err)) {
             ok = false;
@@ -225,7 +229,7 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
             stage = 0;
             phase ^= 1u;
           }
-          if (in_part == kPartBlocks - 1 || kb == p.nK - 1) {
+          if (in_part == p.part_blocks - 1 || kb == p.nK - 1) {
             commit(&ctl->acc_full[acc]);
             if (++acc == ACCS) {
               acc = 0;
@@ -241,7 +245,7 @@ __global__ void __launch_bounds__(NUM_THREADS, 1)
     const int quad = warp & 3;  // TMEM lane quadrant this warp may access
     const int quarter = (warp - 4) >> 2;
     const int r = quad * 32 + lane;
-    const int parts = (p.nK + kPartBlocks - 1) / kPartBlocks;
+    const int parts = (p.nK + p.part_blocks - 1) / p.part_blocks;
     const float scale = p.top.inv_t * kLog2e;
     int a = 0, local = 0;
     uint32_t a_phase = 0;
@@ -446,6 +450,7 @@ sao_status tc_distill_fwd(const void *H, const void *W, const uint8_t *row_mask,
   p.nM = int((N + TM * cg - 1) / (TM * cg));
   p.nN = nvt;
   p.nK = (h + KB - 1) / KB;
+  p.part_blocks = (N <= kFewPartRows ? kFewPart : kPart) / KB;
   p.group_m = 64;  // as the log-prob forward: 32 MB of H stay in L2 while W streams
   p.rows = N;
   p.vocab = V;
