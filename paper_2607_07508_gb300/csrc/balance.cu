@@ -714,12 +714,14 @@ __global__ void __launch_bounds__(kThreads<T, kVec, kC>)
     if (on && r >= seg_end) {
       while (b + 1 < a.B && seg_at(a, b + 1) <= r) ++b;
       seg_end = b + 1 < a.B ? seg_at(a, b + 1) : a.N;
-      const float n = float(ld(rows + b));
+      // weights from the even load on: a constant in all of them has no gradient, and takes digits
+      const int64_t counted = ld(rows + b), even = counted * a.k / a.E;
+      const float n = float(counted);
       const float f = n > 0.f ? g * float(a.E) / (float(a.k) * n * n * float(used)) : 0.f;
 #pragma unroll
       for (int j = 0; j < kC; ++j) {
         const int c = Row<T, kVec, kC>::column(j, l, lanes);
-        w[j] = c < a.E ? f * float(ld(counts + int64_t(b) * a.E + c)) : 0.f;
+        w[j] = c < a.E ? f * float(ld(counts + int64_t(b) * a.E + c) - even) : 0.f;
       }
     }
     x.wait();

@@ -189,6 +189,17 @@ def test_device_checks():
 
 
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("N,E,k", [(37, 4, 4), (300, 12, 12), (500, 8, 1)])
+def test_an_even_load_has_no_gradient(N, E, k, score):
+    x, ids, _, _ = _case(N, E, k, seed=N, mask=False)
+    if k == 1:
+        ids = (np.arange(N, dtype=np.int32) % E)[:N // E * E, None].copy()
+        x = x[:N // E * E]
+    got = run(x, ids, score)
+    assert (got["dlogits"] == 0).all() and abs(got["loss"] - 1) <= (16 + 4 * np.sqrt(N)) * U
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 def test_gradient_against_differences(score):
     """Central differences of the kernels' loss along random directions of at most 1 an element: the curvature term
     is below d^2 |loss| and the loss's rounding (40 u) enters over d."""
