@@ -449,8 +449,10 @@ SAO_API sao_status sao_value_loss(const float *values, const float *ret, const u
  *   loss[t] = sum_k p_k (a_k - la - z_k + lse) + rho (log rho - (lse_rest - lse))
  * the Kullback-Leibler divergence from the teacher's distribution to the
  * student's, with lse over all columns and lse_rest over those without an entry
- * (-inf, and rho = 0, where the entries are the whole vocabulary). Not scaled by
- * T^2. The [N, V] logits are never stored.
+ * (-inf, and rho = 0, where the entries are the whole vocabulary). The p_k are taken
+ * as they are: where they add up to more than 1 (entries rounded to bf16 against the
+ * log-sum-exp of the exact logits), or are the whole vocabulary's and do not add up to
+ * 1, the loss is least, though not 0, at q_k in proportion to p_k. Not scaled by T^2. The [N, V] logits are never stored.
  *   H [N, h], W [V, h] dt      top_ids [N, K] int32 in any order, each below V and
  *                              at most once a row
  *   top_logits [N, K] top_dt   teacher_lse [N] fp32 or NULL
@@ -475,8 +477,9 @@ SAO_API sao_status sao_distill_loss_fwd(const void *H, const void *W, sao_dtype 
                                         void *ws, size_t ws_bytes, sao_stream_t stream);
 
 /*
- * Gradient of sum_t grad_loss[t] * loss[t]: with q = e^(z - lse),
- *   dz_k = q_k - p_k at the entries, dz_v = e^(z_v - lse_rest) (e^(lse_rest - lse)
+ * Gradient of sum_t grad_loss[t] * loss[t]: with q = e^(z - lse) and the teacher's mass
+ * m = sum_k p_k + rho (1 mostly; renormalised: 1),
+ *   dz_k = m q_k - p_k at the entries, dz_v = e^(z_v - lse_rest) (m e^(lse_rest - lse)
  *   - rho) elsewhere, dZ = grad_loss dz / T, dH = dZ W, dW = dZ^T H.
  *   lse, lse_rest, z_top  from the forward on the same inputs
  *   grad_loss [N] fp32    rows with 0 contribute nothing

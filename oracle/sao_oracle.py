@@ -593,7 +593,9 @@ def distill_loss(H, W, top_ids, top_logits, temperature: float, teacher_lse=None
     teacher's entries S (ids >= 0) and the vocabulary outside S as one outcome.
     teacher_lse None: the teacher is renormalised over S and gives the rest no
     mass; otherwise log sum exp(logit / T) over the teacher's vocabulary, whose
-    mass outside S is max(0, 1 - sum p) (0 when S is the whole vocabulary).
+    mass outside S is max(0, 1 - sum p) (0 when S is the whole vocabulary). The
+    teacher's mass sum p + that is 1 unless the entries' p, taken as they are, add
+    up to more, or are the whole vocabulary and add up to something else.
     Returns loss, lse, lse_rest, z_top and, for d sum(grad * loss), dH and dW.
     Masked rows: loss = lse = 0; without anything to learn from: loss 0. Rows
     with an id out of range or twice: loss NaN. None of these has a gradient,
@@ -640,8 +642,9 @@ def distill_loss(H, W, top_ids, top_logits, temperature: float, teacher_lse=None
                 continue
             out["lse_rest"][t] = lse_rest
             if grad is not None and grad[t] != 0:
-                dz = np.exp(z - lse_rest) * (np.exp(lse_rest - lse) - rho) if rest.any() else np.zeros(V)
-                dz[S] = np.exp(zk - lse) - p
+                mass = p.sum() + rho if teacher_lse is not None else 1.0
+                dz = np.exp(z - lse_rest) * (mass * np.exp(lse_rest - lse) - rho) if rest.any() else np.zeros(V)
+                dz[S] = mass * np.exp(zk - lse) - p
                 dz *= float(grad[t]) / temperature
                 out["dH"][t] = dz @ Wd
                 out["dW"] += np.outer(dz, Hd[t])

@@ -10,9 +10,11 @@
 // with lse over all columns and lse_R over those outside S. The forward's epilogues
 // sum e^z outside S and keep z_k, so lse_R comes from a sum of its own terms: as
 // 1 - sum q_k it would have no digits left where the student puts its mass on S.
-//   d loss / d z_k = q_k - p_k on S,  e^{z_v - lse_R} (q_R - rho) outside,
-// q_k = e^{z_k - lse}, q_R = e^{lse_R - lse}: the second is q_v (1 - rho / q_R)
-// without a quotient that overflows as q_R vanishes.
+//   d loss / d z_k = m q_k - p_k on S,  e^{z_v - lse_R} (m q_R - rho) outside,
+// m = sum p + rho, q_k = e^{z_k - lse}, q_R = e^{lse_R - lse}: the second is
+// q_v (m - rho / q_R) without a quotient that overflows as q_R vanishes. The teacher's
+// mass m is 1 but where the entries' p add up to more (logits rounded to bf16 against the
+// log-sum-exp of the exact ones), or are the whole vocabulary and do not add up to 1.
 #include <cuda_bf16.h>
 #include <math.h>
 #include <stdint.h>
@@ -248,24 +250,30 @@ __global__ void __launch_bounds__(256)
   }
   const float la = whole ? (on ? ld(teacher_lse + row) : 0.f) : teacher.log();
   const float l = on ? ld(lse + row) : 0.f, gt = g * inv_t;
-  float psum = 0.f, off = 0.f;  // off: what rounding the entries to bf16 takes
+  const bool none = lr == -INFINITY;  // the entries are all columns
+  float mass = 1.f, rho = 0.f;        // of the teacher: in all, and outside the entries
+  if (whole) {
+    float psum = 0.f;
+    for (int i = sub; i < n; i += kSub)
+      if (ld(ids + base + i) >= 0) psum += expf(teacher_logit(a, adt, base + i) * inv_t - la);
+    psum = sub_sum<kSub>(psum);
+    mass = none ? psum : fmaxf(psum, 1.f);
+    rho = none ? 0.f : fmaxf(1.f - psum, 0.f);
+  }
+  float off = 0.f;  // what rounding the entries to bf16 takes
   for (int i = sub; i < n; i += kSub) {
     if (ld(ids + base + i) < 0) continue;
     const float p = expf(teacher_logit(a, adt, base + i) * inv_t - la);
-    psum += p;
-    const float d = gt * (expf(ld(z_top + base + i) - l) - p);
+    const float d = gt * (mass * expf(ld(z_top + base + i) - l) - p);
     dz_top[base + i] = d;
     off += fabsf(d - __bfloat162float(__float2bfloat16_rn(d)));
   }
-  psum = sub_sum<kSub>(psum);
   off = sub_sum<kSub>(off);
   if (!live || sub != 0) return;
   if (lost != nullptr) lost[row] = off;
   mask[row] = on ? 1 : 0;
   if (!on) return;
-  const bool none = lr == -INFINITY;  // the entries are all columns
-  const float rho = whole && !none ? fmaxf(1.f - psum, 0.f) : 0.f;
-  g_rest[row] = none ? 0.f : gt * (expf(lr - l) - rho);
+  g_rest[row] = none ? 0.f : gt * (mass * expf(lr - l) - rho);
   rest[row] = none ? 0.f : lr;
 }
 
