@@ -467,7 +467,9 @@ SAO_API sao_status sao_value_loss(const float *values, const float *ret, const u
  * bf16 H and W are 16-byte aligned. Their logits' sums leave the tensor cores,
  * which truncate as they add, every 512 elements of h and go on in fp32: lse is
  * within 5e-7 of itself up to h = 6,144.
- * The workspace of both calls: sao_distill_workspace_bytes.
+ * The workspace of both calls: sao_distill_workspace_bytes, which never falls as N or K
+ * grows: one buffer, sized for the most rows, serves every call of fewer (with the same
+ * h, V, dtype and dZ budget), although some of those need more than a call of N does.
  */
 SAO_API size_t sao_distill_workspace_bytes(int64_t N, int32_t h, int32_t V, int32_t K, sao_dtype dt);
 SAO_API sao_status sao_distill_loss_fwd(const void *H, const void *W, sao_dtype dt, const int32_t *top_ids,
@@ -529,8 +531,8 @@ SAO_API sao_status sao_distill_loss_bwd(const void *H, const void *W, sao_dtype 
  *   those up before the backward and form the loss from the sums.
  * A row of logits that are all -inf has no probabilities and no gradient.
  * Deterministic. 1 <= k <= E <= SAO_BALANCE_MAX_EXPERTS. Workspace of
- * the forward: sao_balance_workspace_bytes(N, E, B); the backward needs the error
- * word's 256 bytes only.
+ * the forward: sao_balance_workspace_bytes(N, E, B), which never falls as one of them
+ * grows; the backward needs the error word's 256 bytes only.
  */
 SAO_API size_t sao_balance_workspace_bytes(int64_t N, int32_t E, int32_t B);
 SAO_API sao_status sao_balance_loss_fwd(const void *logits, sao_dtype dt, const int32_t *expert_ids,

@@ -813,9 +813,10 @@ void with_layout(const Layout &l, int score, F f) {
 // trajectories 47 -> 42 us, 98,301 x 63 in 96 42 -> 37; a batch of 65,536 x 128 30 -> 37).
 int ctas_of(bool segments) { return segments ? 4 : 1; }
 // Rows per CTA, at least 64. From N alone: the sums' order does not depend on the device.
+constexpr int64_t kLeastChunk = 64;
 int chunk_rows(int64_t N, bool segments) {
   const int64_t ctas = 152 * ctas_of(segments), c = (N + ctas - 1) / ctas;
-  return int(c < 64 ? 64 : c);
+  return int(c < kLeastChunk ? kLeastChunk : c);
 }
 BalanceArgs make_args(const void *x, const int32_t *ids, const uint8_t *mask, const int32_t *cu, int32_t B, int64_t N,
                       int32_t E, int32_t k, unsigned int *err) {
@@ -878,8 +879,9 @@ struct Scratch {
   unsigned int *ticket;
 };
 Scratch take(Carver &c, int64_t N, int32_t E, int32_t B) {
-  const int64_t chunk = chunk_rows(N, true);  // (a batch takes fewer)
-  const size_t slots = size_t((N + chunk - 1) / chunk) + size_t(B);
+  // the most chunks that up to N rows make (a batch fewer), so that a call of fewer rows fits too
+  const int64_t most = 152 * ctas_of(true), chunks = (N + kLeastChunk - 1) / kLeastChunk;
+  const size_t slots = size_t(chunks < most ? chunks : most) + size_t(B);
   Scratch s;
   s.psum = c.take<float>(slots * size_t(E));
   s.pcount = c.take<int>(slots * size_t(E));

@@ -555,6 +555,22 @@ size_t distill_ws_bytes(int64_t N, int32_t h, int32_t V, int32_t K, sao_dtype dt
   return f.off + head_f > b.off + head_b ? f.off + head_f : b.off + head_b;
 }
 
+size_t distill_ws_most(int64_t N, int32_t h, int32_t V, int32_t K, sao_dtype dt) {
+  if (N <= 0) return 0;
+  Carver f(nullptr, ~size_t(0)), b(nullptr, ~size_t(0));
+  take_fwd(f, N, V, K);
+  take_bwd(b, N, K);
+  const int64_t few = gemv_rows(h, dt), n = N < few ? N : few;
+  size_t head_f = n > 0 ? gemv_fwd_bytes(n, V) : 0, head_b = n > 0 ? gemv_bwd_bytes(n, h, V) : 0;
+  if (N > few) {
+    const size_t more_f = dt == SAO_BF16 ? tc_distill_fwd_bytes(N, h, V) : f32_ws_most(N, h, V);
+    const size_t more_b = dt == SAO_BF16 ? tc_distill_bwd_most(N, h, V) : f32_ws_most(N, h, V);
+    head_f = more_f > head_f ? more_f : head_f;
+    head_b = more_b > head_b ? more_b : head_b;
+  }
+  return f.off + head_f > b.off + head_b ? f.off + head_f : b.off + head_b;
+}
+
 sao_status distill_fwd_launch(const void *H, const void *W, sao_dtype dt, const int32_t *ids, const void *a,
                               sao_dtype adt, const float *teacher_lse, const uint8_t *row_mask, int64_t N, int32_t h,
                               int32_t V, int32_t K, float temperature, float *loss, float *lse, float *lse_rest,

@@ -98,6 +98,7 @@ sao_status distill_finish(const TopRef &top, const TopFinish &f, const float2 *p
 // is left of the call's workspace.
 size_t tc_distill_fwd_bytes(int64_t N, int32_t h, int32_t V);
 size_t tc_distill_bwd_bytes(int64_t N, int32_t h, int32_t V);
+size_t tc_distill_bwd_most(int64_t N, int32_t h, int32_t V);
 sao_status tc_distill_fwd(const void *H, const void *W, const uint8_t *row_mask, int64_t N, int32_t h, int32_t V,
                           const TopRef &top, const TopFinish &f, unsigned int *err, Carver &c, cudaStream_t s);
 sao_status tc_distill_bwd(const void *H, const void *W, const TopGrad &t, int64_t N, int32_t h, int32_t V, void *dH,
@@ -109,6 +110,7 @@ sao_status f32_distill_bwd(const float *H, const float *W, const TopGrad &t, int
 
 // distill_rows.cu: a few rows on the fp32 units, W read once by each direction.
 bool gemv_takes(int64_t N, int32_t h, sao_dtype dt);
+int64_t gemv_rows(int32_t h, sao_dtype dt);  // the most rows that it takes
 size_t gemv_fwd_bytes(int64_t N, int32_t V);
 size_t gemv_bwd_bytes(int64_t N, int32_t h, int32_t V);
 sao_status gemv_distill_fwd(const void *H, const void *W, sao_dtype dt, const uint8_t *row_mask, int64_t N, int32_t h,
@@ -116,8 +118,10 @@ sao_status gemv_distill_fwd(const void *H, const void *W, sao_dtype dt, const ui
 sao_status gemv_distill_bwd(const void *H, const void *W, sao_dtype dt, const TopGrad &t, int64_t N, int32_t h,
                             int32_t V, void *dH, void *dW, sao_dtype dw_dt, int accumulate, Carver &c, cudaStream_t s);
 
-// distill.cu, called by the C entry points
+// distill.cu, called by the C entry points. _bytes: what a call of N rows needs; _most: of up
+// to N rows (the paths for different N need different scratch, and more rows often less).
 size_t distill_ws_bytes(int64_t N, int32_t h, int32_t V, int32_t K, sao_dtype dt);
+size_t distill_ws_most(int64_t N, int32_t h, int32_t V, int32_t K, sao_dtype dt);
 sao_status distill_fwd_launch(const void *H, const void *W, sao_dtype dt, const int32_t *ids, const void *a,
                               sao_dtype adt, const float *teacher_lse, const uint8_t *row_mask, int64_t N, int32_t h,
                               int32_t V, int32_t K, float temperature, float *loss, float *lse, float *lse_rest,

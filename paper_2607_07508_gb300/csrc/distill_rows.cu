@@ -452,11 +452,12 @@ void launch_bwd(const void *H, const void *W, const TopGrad &t, int64_t N, int32
 // fp32, where that path splits W into three planes and multiplies them six times: eight rows of up to
 // 1,024 columns, four of up to 2,048, one of up to 4,096: h = 1,024, V = 32,000 88 / 357 for one row,
 // 100 / 359 for two to four, 135 / 360 for eight; h = 515, V = 20,000 44 / 204, 63 / 207, 94 / 208.
-bool gemv_takes(int64_t N, int32_t h, sao_dtype dt) {
+int64_t gemv_rows(int32_t h, sao_dtype dt) {
   const int u = units_of(dt, h);
-  if (dt == SAO_BF16) return N * u <= (N == 1 ? 3 : N == 2 ? 2 : 0);
-  return N <= (u == 1 ? 8 : u == 2 ? 4 : u <= 4 ? 1 : 0);
+  if (dt == SAO_BF16) return u == 1 ? 2 : u <= 3 ? 1 : 0;
+  return u == 1 ? 8 : u == 2 ? 4 : u <= 4 ? 1 : 0;
 }
+bool gemv_takes(int64_t N, int32_t h, sao_dtype dt) { return N <= gemv_rows(h, dt); }
 
 size_t gemv_fwd_bytes(int64_t N, int32_t V) { return round256(sizeof(float2) * size_t(grid_of(V)) * size_t(N)); }
 size_t gemv_bwd_bytes(int64_t N, int32_t h, int32_t V) {

@@ -79,6 +79,7 @@ sao_status make_map(CUtensorMap *m, const void *ptr, uint64_t inner, uint64_t ou
                     uint32_t box_inner, uint32_t box_outer);
 
 size_t f32_ws_bytes(int64_t N, int32_t h, int32_t V);
+size_t f32_ws_most(int64_t N, int32_t h, int32_t V);
 sao_status f32_fwd(const float *H, const float *W, const int32_t *y, const uint8_t *row_mask, int64_t N,
                     int32_t h, int32_t V, float *logp, float *lse, unsigned int *err, void *ws, size_t ws_bytes,
                     cudaStream_t s);

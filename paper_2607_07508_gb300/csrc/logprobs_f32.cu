@@ -967,6 +967,36 @@ size_t f32_ws_bytes(int64_t N, int32_t h, int32_t V) {
   return fwd > bwd ? fwd : bwd;
 }
 
+// At least f32_ws_bytes of any call of up to N rows, and never less for more rows: each
+// array at the most that those calls give it.
+size_t f32_ws_most(int64_t N, int32_t h, int32_t V) {
+  const F32Plan q = f32_plan(N, h, V), one = f32_plan(1, h, V);  // (fewer rows: no fewer columns in a chunk)
+  const int64_t nvt = (int64_t(V) + HN - 1) / HN, vpad = up(V, TN), nh = up(h, TN) / TN;
+  const int any = V / 512 < 1 ? 1 : V / 512 < 16 ? V / 512 : 16;  // parts of dH over whatever chunk
+  int64_t dh_rows = q.cap;
+  for (int64_t m = 1; m * TM <= q.cap && may_split(m * nh); ++m) {
+    const F32Plan r = f32_plan(m * TM, h, V);
+    const int64_t rows = (r.vc_bwd < V ? any : r.s_dh) * r.cap;
+    dh_rows = rows > dh_rows ? rows : dh_rows;
+  }
+  const int64_t parts = N / 512 < 1 ? 1 : N / 512 < 16 ? N / 512 : 16;  // of dW
+  int64_t dw_cols = (h & 7) != 0 ? one.vc_bwd : 0;
+  if (parts > 1 && may_split(up(q.vc_bwd, TM) / TM * nh)) {
+    int64_t cols = (2 * 152 - 1) / nh * TM;  // of the most tiles that are cut
+    cols = parts * (cols < one.vc_bwd ? cols : one.vc_bwd);
+    dw_cols = cols > dw_cols ? cols : dw_cols;
+  }
+  const size_t budget = dz_budget(), all = size_t(PL) * 2 * size_t(q.cap) * size_t(vpad),
+               least = size_t(PL) * 2 * size_t(q.cap) * TN, bound = budget > least ? budget : least;
+  const size_t common = 256 + list_ws_bytes(N) + round256(size_t(PL) * size_t(q.cap) * size_t(q.hp) * 2);
+  const size_t fwd = common + round256(size_t(PL) * size_t(q.vc_fwd) * size_t(q.hp) * 2) +
+                     round256(sizeof(float2) * size_t(nvt) * size_t(N)) + round256(sizeof(float) * size_t(N));
+  const size_t bwd = common + round256(size_t(PL) * size_t(one.vc_bwd) * size_t(q.hp) * 2) +
+                     round256(all < bound ? all : bound) + round256(sizeof(float) * size_t(dh_rows) * size_t(q.hq)) +
+                     round256(sizeof(float) * size_t(dw_cols) * size_t(q.hq));
+  return fwd > bwd ? fwd : bwd;
+}
+
 namespace {
 
 // Planes of the rows of H listed in `list` (all of them without one) and of

@@ -1615,6 +1615,26 @@ int64_t distill_rows(int64_t N) { return N <= kFewRows ? 2 * kFewRows : extra_ro
 size_t tc_distill_bwd_bytes(int64_t N, int32_t h, int32_t V) {
   return recompute_bytes(bwd_plan(distill_rows(N), h, V, true), h, V, N <= kExtraMost);
 }
+// At least tc_distill_bwd_bytes of any call of up to N rows, and never less for more rows:
+// each array at the most that those calls give it.
+size_t tc_distill_bwd_most(int64_t N, int32_t h, int32_t V) {
+  int64_t R = distill_rows(N);
+  for (const int64_t n : {int64_t(kFewRows), kExtraMost})
+    if (N > n && distill_rows(n) > R) R = distill_rows(n);
+  const int64_t vpad = (int64_t(V) + BN - 1) / BN * BN, nN = (int64_t(h) + BN - 1) / BN;
+  const auto chunked = [&](int64_t rows) { return double(rows) * double(vpad) * 2.0 > double(dz_budget()); };
+  const int any = V / 512 < 1 ? 1 : V / 512 < kMostDhParts ? V / 512 : kMostDhParts;  // parts over whatever chunk
+  const int64_t f32_most = distill_rows(kExtraMost);
+  int64_t dh_rows = R <= f32_most || chunked(R) ? R : f32_most;
+  for (int64_t m = 1; (m - 1) * BM < R && may_split(m * nN); ++m) {
+    const int64_t rows = m * BM < R ? m * BM : R, parts = (chunked(rows) ? any : dh_splits(rows, h, V)) * rows;
+    dh_rows = parts > dh_rows ? parts : dh_rows;
+  }
+  const size_t all = size_t(R) * size_t(vpad) * 2, least = size_t(R) * BN * 2,
+               bound = dz_budget() > least ? dz_budget() : least;
+  return compact_ws_bytes(R, h) + round256(all < bound ? all : bound) +
+         round256(size_t(dh_rows) * size_t(h) * sizeof(float));
+}
 sao_status tc_distill_bwd(const void *H, const void *W, const TopGrad &t, int64_t N, int32_t h, int32_t V, void *dH,
                           void *dW, sao_dtype dw_dt, int accumulate, unsigned int *err, Carver &c, cudaStream_t s) {
   const DwOut out = dw_dt == SAO_BF16 ? DwOut{nullptr, static_cast<__nv_bfloat16 *>(dW)}

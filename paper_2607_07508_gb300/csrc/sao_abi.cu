@@ -483,7 +483,7 @@ static sao_status check_distill(sao_dtype dt, sao_dtype top_dt, int64_t N, int32
 
 size_t sao_distill_workspace_bytes(int64_t N, int32_t h, int32_t V, int32_t K, sao_dtype dt) {
   if (N < 0 || h < 1 || V < 1 || K < 1 || K > SAO_DISTILL_MAX_K || bad_dtype(dt)) return 0;
-  return kWsHeader + distill_ws_bytes(N, h, V, K, dt);
+  return kWsHeader + distill_ws_most(N, h, V, K, dt);
 }
 
 sao_status sao_distill_loss_fwd(const void *H, const void *W, sao_dtype dt, const int32_t *top_ids,
