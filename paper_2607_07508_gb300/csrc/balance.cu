@@ -834,11 +834,13 @@ int block_of(int most, int chunk, int lanes, bool segments) {
 }
 constexpr size_t kPlainSmem = 40u << 10;  // dynamic shared memory that any kernel may have
 
-// Small batches by one cluster, in one launch (another one is 2 us of the host's time, and
-// with the reduction's own latency 2 to 4 of the GPU's). Forward on the GPU alone, us,
-// cluster / two launches: 256 x 60 4.9 / 8.6, 1,024 x 128 8.4 / 8.8, 4,096 x 8 8.3 / 6.4,
-// 4,096 x 60 10.7 / 8.0; a forward and backward of 2,304 x 8, bound by the host, 14.3 / 16.6.
-bool one_cluster(int64_t N, int32_t E) { return N <= 4096 && N * E <= (1 << 17); }
+// Small batches by one cluster, in one launch: up to 512 rows, and on to 3,072 while the rows, at the
+// cost of 16 columns and their own, are few. Chosen for the GPU alone, as in a captured graph (us, fp32,
+// cluster / two launches): 512 x 60 5.3 / 6.9, 512 x 256 8.2 / 8.6, 512 x 1,024 13.3 / 14.2, 640 x 1,024
+// 14.6 / 14.2; 3,072 x 8 7.3 / 7.5, 4,096 x 8 8.4 / 8.0; 1,536 x 32 6.8 / 6.7, 2,048 x 32 8.1 / 6.9;
+// 1,024 x 60 7.0 / 7.1, 4,096 x 60 10.6 / 7.6; 1,024 x 128 8.2 / 7.5. Called one by one, where another launch is
+// 2 us of the host's time, it wins there too (2,304 x 8 7.5 / 9.2), and somewhat beyond (1,024 x 128 8.8 / 9.3).
+bool one_cluster(int64_t N, int32_t E) { return N <= 512 || (N <= 3072 && N * (E + 16) <= 72 << 10); }
 
 // Lets the kernel have an SM's shared memory (once per device).
 template <auto kKernel>
