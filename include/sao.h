@@ -452,7 +452,8 @@ SAO_API sao_status sao_value_loss(const float *values, const float *ret, const u
  * (-inf, and rho = 0, where the entries are the whole vocabulary). The p_k are taken
  * as they are: where they add up to more than 1 (entries rounded to bf16 against the
  * log-sum-exp of the exact logits), or are the whole vocabulary's and do not add up to
- * 1, the loss is least, though not 0, at q_k in proportion to p_k. Not scaled by T^2. The [N, V] logits are never stored.
+ * 1, the loss is least, though not 0, at q_k in proportion to p_k. Not scaled by
+ * T^2. The [N, V] logits are never stored.
  *   H [N, h], W [V, h] dt      top_ids [N, K] int32 in any order, each below V and
  *                              at most once a row
  *   top_logits [N, K] top_dt   teacher_lse [N] fp32 or NULL

@@ -161,15 +161,17 @@ __device__ __forceinline__ void copy_async(uint32_t dst, const void *src) {
 // The rows first, first + step, ... that a group of lanes goes through, those ahead
 // already on their way into slots of the thread's own (no barrier). The words of rows that
 // are not counted are anything (but for the first few rows they are not read), and
-// columns past E read as -inf: they have no score. What a row needs is asked for kDepth rows before, its expert ids too, and
-// the mask 32 rows at a time: with one row ahead, or a byte of the mask read per row, the
-// kernels waited for memory half of their time (2^20 x 160 bf16 forward 93-128 us).
+// columns past E read as -inf: they have no score. What a row needs is asked for kDepth rows
+// before, its expert ids too, and the mask 32 rows at a time: with one row ahead, or a byte of the
+// mask read per row, the kernels waited for memory half of their time (2^20 x 160 bf16 forward
+// 93-128 us).
 template <class T, int kVec, int kC>
 struct Stream {
   static constexpr bool kSlots = kAsync<kVec>;
   static constexpr int kDepth = kDepthOf<T, kVec, kC>, kLoads = kC / kVec;
   static constexpr int kBytes = kVec * int(sizeof(T));
-  __device__ __forceinline__ uint32_t pitch() const { return blockDim.x * uint32_t(kBytes); }  // from a load's slots to the next one's
+  // from a load's slots to the next one's
+  __device__ __forceinline__ uint32_t pitch() const { return blockDim.x * uint32_t(kBytes); }
   const T *src;         // this lane's first column of the row kDepth steps ahead
   const int32_t *ids;   // this lane's first id of that row, or null
   const uint8_t *mask;  // of the warp's first row 64 steps after the last refill, or null
@@ -227,8 +229,8 @@ struct Stream {
     }
   }
   // `lane_ids`: expert ids [N, k], or null.
-  __device__ __forceinline__ Stream(const BalanceArgs &a, const Rows &rows, int lane, int group, const int32_t *lane_ids,
-                                    const void *ring, const void *id_ring)
+  __device__ __forceinline__ Stream(const BalanceArgs &a, const Rows &rows, int lane, int group,
+                                    const int32_t *lane_ids, const void *ring, const void *id_ring)
       : left(int(rows.end > rows.first ? rows.end - rows.first : 0)), step(rows.step), k(a.k), l(lane),
         lanes(group), loads((a.E / kVec - lane + group - 1) / group) {
     const int64_t warp_first = rows.first, first = warp_first + (threadIdx.x & 31) / group;
@@ -477,7 +479,7 @@ __device__ __forceinline__ void cluster_finish(const BalanceArgs &a, const Balan
 
 // Each group of `lanes` lanes takes a row at a time, the next ones' logits in flight, and
 // keeps the sums of its columns in registers. One pass over the logits. 2^20 x 160 bf16:
-// (a quarter masked) 94 us, 3.0 TB/s, bound by instructions (2.9 a cycle and SM);
+// (a quarter masked) 94 us, 3.0 TB/s, bound by instructions (2.7 a cycle and SM);
 // 2^20 x 128 fp32: 92 us, 5.8 TB/s.
 template <class T, int kVec, int kC, bool kSigmoid>
 __global__ void __launch_bounds__(kThreads<T, kVec, kC>)
@@ -567,9 +569,10 @@ __global__ void __launch_bounds__(kThreads<T, kVec, kC>)
 
 // CTA (b, 32 columns): adds the segment's partials, kSlices warps side by side; the
 // CTAs of a batch of up to 256 experts are one cluster, whose first CTA adds their products
-// (2 us less than by the ticket); else the last CTA adds those of all. Bound by latency: a batch's 152 partials are
-// asked for at once (in three rounds a forward of 65,536 x 128 was 1 us longer). (The sums are of positive numbers, in a fixed order, in fp32; fp64, on which
-// GB300 has few units, took longer than the loads.)
+// (2 us less than by the ticket); else the last CTA adds those of all. Bound by latency: a batch's
+// 152 partials are asked for at once (in three rounds a forward of 65,536 x 128 was 1 us longer). (The
+// sums are of positive numbers, in a fixed order, in fp32; fp64, on which GB300 has few units,
+// took longer than the loads.)
 template <int kSlices>
 __global__ void __launch_bounds__(32 * kSlices)
     balance_reduce_kernel(const BalanceArgs a, int cols, bool cluster, const float *psum, const int *pcount,

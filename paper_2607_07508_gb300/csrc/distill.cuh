@@ -55,6 +55,10 @@ constexpr int kFewRows = 64;
 // error of dH and dW is that of a few of them, and a rounding is 1 to 3 times its mean. Against the error
 // of rounding the outputs alone, 130 to 1,500 rows with one entry: 1.3 to 1.4 times on average, up to
 // 2.0; with 32 such rows 1.0 to 1.1, up to 1.2; with five entries 1.4 and 1.7, 1.1 and 1.4.
+// What that costs a backward of the moe head (us, with / without; one entry a row, error of an fp32 dW):
+// where the padding to 128 rows has room 96 rows 470 / 446 (0.0007 / 0.0014), 224 524 / 508, 480 785 / 766;
+// where it opens a tile 128 509 / 457 (0.0009 / 0.0016), 256 606 / 515 (0.0013 / 0.0017), 512 933 / 773
+// (0.0014 / 0.0017); 1,024 1,390 / 1,396 (0.0016 / 0.0017), 4,096 5,010 / 4,970 (0.0016 both).
 constexpr int kExtraRows = 32;
 constexpr int64_t kExtraMost = 8192;
 inline bool extra_rows(int64_t N) { return N > kFewRows && N <= kExtraMost; }

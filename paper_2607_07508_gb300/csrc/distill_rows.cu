@@ -428,8 +428,8 @@ void launch_fwd(const void *H, const void *W, const uint8_t *row_mask, int64_t N
                 const TopRef &top, float2 *part, cudaStream_t s, S with_sizes) {
   const GemvArgs<T> a{static_cast<const T *>(H), static_cast<const T *>(W), V, int(N), h, range_of(V)};
   with_sizes([&](auto nv, auto n, auto r) {
-    pdl(distill_gemv_fwd_kernel<T, kVec, nv.value, n.value, r.value>, unsigned(grid_of(V)), kBlock, 0, s)(a, top, row_mask,
-                                                                                                   part);
+    pdl(distill_gemv_fwd_kernel<T, kVec, nv.value, n.value, r.value>, unsigned(grid_of(V)), kBlock, 0, s)(
+        a, top, row_mask, part);
   });
 }
 template <class T, bool kVec, class TW, class S>

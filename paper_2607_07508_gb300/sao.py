@@ -430,7 +430,7 @@ def sao_distill_workspace_bytes(N: int, h: int, V: int, K: int, dtype=torch.bflo
 
 
 def distill_workspace(N: int, h: int, V: int, K: int, dtype=torch.bfloat16, device=None) -> torch.Tensor:
-    """Allocate the workspace of sao_distill_loss_fwd/bwd."""
+    """Allocate the workspace of sao_distill_loss_fwd/bwd for up to N rows."""
     n = sao_distill_workspace_bytes(N, h, V, K, dtype)
     return torch.empty(max(n, 256), dtype=torch.uint8, device=device or "cuda")
 

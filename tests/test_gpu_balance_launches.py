@@ -11,8 +11,8 @@ pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
 
 
-@pytest.mark.parametrize("N,E,one", [(1, 1, True), (512, 8, True), (512, 1000, True), (513, 1024, False), (3072, 8, True),
-                                     (3073, 1, False), (3073, 8, False), (4096, 8, False), (1536, 32, True),
+@pytest.mark.parametrize("N,E,one", [(1, 1, True), (512, 8, True), (512, 1000, True), (513, 1024, False),
+                                     (3072, 8, True), (3073, 1, False), (3073, 8, False), (4096, 8, False), (1536, 32, True),
                                      (1537, 32, False), (512, 128, True), (513, 128, False), (1024, 128, False)])
 def test_one_cluster_where_it_is_the_faster_form(N, E, one):
     g = torch.Generator().manual_seed(N + E)

@@ -1,12 +1,13 @@
 """How many roundings to bf16 the gradients of 65 and more rows of a bf16 head lose.
 
 dZ is rounded to bf16 once, and a bf16 output once more. A rounding moves an element of significand m in [1, 2) by
-e uniform in +-2^-8 / m, which is sqrt(log2(e) 3 / 8 / 3) 2^-8 = 0.425 2^-8 = 0.00166 of it in the mean square (significands
-spread evenly over their logarithm), so independent roundings leave r = 0.00166 of an fp32 dW and sqrt(2) r = 0.00235 of a
-bf16 output. With n terms of like weight the mean square scatters by 0.9 / sqrt(n) (a squared uniform's spread): 700 entries
-and more make that 3.4 % of the square, 1.7 % of the norm; the weights, which are not alike, double it. Five of that, and
-5 % for the logits' truncation and what the rest of the vocabulary adds: 1.22 r, 1.22 sqrt(2) r. Where a row has one entry,
-the 32 rows that lose most have second pieces, so the others' largest losses are cut: no more than that either."""
+e uniform in +-2^-8 / m, which is sqrt(log2(e) 3 / 8 / 3) 2^-8 = 0.425 2^-8 = 0.00166 of it in the mean square
+(significands spread evenly over their logarithm), so independent roundings leave r = 0.00166 of an fp32 dW and
+sqrt(2) r = 0.00235 of a bf16 output. With n terms of like weight the mean square scatters by 0.9 / sqrt(n) (a
+squared uniform's spread): 700 entries and more make that 3.4 % of the square, 1.7 % of the norm; the weights, which
+are not alike, double it. Five of that, and 5 % for the logits' truncation and what the rest of the vocabulary adds:
+1.22 r, 1.22 sqrt(2) r. Where a row has one entry, the 32 rows that lose most have second pieces, so the others'
+largest losses are cut: no more than that either."""
 import numpy as np
 import pytest
 import torch

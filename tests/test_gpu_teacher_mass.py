@@ -1,10 +1,10 @@
 """Distillation where a teacher's probabilities do not add up to 1 (bf16 logits against the exact log-sum-exp; the
 whole vocabulary against another one), against the differentiated definition in fp64.
 
-Bounds: of gradients as in test_gpu_distill.py, relative to dZ's largest cancellation. dz = m q - p, so an error of e
-of q or p is one of e (m q + p) of dz: for a student that is far from its teacher as there (2^-7 with a bf16 head, dZ and
-the outputs rounded; 1e-5 fp32). At the best student dz is 0 and what is left is e (m q + p) = 2 e p: exponents of up
-to 25 off by 2^-24 of themselves, exponentials and log-sum-exps by as much, sums of 20, 64 u in all."""
+Bounds: dz = m q - p, so an error of e of q or p is one of e (m q + p) of dz. For a student that is far from its
+teacher, of gradients as in test_gpu_distill.py (2^-7 with a bf16 head, dZ and the outputs rounded; 1e-5 fp32). At the
+best student dz is 0 and what is left is e (m q + p) = 2 e p: exponents of up to 25 off by 2^-24 of themselves,
+exponentials and log-sum-exps by as much, sums of 20, 64 u in all."""
 import numpy as np
 import pytest
 import torch
