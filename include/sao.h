@@ -18,6 +18,8 @@
  *   - sao_distill_loss_fwd/bwd   : distillation from a teacher's top logits
  *     over the LM head;
  *   - sao_balance_loss_fwd/bwd   : load balance of a mixture of experts.
+ * And what stands directly around the losses in that step:
+ *   - sao_grad_sumsq, sao_grad_clip : the global norm of all gradients, clipping.
  *
  * Conventions shared by every entry point:
  *   - Every array argument is a DEVICE pointer owned by the caller; the
@@ -559,6 +561,37 @@ SAO_API sao_status sao_balance_loss_bwd(const void *logits, sao_dtype dt, const 
                                         int score, const int64_t *counts, const int64_t *rows,
                                         const float *grad_loss, void *grad_logits, void *ws, size_t ws_bytes,
                                         sao_stream_t stream);
+
+/* One tensor of a list on the host: n contiguous elements of device memory, aligned to
+ * their size (vectorised paths: 16 bytes). data may be NULL if n is 0. */
+typedef struct sao_tensor {
+  void *data;
+  int64_t n;
+  sao_dtype dt;
+} sao_tensor;
+
+/*
+ * Global norm of a step's gradients, in two calls so that data-parallel ranks with
+ * gradients of their own can add up the first one's result (the paper has no
+ * counterpart):
+ *   sumsq[0] = sum over the tensors' elements of g^2                  [1] fp64 output
+ *   norm[0] = sqrt(sumsq[0]), coef[0] = max_norm / norm where norm > max_norm, else 1
+ *   out[i] = coef grads[i], with the fp32 coef, rounded to out's type   norm, coef [1] fp32
+ * out NULL: in place, and nothing is read or written where coef is 1. Otherwise out[i]
+ * has the elements of grads[i], of either type, and is grads[i] itself or overlaps none of the
+ * tensors. Where sumsq is not finite (or negative) coef is NaN and the gradients are passed on
+ * as they are: the step is to be dropped. (A norm past fp32's range reads +inf, with its coef.)
+ * The lists are read before the calls return; they hold no tensor twice, nor two that
+ * overlap. Sums are fp64 (each of 32 or 64 squares fp32 where those are in its range), in a
+ * fixed order. max_norm > 0; +inf: only the norm.
+ * Workspace: sao_grad_workspace_bytes(), whatever the lists.
+ */
+SAO_API size_t sao_grad_workspace_bytes(void);
+SAO_API sao_status sao_grad_sumsq(const sao_tensor *grads, int32_t count, double *sumsq, void *ws, size_t ws_bytes,
+                                  sao_stream_t stream);
+SAO_API sao_status sao_grad_clip(const sao_tensor *grads, const sao_tensor *out, int32_t count, const double *sumsq,
+                                 float max_norm, float *norm, float *coef, void *ws, size_t ws_bytes,
+                                 sao_stream_t stream);
 
 /*
  * Kernel timing for profiling. When enabled, every kernel the library

@@ -9,6 +9,7 @@
 
 #include "balance.cuh"
 #include "distill.cuh"
+#include "grads.cuh"
 #include "logprobs_common.cuh"
 #include "sao_common.cuh"
 #include "sao_internal.h"
@@ -600,6 +601,61 @@ sao_status sao_balance_loss_bwd(const void *logits, sao_dtype dt, const uint8_t 
   SAO_TRY(begin_call(ws, s));
   SAO_TRY(balance_bwd_launch(logits, dt, row_mask, cu_seqlens, cu_seqlens ? B : 1, N, E, k, score, counts, rows,
                              grad_loss, grad_logits, w.err, s));
+  return finish_call(ws, s);
+}
+
+static sao_status check_tensors(const sao_tensor *t, int32_t count, const char *what) {
+  for (int32_t i = 0; i < count; ++i) {
+    if (bad_dtype(t[i].dt)) return fail(SAO_ERR_UNSUPPORTED, "%s[%d]: unknown dtype %d", what, i, int(t[i].dt));
+    if (t[i].n < 0 || t[i].n >= (int64_t(1) << 48))
+      return fail(SAO_ERR_SHAPE, "%s[%d]: %lld elements", what, i, (long long)t[i].n);
+    if (t[i].n > 0 && !t[i].data) return fail(SAO_ERR_INVALID_ARG, "%s[%d] is NULL", what, i);
+    if ((reinterpret_cast<uintptr_t>(t[i].data) & (t[i].dt == SAO_BF16 ? 1u : 3u)) != 0)
+      return fail(SAO_ERR_INVALID_ARG, "%s[%d] is not aligned to its elements", what, i);
+  }
+  return SAO_OK;
+}
+
+static sao_status check_lists(const sao_tensor *grads, const sao_tensor *out, int32_t count) {
+  if (count < 0) return fail(SAO_ERR_SHAPE, "count = %d", count);
+  if (count > 0 && !grads) return fail(SAO_ERR_INVALID_ARG, "NULL list");
+  SAO_TRY(check_tensors(grads, count, "grads"));
+  if (out) {
+    SAO_TRY(check_tensors(out, count, "out"));
+    for (int32_t i = 0; i < count; ++i)
+      if (out[i].n != grads[i].n)
+        return fail(SAO_ERR_SHAPE, "out[%d] has %lld elements, grads[%d] %lld", i, (long long)out[i].n, i,
+                    (long long)grads[i].n);
+  }
+  return check_disjoint(grads, out, count);
+}
+
+size_t sao_grad_workspace_bytes(void) { return kWsHeader + grad_ws_bytes(); }
+
+sao_status sao_grad_sumsq(const sao_tensor *grads, int32_t count, double *sumsq, void *ws, size_t ws_bytes,
+                          sao_stream_t stream) {
+  SAO_RANGE();
+  SAO_TRY(check_lists(grads, nullptr, count));
+  if (!sumsq) return fail(SAO_ERR_INVALID_ARG, "NULL sumsq");
+  Ws w;
+  SAO_TRY(take_ws(ws, ws_bytes, grad_ws_bytes(), &w));
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  SAO_TRY(begin_call(ws, s));
+  SAO_TRY(grad_sumsq_launch(grads, count, sumsq, w.body, w.body_bytes, s));
+  return finish_call(ws, s);
+}
+
+sao_status sao_grad_clip(const sao_tensor *grads, const sao_tensor *out, int32_t count, const double *sumsq,
+                         float max_norm, float *norm, float *coef, void *ws, size_t ws_bytes, sao_stream_t stream) {
+  SAO_RANGE();
+  SAO_TRY(check_lists(grads, out, count));
+  if (!(max_norm > 0.f)) return fail(SAO_ERR_INVALID_ARG, "max_norm must be positive (%g)", max_norm);
+  if (!sumsq || !norm || !coef) return fail(SAO_ERR_INVALID_ARG, "NULL sumsq, norm or coef");
+  Ws w;
+  SAO_TRY(take_ws(ws, ws_bytes, 0, &w));
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  SAO_TRY(begin_call(ws, s));
+  SAO_TRY(grad_clip_launch(grads, out, count, sumsq, max_norm, norm, coef, s));
   return finish_call(ws, s);
 }
 

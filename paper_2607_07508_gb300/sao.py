@@ -37,6 +37,7 @@ EXPORTS = ("sao_version", "sao_last_error_string", "sao_set_checked", "sao_get_c
            "sao_token_logprobs_bwd_cached",
            "sao_distill_workspace_bytes", "sao_distill_loss_fwd", "sao_distill_loss_bwd",
            "sao_balance_workspace_bytes", "sao_balance_loss_fwd", "sao_balance_loss_bwd",
+           "sao_grad_workspace_bytes", "sao_grad_sumsq", "sao_grad_clip",
            "sao_value_loss", "sao_profile_enable", "sao_profile_reset", "sao_profile_read")
 
 
@@ -101,6 +102,9 @@ def load(path: Optional[str] = None):
                                                 P, SZ, P]),
         "sao_balance_loss_bwd": (ctypes.c_int, [P, ctypes.c_int, P, P, I32, I64, I32, I32, ctypes.c_int, P, P, P, P, P,
                                                 SZ, P]),
+        "sao_grad_workspace_bytes": (SZ, []),
+        "sao_grad_sumsq": (ctypes.c_int, [P, I32, P, P, SZ, P]),
+        "sao_grad_clip": (ctypes.c_int, [P, P, I32, P, F, P, P, P, SZ, P]),
         "sao_profile_enable": (None, [ctypes.c_int]),
         "sao_profile_reset": (None, []),
         "sao_profile_read": (ctypes.c_int, [P, P, P, ctypes.c_int]),
@@ -508,6 +512,60 @@ def sao_balance_loss_bwd(logits, k, score, counts, rows, grad_loss, grad_logits,
                                        _arg(grad_loss, _F32, 1, "grad_loss"),
                                        _arg(grad_logits, logits.dtype, N * E, "grad_logits"), _ptr(ws), ws.numel(),
                                        _stream(stream)))
+
+
+class _Tensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("n", ctypes.c_int64), ("dt", ctypes.c_int)]
+
+
+class TensorList:
+    """Gradients, or their clipped copies, as the calls below take them: made once for tensors that stay where
+    they are, which it keeps alive."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        self.device = self.tensors[0].get_device() if self.tensors else None
+        for t in self.tensors:
+            if t.get_device() != self.device:
+                raise ValueError("the tensors of a list lie on one device")
+        self.array = (_Tensor * len(self.tensors))(*[(_ptr(t), t.numel(), _dtype_code(t)) for t in self.tensors])
+
+    def __len__(self):
+        return len(self.tensors)
+
+
+def _current(device) -> None:
+    if device is not None and device != _device():
+        raise ValueError(f"the tensors lie on device {device}, the current one is {_device()}")
+
+
+def sao_grad_workspace_bytes() -> int:
+    return int(load().sao_grad_workspace_bytes())
+
+
+def grad_workspace(device=None) -> torch.Tensor:
+    """Allocate the workspace of sao_grad_sumsq and sao_grad_clip, whatever their lists."""
+    return torch.empty(sao_grad_workspace_bytes(), dtype=torch.uint8, device=device or "cuda")
+
+
+def sao_grad_sumsq(grads, sumsq, ws, stream=None):
+    """grads: a TensorList, or tensors; sumsq fp64."""
+    grads = grads if isinstance(grads, TensorList) else TensorList(grads)
+    _current(grads.device)
+    _check(load().sao_grad_sumsq(grads.array, len(grads), _arg(sumsq, _F64, 1, "sumsq"), _ptr(ws), ws.numel(),
+                                 _stream(stream)))
+
+
+def sao_grad_clip(grads, sumsq, max_norm, norm, coef, ws, out=None, stream=None):
+    """grads, out: TensorLists, or tensors; out None: in place."""
+    grads = grads if isinstance(grads, TensorList) else TensorList(grads)
+    out = out if out is None or isinstance(out, TensorList) else TensorList(out)
+    if out is not None and (len(out) != len(grads) or out.device != grads.device):
+        raise ValueError("out must have a tensor for each of grads, on their device")
+    _current(grads.device)
+    _check(load().sao_grad_clip(grads.array, None if out is None else out.array, len(grads),
+                                _arg(sumsq, _F64, 1, "sumsq"), float(max_norm), _arg(norm, _F32, 1, "norm"),
+                                _arg(coef, _F32, 1, "coef"), _ptr(ws), ws.numel(), _stream(stream)))
 
 
 # ---------------------------------------------------------------------------
