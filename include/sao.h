@@ -19,6 +19,8 @@
  *     over the LM head;
  *   - sao_balance_loss_fwd/bwd   : load balance of a mixture of experts.
  * And what stands directly around the losses in that step:
+ *   - sao_rms_norm_fwd/bwd       : the root-mean-square norm in front of the LM
+ *     head, of the residual stream's sum, in 8 bits too;
  *   - sao_grad_sumsq, sao_grad_clip : the global norm of all gradients, clipping.
  *
  * Conventions shared by every entry point:
@@ -561,6 +563,53 @@ SAO_API sao_status sao_balance_loss_bwd(const void *logits, sao_dtype dt, const 
                                         int score, const int64_t *counts, const int64_t *rows,
                                         const float *grad_loss, void *grad_logits, void *ws, size_t ws_bytes,
                                         sao_stream_t stream);
+
+/* Widest rows of sao_rms_norm_fwd/bwd. */
+#define SAO_NORM_MAX_H 16384
+
+/* What shares a scale in the 8-bit rows of sao_rms_norm_fwd. */
+#define SAO_SCALE_NONE 0     /* no 8-bit rows */
+#define SAO_SCALE_ROW 1      /* a row: scales [N] fp32 */
+#define SAO_SCALE_BLOCK128 2 /* 128 columns: scales [N, ceil(h / 128)] fp32 */
+#define SAO_SCALE_MX32 3     /* 32 columns: scales [N, ceil(h / 32)] uint8, 2^(scale - 127) */
+
+/*
+ * Root-mean-square norm, of the sum with a residual stream if there is one (in front
+ * of the LM head: H = y; the paper has no counterpart):
+ *   sum[t, c] = x + residual, rounded to dt; without a residual it is x
+ *   rstd[t] = (mean_c sum[t, c]^2 + eps)^-1/2,   y[t, c] = sum[t, c] rstd[t] weight[c]
+ * and in 8 bits y8 = e4m3(y (1 / scale)), y before its rounding to dt, to the nearest (ties
+ * to even), with scale = max(amax / 448, 2^-126) of the row or the block, or the least power
+ * of two 2^b >= amax / 448, -127 <= b. A NaN in y makes its scale NaN.
+ *   x, residual, sum, y [N, h] dt     weight [h] w_dt     rstd [N] fp32
+ *   y8 [N, h] uint8 (e4m3)            scales as `scaling` says
+ * residual and sum are both given or both NULL; rstd and one of y and y8 may be NULL;
+ * y8 and scales with scaling != SAO_SCALE_NONE only. sum may be x or residual; the
+ * other outputs overlap nothing. Squares are summed in fp32: |sum| up to 2^56.
+ * 1 <= h <= SAO_NORM_MAX_H; eps >= 0 and finite. The forward's workspace: the error word's 256
+ * bytes; the backward's: sao_norm_workspace_bytes(N, h), which never falls as one of
+ * them grows.
+ */
+SAO_API size_t sao_norm_workspace_bytes(int64_t N, int32_t h);
+SAO_API sao_status sao_rms_norm_fwd(const void *x, const void *residual, sao_dtype dt, const void *weight,
+                                    sao_dtype w_dt, float eps, int64_t N, int32_t h, void *sum, void *y, float *rstd,
+                                    uint8_t *y8, void *scales, int scaling, void *ws, size_t ws_bytes,
+                                    sao_stream_t stream);
+
+/*
+ * Gradients of the norm, given those of y and, past the norm, of sum:
+ *   dx = dsum + rstd (weight dy - sum rstd^2 mean_c(weight dy sum))   (x's and residual's)
+ *   dweight = sum_t dy sum rstd
+ *   sum [N, h] dt, rstd [N]   the forward's (sum: x without a residual)
+ *   dy, dsum [N, h] dt        dsum may be NULL (nothing behind the norm)
+ *   dx [N, h] dt              may be dy or dsum
+ *   dweight [h] fp32          overwritten or (accumulate != 0) added to; or NULL
+ * Deterministic.
+ */
+SAO_API sao_status sao_rms_norm_bwd(const void *sum, sao_dtype dt, const void *weight, sao_dtype w_dt,
+                                    const float *rstd, const void *dy, const void *dsum, int64_t N, int32_t h,
+                                    void *dx, float *dweight, int accumulate, void *ws, size_t ws_bytes,
+                                    sao_stream_t stream);
 
 /* One tensor of a list on the host: n contiguous elements of device memory, aligned to
  * their size (vectorised paths: 16 bytes). data may be NULL if n is 0. */

@@ -1,0 +1,38 @@
+// Root-mean-square norm (norm.cu), for the C entry points.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/sao.h"
+
+namespace sao {
+
+struct NormFwd {
+  const void *x, *residual;  // residual, sum: or null
+  const void *weight;
+  void *sum, *y;             // y: or null
+  float *rstd;               // or null
+  uint8_t *y8;               // or null
+  void *scales;
+  int scaling;
+  float eps;
+  int64_t N;
+  int h;
+};
+struct NormBwd {
+  const void *x, *weight;
+  const float *rstd;
+  const void *dy, *dsum;     // dsum: or null
+  void *dx;
+  float *dweight;            // or null
+  int accumulate;
+  int64_t N;
+  int h;
+};
+
+size_t norm_ws_bytes(int64_t N, int32_t h);
+sao_status norm_fwd_launch(const NormFwd &a, sao_dtype dt, sao_dtype w_dt, cudaStream_t s);
+sao_status norm_bwd_launch(const NormBwd &a, sao_dtype dt, sao_dtype w_dt, void *ws, size_t ws_bytes, cudaStream_t s);
+
+}  // namespace sao

@@ -11,6 +11,7 @@
 #include "distill.cuh"
 #include "grads.cuh"
 #include "logprobs_common.cuh"
+#include "norm.cuh"
 #include "sao_common.cuh"
 #include "sao_internal.h"
 
@@ -601,6 +602,72 @@ sao_status sao_balance_loss_bwd(const void *logits, sao_dtype dt, const uint8_t 
   SAO_TRY(begin_call(ws, s));
   SAO_TRY(balance_bwd_launch(logits, dt, row_mask, cu_seqlens, cu_seqlens ? B : 1, N, E, k, score, counts, rows,
                              grad_loss, grad_logits, w.err, s));
+  return finish_call(ws, s);
+}
+
+static sao_status check_norm(sao_dtype dt, sao_dtype w_dt, int64_t N, int32_t h) {
+  if (bad_dtype(dt) || bad_dtype(w_dt)) return fail(SAO_ERR_UNSUPPORTED, "unknown dtype %d or %d", int(dt), int(w_dt));
+  if (N < 0 || N >= (int64_t(1) << 31)) return fail(SAO_ERR_SHAPE, "N = %lld out of range", (long long)N);
+  if (h < 1 || h > SAO_NORM_MAX_H) return fail(SAO_ERR_SHAPE, "h = %d: 1 <= h <= %d", h, SAO_NORM_MAX_H);
+  return SAO_OK;
+}
+
+size_t sao_norm_workspace_bytes(int64_t N, int32_t h) {
+  if (N < 0 || h < 1 || h > SAO_NORM_MAX_H) return 0;
+  return kWsHeader + norm_ws_bytes(N, h);
+}
+
+sao_status sao_rms_norm_fwd(const void *x, const void *residual, sao_dtype dt, const void *weight, sao_dtype w_dt,
+                            float eps, int64_t N, int32_t h, void *sum, void *y, float *rstd, uint8_t *y8,
+                            void *scales, int scaling, void *ws, size_t ws_bytes, sao_stream_t stream) {
+  SAO_RANGE();
+  SAO_TRY(check_norm(dt, w_dt, N, h));
+  if (!(eps >= 0.f) || isinf(eps)) return fail(SAO_ERR_INVALID_ARG, "eps must be finite and not negative (%g)", eps);
+  if (scaling < SAO_SCALE_NONE || scaling > SAO_SCALE_MX32)
+    return fail(SAO_ERR_INVALID_ARG, "unknown scaling %d", scaling);
+  if (N == 0) return SAO_OK;
+  if (!x || !weight || (!y && !y8)) return fail(SAO_ERR_INVALID_ARG, "NULL x, weight, or neither y nor y8");
+  if (!residual != !sum) return fail(SAO_ERR_INVALID_ARG, "residual and sum are given together or not at all");
+  if (!y8 != !scales || !y8 != (scaling == SAO_SCALE_NONE))
+    return fail(SAO_ERR_INVALID_ARG, "y8, scales and a scaling are given together or not at all");
+  const uintptr_t unit = dt == SAO_BF16 ? 1 : 3, w_unit = w_dt == SAO_BF16 ? 1 : 3;
+  for (const void *p : {x, residual, static_cast<const void *>(sum), static_cast<const void *>(y)})
+    if ((reinterpret_cast<uintptr_t>(p) & unit) != 0)
+      return fail(SAO_ERR_INVALID_ARG, "an array is not aligned to its elements");
+  if ((reinterpret_cast<uintptr_t>(weight) & w_unit) != 0 || (reinterpret_cast<uintptr_t>(rstd) & 3u) != 0 ||
+      (scaling != SAO_SCALE_MX32 && (reinterpret_cast<uintptr_t>(scales) & 3u) != 0))
+    return fail(SAO_ERR_INVALID_ARG, "an array is not aligned to its elements");
+  Ws w;
+  SAO_TRY(take_ws(ws, ws_bytes, 0, &w));
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  SAO_TRY(begin_call(ws, s));
+  SAO_TRY(norm_fwd_launch({x, residual, weight, sum, y, rstd, y8, scales, scaling, eps, N, h}, dt, w_dt, s));
+  return finish_call(ws, s);
+}
+
+sao_status sao_rms_norm_bwd(const void *sum, sao_dtype dt, const void *weight, sao_dtype w_dt, const float *rstd,
+                            const void *dy, const void *dsum, int64_t N, int32_t h, void *dx, float *dweight,
+                            int accumulate, void *ws, size_t ws_bytes, sao_stream_t stream) {
+  SAO_RANGE();
+  SAO_TRY(check_norm(dt, w_dt, N, h));
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  if (N == 0) {
+    if (dweight && !accumulate) SAO_CUDA_TRY(cudaMemsetAsync(dweight, 0, sizeof(float) * size_t(h), s));
+    return SAO_OK;
+  }
+  if (!sum || !weight || !rstd || !dy || !dx) return fail(SAO_ERR_INVALID_ARG, "NULL array argument");
+  const uintptr_t unit = dt == SAO_BF16 ? 1 : 3, w_unit = w_dt == SAO_BF16 ? 1 : 3;
+  for (const void *p : {sum, dy, dsum, static_cast<const void *>(dx)})
+    if ((reinterpret_cast<uintptr_t>(p) & unit) != 0)
+      return fail(SAO_ERR_INVALID_ARG, "an array is not aligned to its elements");
+  if ((reinterpret_cast<uintptr_t>(weight) & w_unit) != 0 || (reinterpret_cast<uintptr_t>(rstd) & 3u) != 0 ||
+      (reinterpret_cast<uintptr_t>(dweight) & 3u) != 0)
+    return fail(SAO_ERR_INVALID_ARG, "an array is not aligned to its elements");
+  Ws w;
+  SAO_TRY(take_ws(ws, ws_bytes, dweight ? norm_ws_bytes(N, h) : 0, &w));
+  SAO_TRY(begin_call(ws, s));
+  SAO_TRY(norm_bwd_launch({sum, weight, rstd, dy, dsum, dx, dweight, accumulate, N, h}, dt, w_dt, w.body,
+                          w.body_bytes, s));
   return finish_call(ws, s);
 }
 

@@ -21,6 +21,8 @@ SAO_F32, SAO_BF16 = 0, 1
 SAO_STEP_AVERAGE, SAO_STEP_LAST = 0, 1
 SAO_NORM_TOKEN, SAO_NORM_SEQUENCE = 0, 1
 SAO_SCORE_SOFTMAX, SAO_SCORE_SIGMOID = 0, 1
+SAO_SCALE_NONE, SAO_SCALE_ROW, SAO_SCALE_BLOCK128, SAO_SCALE_MX32 = 0, 1, 2, 3
+SAO_NORM_MAX_H = 16384
 SAO_DISTILL_MAX_K, SAO_BALANCE_MAX_EXPERTS = 1024, 1024
 STATUS = {0: "SAO_OK", 1: "SAO_ERR_INVALID_ARG", 2: "SAO_ERR_SHAPE", 3: "SAO_ERR_WORKSPACE",
           4: "SAO_ERR_UNSUPPORTED", 5: "SAO_ERR_CUDA", 6: "SAO_ERR_DEVICE_CHECK"}
@@ -37,6 +39,7 @@ EXPORTS = ("sao_version", "sao_last_error_string", "sao_set_checked", "sao_get_c
            "sao_token_logprobs_bwd_cached",
            "sao_distill_workspace_bytes", "sao_distill_loss_fwd", "sao_distill_loss_bwd",
            "sao_balance_workspace_bytes", "sao_balance_loss_fwd", "sao_balance_loss_bwd",
+           "sao_norm_workspace_bytes", "sao_rms_norm_fwd", "sao_rms_norm_bwd",
            "sao_grad_workspace_bytes", "sao_grad_sumsq", "sao_grad_clip",
            "sao_value_loss", "sao_profile_enable", "sao_profile_reset", "sao_profile_read")
 
@@ -102,6 +105,11 @@ def load(path: Optional[str] = None):
                                                 P, SZ, P]),
         "sao_balance_loss_bwd": (ctypes.c_int, [P, ctypes.c_int, P, P, I32, I64, I32, I32, ctypes.c_int, P, P, P, P, P,
                                                 SZ, P]),
+        "sao_norm_workspace_bytes": (SZ, [I64, I32]),
+        "sao_rms_norm_fwd": (ctypes.c_int, [P, P, ctypes.c_int, P, ctypes.c_int, F, I64, I32, P, P, P, P, P,
+                                            ctypes.c_int, P, SZ, P]),
+        "sao_rms_norm_bwd": (ctypes.c_int, [P, ctypes.c_int, P, ctypes.c_int, P, P, P, I64, I32, P, P, ctypes.c_int, P,
+                                            SZ, P]),
         "sao_grad_workspace_bytes": (SZ, []),
         "sao_grad_sumsq": (ctypes.c_int, [P, I32, P, P, SZ, P]),
         "sao_grad_clip": (ctypes.c_int, [P, P, I32, P, F, P, P, P, SZ, P]),
@@ -176,6 +184,7 @@ def _dtype_code(t: torch.Tensor) -> int:
 
 _F32, _F64, _BF16 = torch.float32, torch.float64, torch.bfloat16
 _U8, _I32, _I64 = torch.uint8, torch.int32, torch.int64
+_E4M3, _E8M0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
 
 
 # ---------------------------------------------------------------------------
@@ -514,6 +523,74 @@ def sao_balance_loss_bwd(logits, k, score, counts, rows, grad_loss, grad_logits,
                                        _stream(stream)))
 
 
+def _current(device) -> None:
+    if device is not None and device != _device():
+        raise ValueError(f"the tensors lie on device {device}, the current one is {_device()}")
+
+
+def sao_norm_workspace_bytes(N: int, h: int) -> int:
+    return int(load().sao_norm_workspace_bytes(int(N), int(h)))
+
+
+def norm_workspace(N: int, h: int, device=None) -> torch.Tensor:
+    """Allocate the workspace of sao_rms_norm_fwd/bwd for up to N rows of up to h columns."""
+    return torch.empty(max(sao_norm_workspace_bytes(N, h), 256), dtype=torch.uint8, device=device or "cuda")
+
+
+_SCALINGS = {"none": (0, 0, None), "row": (1, 0, _F32), "block": (2, 128, _F32), "mx": (3, 32, _E8M0)}
+
+
+def _scales(scaling, h):
+    """(code, scales to a row, their type) of a scaling's name."""
+    if scaling not in _SCALINGS:
+        raise ValueError(f"scaling is one of {', '.join(_SCALINGS)}, got {scaling!r}")
+    code, size, dtype = _SCALINGS[scaling]
+    return code, 1 if size == 0 else -(-h // size), dtype
+
+
+def norm_out8(N: int, h: int, scaling: str, device=None):
+    """Allocate the 8-bit rows [N, h] (e4m3) and their scales of sao_rms_norm_fwd: [N, 1] fp32 for "row", [N, ceil(h /
+    128)] fp32 for "block", [N, ceil(h / 32)] e8m0 for "mx"."""
+    code, n, dtype = _scales(scaling, h)
+    if code == 0:
+        raise ValueError("no 8-bit rows without a scaling")
+    return (torch.empty(N, h, dtype=_E4M3, device=device or "cuda"),
+            torch.empty(N, n, dtype=dtype, device=device or "cuda"))
+
+
+def _norm(x, weight):
+    """(N, h, code of x, code of the weight)"""
+    if x.dim() != 2 or weight.numel() != x.shape[1]:
+        raise ValueError("x must be [N, h], weight [h]")
+    _current(x.get_device() if x.is_cuda else None)
+    return (*x.shape, _dtype_code(x), _dtype_code(weight))
+
+
+def sao_rms_norm_fwd(x, weight, eps, ws, residual=None, sum=None, y=None, rstd=None, y8=None, scales=None,
+                     scaling="none", stream=None):
+    """y8, scales: of norm_out8, or uint8 tensors of their sizes."""
+    N, h, code, w_code = _norm(x, weight)
+    scale_code, n, dtype = _scales(scaling, h)
+    y8 = y8 if y8 is None or y8.dtype is _U8 else y8.view(_U8) if y8.dtype is _E4M3 else y8
+    if scales is not None and scales.dtype is _E8M0:
+        scales = scales.view(_U8)
+    dtype = _U8 if dtype is _E8M0 else dtype
+    _check(load().sao_rms_norm_fwd(_ptr(x), _arg(residual, x.dtype, N * h, "residual"), code, _ptr(weight), w_code,
+                                   float(eps), N, h, _arg(sum, x.dtype, N * h, "sum"), _arg(y, x.dtype, N * h, "y"),
+                                   _arg(rstd, _F32, N, "rstd"), _arg(y8, _U8, N * h, "y8"),
+                                   _arg(scales, dtype, N * n, "scales"), scale_code, _ptr(ws), ws.numel(),
+                                   _stream(stream)))
+
+
+def sao_rms_norm_bwd(sum, weight, rstd, dy, dx, dweight, ws, dsum=None, accumulate=False, stream=None):
+    """sum: the forward's (x without a residual); dsum: the gradient that reaches it past the norm; dweight or None."""
+    N, h, code, w_code = _norm(sum, weight)
+    _check(load().sao_rms_norm_bwd(_ptr(sum), code, _ptr(weight), w_code, _arg(rstd, _F32, N, "rstd"),
+                                   _arg(dy, sum.dtype, N * h, "dy"), _arg(dsum, sum.dtype, N * h, "dsum"), N, h,
+                                   _arg(dx, sum.dtype, N * h, "dx"), _arg(dweight, _F32, h, "dweight"),
+                                   1 if accumulate else 0, _ptr(ws), ws.numel(), _stream(stream)))
+
+
 class _Tensor(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("n", ctypes.c_int64), ("dt", ctypes.c_int)]
 
@@ -532,11 +609,6 @@ class TensorList:
 
     def __len__(self):
         return len(self.tensors)
-
-
-def _current(device) -> None:
-    if device is not None and device != _device():
-        raise ValueError(f"the tensors lie on device {device}, the current one is {_device()}")
 
 
 def sao_grad_workspace_bytes() -> int:

@@ -55,8 +55,8 @@ def close(grads, limit, result, out):
     assert abs(coef - c) <= 6 * U * c
     for g, o in zip(grads, out):
         d = g.double() * c
-        step = 2.0 ** -9 if o.dtype is BF16 else U  # half a step, of the value
-        assert ((o.double() - d).abs() <= (6 * U + 2 * step) * d.abs() + 2.0 ** -134).all()
+        half = torch.finfo(o.dtype).eps / 2  # of a step, relative to the value
+        assert ((o.double() - d).abs() <= (7 * U + half) * d.abs() + 2.0 ** -134).all()
 
 
 MIXED = [(70001, F32), (1, BF16), (0, F32), (8192, F32), (8193, F32), (16384, BF16), (16385, BF16), (7, F32), (0, BF16),
