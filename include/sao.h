@@ -19,6 +19,7 @@
  *     over the LM head;
  *   - sao_balance_loss_fwd/bwd   : load balance of a mixture of experts.
  * And what stands directly around the losses in that step:
+ *   - sao_route_fwd/bwd          : a router's choice of experts and their weights;
  *   - sao_rms_norm_fwd/bwd       : the root-mean-square norm in front of the LM
  *     head, of the residual stream's sum, in 8 bits too;
  *   - sao_grad_sumsq, sao_grad_clip : the global norm of all gradients, clipping.
@@ -91,6 +92,7 @@ typedef enum sao_dtype {
 #define SAO_DEVERR_CACHE_ROW 0x10u   /* cached backward: a row with grad != 0 the forward skipped */
 #define SAO_DEVERR_TOP_ID 0x20u      /* a teacher's entry with an id >= V, or one id twice in a row */
 #define SAO_DEVERR_EXPERT_ID 0x40u   /* some expert id >= E */
+#define SAO_DEVERR_LOGITS 0x80u      /* a row of router logits without scores (NaN, +inf under softmax) */
 
 /* Library version, major * 10000 + minor * 100 + patch. */
 SAO_API int sao_version(void);
@@ -563,6 +565,73 @@ SAO_API sao_status sao_balance_loss_bwd(const void *logits, sao_dtype dt, const 
                                         int score, const int64_t *counts, const int64_t *rows,
                                         const float *grad_loss, void *grad_logits, void *ws, size_t ws_bytes,
                                         sao_stream_t stream);
+
+/* Most experts that sao_route_fwd/bwd take, and most of them a token. */
+#define SAO_ROUTE_MAX_EXPERTS 1024
+#define SAO_ROUTE_MAX_K 32
+/* Most groups of experts. */
+#define SAO_ROUTE_MAX_GROUPS 32
+
+/* What a group of experts is chosen by. */
+#define SAO_GROUP_MAX 0  /* its largest key */
+#define SAO_GROUP_TOP2 1 /* the sum of its two largest keys */
+
+/*
+ * Routing to experts: each token's k experts and their weights (beside the balance
+ * loss, which takes both logits and choices; the paper has no counterpart). Of the
+ * logits x of a row,
+ *   s_e = softmax(x)_e (SAO_SCORE_SOFTMAX) or sigmoid(x_e) (SAO_SCORE_SIGMOID; not
+ *         divided by their sum, as the balance loss does)
+ *   key_e = s_e + bias_e; the k experts of the largest keys, in falling order, equal
+ *         keys by the lower index
+ *   w_j = scale s_{e_j}, divided by the sum of the chosen s if renormalise != 0
+ * With groups > 1 the experts form that many runs of E / groups; groups_kept of them
+ * stay, by their largest key or the sum of their two largest (group_score), equal ones
+ * by the lower index, and the choice is among their experts.
+ * Choices are those of the exact scores: keys too near one another for fp32 are
+ * compared in 64 bits, keys without a bias by their logits. (Softmax and sigmoid keep
+ * the logits' order, so experts whose scores are equal in any precision, as of
+ * logits past 40, go by the logits too unless there is a bias.)
+ * An expert of logit -inf, or of a bias that is -inf or NaN, is never chosen and counts for nothing in
+ * its group (one with a single other expert is worth that one's key): where fewer than k are left, the
+ * row's last ids are -1 with weight 0. Chosen scores that add up to 0 have weights 0 too.
+ * replay != 0: expert_ids are given (a rollout's choices), each row's weights are those
+ * of its ids, negative ones have none, and bias, groups and group_score are not used.
+ * Ids of E or more have no weight either (and SAO_DEVERR_EXPERT_ID).
+ *   logits [N, E] dt           bias [E] fp32 or NULL
+ *   row_mask [N] uint8 or NULL: rows with 0 have ids -1 (not if given) and weights 0
+ *   expert_ids [N, k] int32    output, or input (replay)
+ *   weights [N, k] fp32        output
+ * A row with a NaN, or under softmax with a +inf, has no scores: ids -1 (not if given), weights 0 (and
+ * SAO_DEVERR_LOGITS). Neither has one that is -inf throughout, which is no error.
+ * 1 <= k <= min(SAO_ROUTE_MAX_K, groups_kept E / groups), E <= SAO_ROUTE_MAX_EXPERTS, 1 <=
+ * groups_kept <= groups <= SAO_ROUTE_MAX_GROUPS, groups divides E; scale finite.
+ * Workspace of both calls: sao_route_workspace_bytes(N, E), which never falls as
+ * one of them grows.
+ */
+SAO_API size_t sao_route_workspace_bytes(int64_t N, int32_t E);
+SAO_API sao_status sao_route_fwd(const void *logits, sao_dtype dt, const float *bias, const uint8_t *row_mask,
+                                 int64_t N, int32_t E, int32_t k, int score, int32_t groups, int32_t groups_kept,
+                                 int group_score, int renormalise, float scale, int replay, int32_t *expert_ids,
+                                 float *weights, void *ws, size_t ws_bytes, sao_stream_t stream);
+
+/*
+ * Gradient of sum_tj grad_weights[t, j] weights[t, j] in the logits (the choice is not
+ * differentiated). With c = sum_j g_j w_j of the row:
+ *   renormalised   softmax d x_j = w_j (g_j - c / scale), sigmoid the same times 1 - s_j;
+ *                  0 for experts that were not chosen
+ *   else           softmax d x_e = s_e (scale g_e - c), g_e = 0 for those that were not
+ *                  chosen; sigmoid d x_j = g_j w_j (1 - s_j)
+ *   expert_ids, weights   the forward's (ids as given, with replay); an id that a row
+ *                  has twice gets both of its gradients
+ *   grad_logits [N, E] dt   overwritten (0 on masked rows), or (accumulate != 0) added
+ *                  to: to the balance loss's. A bf16 sum is rounded once more.
+ * scale 0 gives gradients of 0, as do rows without scores.
+ */
+SAO_API sao_status sao_route_bwd(const void *logits, sao_dtype dt, const uint8_t *row_mask, int64_t N, int32_t E,
+                                 int32_t k, int score, int renormalise, float scale, const int32_t *expert_ids,
+                                 const float *weights, const float *grad_weights, void *grad_logits, int accumulate,
+                                 void *ws, size_t ws_bytes, sao_stream_t stream);
 
 /* Widest rows of sao_rms_norm_fwd/bwd. */
 #define SAO_NORM_MAX_H 16384

@@ -12,6 +12,7 @@
 #include "grads.cuh"
 #include "logprobs_common.cuh"
 #include "norm.cuh"
+#include "route.cuh"
 #include "sao_common.cuh"
 #include "sao_internal.h"
 
@@ -605,6 +606,74 @@ sao_status sao_balance_loss_bwd(const void *logits, sao_dtype dt, const uint8_t 
   return finish_call(ws, s);
 }
 
+static sao_status check_route(sao_dtype dt, int64_t N, int32_t E, int32_t k, int score, float scale) {
+  if (bad_dtype(dt)) return fail(SAO_ERR_UNSUPPORTED, "unknown dtype %d", int(dt));
+  if (N < 0 || N >= (int64_t(1) << 31)) return fail(SAO_ERR_SHAPE, "N = %lld out of range", (long long)N);
+  if (E < 1 || E > SAO_ROUTE_MAX_EXPERTS) return fail(SAO_ERR_SHAPE, "E = %d: 1 <= E <= %d", E, SAO_ROUTE_MAX_EXPERTS);
+  if (k < 1 || k > SAO_ROUTE_MAX_K || k > E)
+    return fail(SAO_ERR_SHAPE, "k = %d of %d experts: 1 <= k <= %d", k, E, SAO_ROUTE_MAX_K);
+  if (score != SAO_SCORE_SOFTMAX && score != SAO_SCORE_SIGMOID)
+    return fail(SAO_ERR_INVALID_ARG, "unknown score %d", score);
+  if (!isfinite(scale)) return fail(SAO_ERR_INVALID_ARG, "scale must be finite (%g)", scale);
+  return SAO_OK;
+}
+
+static bool aligned_to(const void *p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+
+size_t sao_route_workspace_bytes(int64_t N, int32_t E) {
+  if (N < 0 || E < 1 || E > SAO_ROUTE_MAX_EXPERTS) return 0;
+  return kWsHeader;
+}
+
+sao_status sao_route_fwd(const void *logits, sao_dtype dt, const float *bias, const uint8_t *row_mask, int64_t N,
+                         int32_t E, int32_t k, int score, int32_t groups, int32_t groups_kept, int group_score,
+                         int renormalise, float scale, int replay, int32_t *expert_ids, float *weights, void *ws,
+                         size_t ws_bytes, sao_stream_t stream) {
+  SAO_RANGE();
+  SAO_TRY(check_route(dt, N, E, k, score, scale));
+  if (!replay) {
+    if (groups < 1 || groups > SAO_ROUTE_MAX_GROUPS || E % groups != 0 || groups_kept < 1 || groups_kept > groups)
+      return fail(SAO_ERR_SHAPE, "%d of %d groups of %d experts", groups_kept, groups, E);
+    if (k > groups_kept * (E / groups))
+      return fail(SAO_ERR_SHAPE, "k = %d of %d experts that stay", k, groups_kept * (E / groups));
+    if (group_score != SAO_GROUP_MAX && group_score != SAO_GROUP_TOP2)
+      return fail(SAO_ERR_INVALID_ARG, "unknown group_score %d", group_score);
+  }
+  if (N == 0) return SAO_OK;
+  if (!logits || !expert_ids || !weights) return fail(SAO_ERR_INVALID_ARG, "NULL array argument");
+  if (!aligned_to(logits, dt == SAO_BF16 ? 2 : 4) || !aligned_to(bias, 4) || !aligned_to(expert_ids, 4) ||
+      !aligned_to(weights, 4))
+    return fail(SAO_ERR_INVALID_ARG, "an array is not aligned to its elements");
+  Ws w;
+  SAO_TRY(take_ws(ws, ws_bytes, 0, &w));
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  SAO_TRY(begin_call(ws, s));
+  SAO_TRY(route_fwd_launch({logits, bias, row_mask, N, E, k, score, groups, groups_kept, group_score == SAO_GROUP_TOP2,
+                            renormalise, scale, replay, expert_ids, weights, w.err}, dt, s));
+  return finish_call(ws, s);
+}
+
+sao_status sao_route_bwd(const void *logits, sao_dtype dt, const uint8_t *row_mask, int64_t N, int32_t E, int32_t k,
+                         int score, int renormalise, float scale, const int32_t *expert_ids, const float *weights,
+                         const float *grad_weights, void *grad_logits, int accumulate, void *ws, size_t ws_bytes,
+                         sao_stream_t stream) {
+  SAO_RANGE();
+  SAO_TRY(check_route(dt, N, E, k, score, scale));
+  if (N == 0) return SAO_OK;
+  if (!logits || !expert_ids || !weights || !grad_weights || !grad_logits)
+    return fail(SAO_ERR_INVALID_ARG, "NULL array argument");
+  if (!aligned_to(logits, dt == SAO_BF16 ? 2 : 4) || !aligned_to(grad_logits, dt == SAO_BF16 ? 2 : 4) ||
+      !aligned_to(expert_ids, 4) || !aligned_to(weights, 4) || !aligned_to(grad_weights, 4))
+    return fail(SAO_ERR_INVALID_ARG, "an array is not aligned to its elements");
+  Ws w;
+  SAO_TRY(take_ws(ws, ws_bytes, 0, &w));
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  SAO_TRY(begin_call(ws, s));
+  SAO_TRY(route_bwd_launch({logits, row_mask, N, E, k, score, renormalise, scale, expert_ids, weights, grad_weights,
+                            grad_logits, accumulate, w.err}, dt, s));
+  return finish_call(ws, s);
+}
+
 static sao_status check_norm(sao_dtype dt, sao_dtype w_dt, int64_t N, int32_t h) {
   if (bad_dtype(dt) || bad_dtype(w_dt)) return fail(SAO_ERR_UNSUPPORTED, "unknown dtype %d or %d", int(dt), int(w_dt));
   if (N < 0 || N >= (int64_t(1) << 31)) return fail(SAO_ERR_SHAPE, "N = %lld out of range", (long long)N);
@@ -630,12 +699,10 @@ sao_status sao_rms_norm_fwd(const void *x, const void *residual, sao_dtype dt, c
   if (!residual != !sum) return fail(SAO_ERR_INVALID_ARG, "residual and sum are given together or not at all");
   if (!y8 != !scales || !y8 != (scaling == SAO_SCALE_NONE))
     return fail(SAO_ERR_INVALID_ARG, "y8, scales and a scaling are given together or not at all");
-  const uintptr_t unit = dt == SAO_BF16 ? 1 : 3, w_unit = w_dt == SAO_BF16 ? 1 : 3;
-  for (const void *p : {x, residual, static_cast<const void *>(sum), static_cast<const void *>(y)})
-    if ((reinterpret_cast<uintptr_t>(p) & unit) != 0)
-      return fail(SAO_ERR_INVALID_ARG, "an array is not aligned to its elements");
-  if ((reinterpret_cast<uintptr_t>(weight) & w_unit) != 0 || (reinterpret_cast<uintptr_t>(rstd) & 3u) != 0 ||
-      (scaling != SAO_SCALE_MX32 && (reinterpret_cast<uintptr_t>(scales) & 3u) != 0))
+  const unsigned unit = dt == SAO_BF16 ? 2 : 4;
+  if (!aligned_to(x, unit) || !aligned_to(residual, unit) || !aligned_to(sum, unit) || !aligned_to(y, unit) ||
+      !aligned_to(weight, w_dt == SAO_BF16 ? 2 : 4) || !aligned_to(rstd, 4) ||
+      (scaling != SAO_SCALE_MX32 && !aligned_to(scales, 4)))
     return fail(SAO_ERR_INVALID_ARG, "an array is not aligned to its elements");
   Ws w;
   SAO_TRY(take_ws(ws, ws_bytes, 0, &w));
@@ -656,12 +723,9 @@ sao_status sao_rms_norm_bwd(const void *sum, sao_dtype dt, const void *weight, s
     return SAO_OK;
   }
   if (!sum || !weight || !rstd || !dy || !dx) return fail(SAO_ERR_INVALID_ARG, "NULL array argument");
-  const uintptr_t unit = dt == SAO_BF16 ? 1 : 3, w_unit = w_dt == SAO_BF16 ? 1 : 3;
-  for (const void *p : {sum, dy, dsum, static_cast<const void *>(dx)})
-    if ((reinterpret_cast<uintptr_t>(p) & unit) != 0)
-      return fail(SAO_ERR_INVALID_ARG, "an array is not aligned to its elements");
-  if ((reinterpret_cast<uintptr_t>(weight) & w_unit) != 0 || (reinterpret_cast<uintptr_t>(rstd) & 3u) != 0 ||
-      (reinterpret_cast<uintptr_t>(dweight) & 3u) != 0)
+  const unsigned unit = dt == SAO_BF16 ? 2 : 4;
+  if (!aligned_to(sum, unit) || !aligned_to(dy, unit) || !aligned_to(dsum, unit) || !aligned_to(dx, unit) ||
+      !aligned_to(weight, w_dt == SAO_BF16 ? 2 : 4) || !aligned_to(rstd, 4) || !aligned_to(dweight, 4))
     return fail(SAO_ERR_INVALID_ARG, "an array is not aligned to its elements");
   Ws w;
   SAO_TRY(take_ws(ws, ws_bytes, dweight ? norm_ws_bytes(N, h) : 0, &w));
@@ -677,7 +741,7 @@ static sao_status check_tensors(const sao_tensor *t, int32_t count, const char *
     if (t[i].n < 0 || t[i].n >= (int64_t(1) << 48))
       return fail(SAO_ERR_SHAPE, "%s[%d]: %lld elements", what, i, (long long)t[i].n);
     if (t[i].n > 0 && !t[i].data) return fail(SAO_ERR_INVALID_ARG, "%s[%d] is NULL", what, i);
-    if ((reinterpret_cast<uintptr_t>(t[i].data) & (t[i].dt == SAO_BF16 ? 1u : 3u)) != 0)
+    if (!aligned_to(t[i].data, t[i].dt == SAO_BF16 ? 2 : 4))
       return fail(SAO_ERR_INVALID_ARG, "%s[%d] is not aligned to its elements", what, i);
   }
   return SAO_OK;

@@ -190,6 +190,7 @@ sao_status finish_call(void *ws, cudaStream_t s) {
     if (word & SAO_DEVERR_CACHE_ROW) what += " cached-row-not-computed";
     if (word & SAO_DEVERR_TOP_ID) what += " teacher-entry-out-of-range-or-twice";
     if (word & SAO_DEVERR_EXPERT_ID) what += " expert-id-out-of-range";
+    if (word & SAO_DEVERR_LOGITS) what += " router-logits-without-scores";
     return fail(SAO_ERR_DEVICE_CHECK, "device check failed (0x%x):%s", word, what.c_str());
   }
   return SAO_OK;

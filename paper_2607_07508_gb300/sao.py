@@ -21,6 +21,8 @@ SAO_F32, SAO_BF16 = 0, 1
 SAO_STEP_AVERAGE, SAO_STEP_LAST = 0, 1
 SAO_NORM_TOKEN, SAO_NORM_SEQUENCE = 0, 1
 SAO_SCORE_SOFTMAX, SAO_SCORE_SIGMOID = 0, 1
+SAO_GROUP_MAX, SAO_GROUP_TOP2 = 0, 1
+SAO_ROUTE_MAX_EXPERTS, SAO_ROUTE_MAX_K, SAO_ROUTE_MAX_GROUPS = 1024, 32, 32
 SAO_SCALE_NONE, SAO_SCALE_ROW, SAO_SCALE_BLOCK128, SAO_SCALE_MX32 = 0, 1, 2, 3
 SAO_NORM_MAX_H = 16384
 SAO_DISTILL_MAX_K, SAO_BALANCE_MAX_EXPERTS = 1024, 1024
@@ -39,6 +41,7 @@ EXPORTS = ("sao_version", "sao_last_error_string", "sao_set_checked", "sao_get_c
            "sao_token_logprobs_bwd_cached",
            "sao_distill_workspace_bytes", "sao_distill_loss_fwd", "sao_distill_loss_bwd",
            "sao_balance_workspace_bytes", "sao_balance_loss_fwd", "sao_balance_loss_bwd",
+           "sao_route_workspace_bytes", "sao_route_fwd", "sao_route_bwd",
            "sao_norm_workspace_bytes", "sao_rms_norm_fwd", "sao_rms_norm_bwd",
            "sao_grad_workspace_bytes", "sao_grad_sumsq", "sao_grad_clip",
            "sao_value_loss", "sao_profile_enable", "sao_profile_reset", "sao_profile_read")
@@ -105,6 +108,11 @@ def load(path: Optional[str] = None):
                                                 P, SZ, P]),
         "sao_balance_loss_bwd": (ctypes.c_int, [P, ctypes.c_int, P, P, I32, I64, I32, I32, ctypes.c_int, P, P, P, P, P,
                                                 SZ, P]),
+        "sao_route_workspace_bytes": (SZ, [I64, I32]),
+        "sao_route_fwd": (ctypes.c_int, [P, ctypes.c_int, P, P, I64, I32, I32, ctypes.c_int, I32, I32, ctypes.c_int,
+                                         ctypes.c_int, F, ctypes.c_int, P, P, P, SZ, P]),
+        "sao_route_bwd": (ctypes.c_int, [P, ctypes.c_int, P, I64, I32, I32, ctypes.c_int, ctypes.c_int, F, P, P, P, P,
+                                         ctypes.c_int, P, SZ, P]),
         "sao_norm_workspace_bytes": (SZ, [I64, I32]),
         "sao_rms_norm_fwd": (ctypes.c_int, [P, P, ctypes.c_int, P, ctypes.c_int, F, I64, I32, P, P, P, P, P,
                                             ctypes.c_int, P, SZ, P]),
@@ -526,6 +534,47 @@ def sao_balance_loss_bwd(logits, k, score, counts, rows, grad_loss, grad_logits,
 def _current(device) -> None:
     if device is not None and device != _device():
         raise ValueError(f"the tensors lie on device {device}, the current one is {_device()}")
+
+
+def sao_route_workspace_bytes(N: int, E: int) -> int:
+    return int(load().sao_route_workspace_bytes(int(N), int(E)))
+
+
+def route_workspace(N: int, E: int, device=None) -> torch.Tensor:
+    """Allocate the workspace of sao_route_fwd/bwd for up to N tokens and E experts."""
+    return torch.empty(max(sao_route_workspace_bytes(N, E), 256), dtype=torch.uint8, device=device or "cuda")
+
+
+def _router(logits, expert_ids):
+    """(N, E, k)"""
+    N, E = logits.shape
+    if expert_ids.dim() != 2 or expert_ids.shape[0] != N:
+        raise ValueError("expert_ids must be [N, k]")
+    _current(logits.get_device() if logits.is_cuda else None)
+    return N, E, expert_ids.shape[1]
+
+
+def sao_route_fwd(logits, score, expert_ids, weights, ws, bias=None, row_mask=None, groups=1, groups_kept=1,
+                  group_score=SAO_GROUP_MAX, renormalise=True, scale=1.0, replay=False, stream=None):
+    """expert_ids [N, k] int32: written, or read with `replay`."""
+    N, E, k = _router(logits, expert_ids)
+    _check(load().sao_route_fwd(_ptr(logits), _dtype_code(logits), _arg(bias, _F32, E, "bias"),
+                                _arg(row_mask, _U8, N, "row_mask"), N, E, k, int(score), int(groups), int(groups_kept),
+                                int(group_score), 1 if renormalise else 0, float(scale), 1 if replay else 0,
+                                _arg(expert_ids, _I32, N * k, "expert_ids"), _arg(weights, _F32, N * k, "weights"),
+                                _ptr(ws), ws.numel(), _stream(stream)))
+
+
+def sao_route_bwd(logits, score, expert_ids, weights, grad_weights, grad_logits, ws, row_mask=None, renormalise=True,
+                  scale=1.0, accumulate=False, stream=None):
+    """accumulate: added to grad_logits, which holds another loss's gradient."""
+    N, E, k = _router(logits, expert_ids)
+    _check(load().sao_route_bwd(_ptr(logits), _dtype_code(logits), _arg(row_mask, _U8, N, "row_mask"), N, E, k,
+                                int(score), 1 if renormalise else 0, float(scale),
+                                _arg(expert_ids, _I32, N * k, "expert_ids"), _arg(weights, _F32, N * k, "weights"),
+                                _arg(grad_weights, _F32, N * k, "grad_weights"),
+                                _arg(grad_logits, logits.dtype, N * E, "grad_logits"), 1 if accumulate else 0, _ptr(ws),
+                                ws.numel(), _stream(stream)))
 
 
 def sao_norm_workspace_bytes(N: int, h: int) -> int:
