@@ -1,30 +1,20 @@
-// Routing to experts: each token's k experts and their weights, and the gradient of the logits.
+// Routing to experts: each token's k experts and their weights.
 //
 //   s_e = softmax(x)_e or sigmoid(x_e),  key_e = s_e + bias_e,  the k largest keys of the groups that stay
 //   w_j = scale s_j, over the sum of the chosen s where weights are renormalised
 //
-// A warp takes a row; a lane holds consecutive experts of one group, so that the lowest index of equal keys is
-// the lowest lane's, and a group's best two come from the few lanes that share it. Softmax and sigmoid keep the
-// logits' order: without a bias experts are picked by their logits, which is exact, and renormalised weights need
-// the chosen logits alone. Keys with a bias (and sums of two keys) are formed in fp32 first; a row in which two of
-// them are nearer to one another than their errors, and not the same logit and bias, is chosen again in fp64.
-#include <cuda_bf16.h>
-#include <math.h>
-#include <stdint.h>
-
-#include <type_traits>
-
-#include "route.cuh"
-#include "sao_common.cuh"
-#include "sao_internal.h"
+// Softmax and sigmoid keep the logits' order: without a bias experts are picked by their logits, which is exact, and
+// renormalised weights need the chosen logits alone. Keys with a bias (and sums of two keys) are formed in fp32; a row in
+// which two of them are nearer to one another than their errors, and not of the same logit and bias, is chosen again in
+// fp64.
+#include "route_common.cuh"
 
 namespace sao {
 namespace {
 
-constexpr int kWarps = 8;  // rows of a CTA at a time
-constexpr unsigned kAll = 0xffffffffu;
+using namespace route;
 
-// Where a lane's experts lie: `per` of them from `first` on, `count` of them there.
+// Where a lane's experts lie: consecutive ones of one group, `per` of them or fewer.
 struct Lanes {
   int share;  // lanes to a group (a power of two)
   int per;    // experts to a lane
@@ -40,12 +30,7 @@ __device__ __forceinline__ int count_of(const Lanes &l, int lane) {
   return left < l.per ? (left > 0 ? left : 0) : l.per;
 }
 
-__device__ __forceinline__ float value(const float *p) { return ld(p); }
-__device__ __forceinline__ float value(const __nv_bfloat16 *p) {
-  return __uint_as_float(uint32_t(ld(reinterpret_cast<const uint16_t *>(p))) << 16);
-}
-
-// fp32 values in the order of unsigned integers.
+// Values in the order of unsigned integers.
 __device__ __forceinline__ uint32_t ordered(float v) {
   const uint32_t u = __float_as_uint(v);
   return u ^ (uint32_t(int32_t(u) >> 31) | 0x80000000u);
@@ -53,25 +38,15 @@ __device__ __forceinline__ uint32_t ordered(float v) {
 __device__ __forceinline__ float unordered(uint32_t u) {
   return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u);
 }
+__device__ __forceinline__ uint64_t ordered(double v) {
+  const uint64_t u = uint64_t(__double_as_longlong(v));
+  return u ^ (uint64_t(int64_t(u) >> 63) | 0x8000000000000000ull);
+}
 __device__ __forceinline__ float warp_max(float v) { return unordered(__reduce_max_sync(kAll, ordered(v))); }
-__device__ __forceinline__ double warp_max(double v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v = fmax(v, __shfl_xor_sync(kAll, v, o));
-  return v;
-}
-template <class F>
-__device__ __forceinline__ F warp_sum(F v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(kAll, v, o);
-  return v;
-}
-
-__device__ __forceinline__ float exp_of(float v) { return expf(v); }
-__device__ __forceinline__ double exp_of(double v) { return exp(v); }
-template <class F>
-__device__ __forceinline__ F sigmoid(F x) {
-  const F e = exp_of(-fabs(x));  // never past the range, and small scores keep their digits
-  return (x < F(0) ? e : F(1)) / (F(1) + e);
+__device__ __forceinline__ uint64_t warp_max(uint64_t v) {
+  const uint32_t high = __reduce_max_sync(kAll, uint32_t(v >> 32));
+  const uint32_t low = __reduce_max_sync(kAll, uint32_t(v >> 32) == high ? uint32_t(v) : 0u);
+  return uint64_t(high) << 32 | low;
 }
 
 template <class F>
@@ -80,308 +55,470 @@ __device__ __forceinline__ void merge_two(F &a1, F &a2, F b1, F b2) {
   a1 = fmax(a1, b1);
 }
 
-// The choice of one row from its logits x (-inf: none there, or never chosen). Lane j gets choice j, -1 if there
-// is none. F: float, or double where fp32 cannot tell (*near).
-template <class F, int kPer>
-__device__ __forceinline__ int choose(const RouteArgs &a, const Lanes &l, const float (&x)[kPer], float top,
-                                      bool *near) {
-  constexpr bool k32 = std::is_same<F, float>::value;
+// The choice of one row in fp64 (without a bias: by its logits, and sums of scores in fp64). Lane j gets choice j, -1 if
+// there is none. Few rows come here; keys are compared as integers, as the fp64 units are few.
+template <class T, int kPer, bool kBiased>
+__device__ __noinline__ int choose_exactly(const RouteArgs *args, const Lanes *lanes, const T *row) {
+  const RouteArgs &a = *args;
+  const Lanes &l = *lanes;
   const int lane = threadIdx.x & 31, e0 = first_of(l, lane), n = count_of(l, lane);
-  const F none = -INFINITY;
-  const bool soft = a.score == SAO_SCORE_SOFTMAX, biased = a.bias != nullptr;
-  F key[kPer];
-  F inverse = 1, most = 1;  // most: no score is larger
-  if (soft && biased) {
-    F sum = 0;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) sum += exp_of(F(x[i]) - F(top));
-    inverse = most = F(1) / warp_sum(sum);
+  const bool soft = a.score == SAO_SCORE_SOFTMAX;
+  constexpr int kUnroll = kPer <= 8 ? kPer : 1;  // (else in local memory, which costs the kernel no registers)
+  float top = -INFINITY;
+#pragma unroll 1
+  for (int i = 0; i < n; ++i) top = fmaxf(top, value(row + e0 + i));
+  top = warp_max(top);
+  double inverse = 1.0;
+  if (kBiased && soft) {
+    double sum = 0.0;
+#pragma unroll 1
+    for (int i = 0; i < n; ++i) sum += exp(double(value(row + e0 + i)) - double(top));
+    inverse = 1.0 / warp_sum(sum);
   }
-#pragma unroll
+  uint64_t key[kPer];  // 0: none
+#pragma unroll kUnroll
   for (int i = 0; i < kPer; ++i) {
-    key[i] = F(x[i]);
-    if (biased && i < n && x[i] > -INFINITY) {
-      const float b = ld(a.bias + e0 + i);
-      const F s = soft ? exp_of(F(x[i]) - F(top)) * inverse : sigmoid(F(x[i]));
-      key[i] = b > -INFINITY ? s + F(b) + F(0) : none;
-    }
+    key[i] = 0;
+    if (i >= n) continue;
+    const float x = value(row + e0 + i) + 0.f, b = kBiased ? ld(a.bias + e0 + i) : 0.f;  // -0 and 0 are one key
+    if (!(x > -INFINITY && b > -INFINITY)) continue;
+    double k = double(x);
+    if (kBiased) k = (soft ? exp(double(x) - double(top)) * inverse : sigmoid(double(x))) + double(b) + 0.0;
+    key[i] = ordered(k);
   }
-  *near = false;
-  // fp32: a score is off by at most 2^-19 of the row's largest one (exponential, difference from the largest logit,
-  // sum of up to 1024, quotient), a key by another 2^-24 of itself; twice that for a difference
-  const auto tell = [&](F v) { return F(0x1p-18) * most + F(0x1p-22) * fabs(v); };
-
+  bool stays = true;
   if (l.groups > 1) {
-    F b1 = none, b2 = none;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) merge_two(b1, b2, key[i], none);
-    for (int o = 1; o < l.share; o <<= 1) {
-      const F c1 = __shfl_xor_sync(kAll, b1, o), c2 = __shfl_xor_sync(kAll, b2, o);
-      merge_two(b1, b2, c1, c2);
+    uint64_t b1 = 0, b2 = 0;
+#pragma unroll kUnroll
+    for (int i = 0; i < kPer; ++i) {
+      b2 = max(b2, min(b1, key[i]));
+      b1 = max(b1, key[i]);
     }
-    const bool exact = !biased && !a.two;
-    F v = b1;
-    if (a.two) {
-      if (!biased) {  // the scores of the two largest logits (softmax: times their common sum)
-        const F s1 = soft ? exp_of(b1 - F(top)) : sigmoid(b1), s2 = soft ? exp_of(b2 - F(top)) : sigmoid(b2);
-        v = b1 > none ? s1 + s2 : none;
-      } else if (b2 > none) {
-        v = b1 + b2;
-      }
+    for (int o = 1; o < l.share; o <<= 1) {
+      const uint64_t c1 = __shfl_xor_sync(kAll, b1, o), c2 = __shfl_xor_sync(kAll, b2, o);
+      b2 = max(min(b1, c1), max(b2, c2));
+      b1 = max(b1, c1);
+    }
+    uint64_t v = b1;
+    if (a.two && b1 != 0) {
+      const auto plain = [&](uint64_t u) {  // its score, or key with the bias
+        const double k = __longlong_as_double(int64_t(u & 0x8000000000000000ull ? u ^ 0x8000000000000000ull : ~u));
+        return u == 0 ? 0.0 : kBiased ? k : soft ? exp(k - double(top)) : sigmoid(k);
+      };
+      v = ordered(plain(b1) + plain(b2) + 0.0);
     }
     const int mine = lane / l.share;
     int rank = 0;
     for (int g = 0; g < l.groups; ++g) {
-      const F other = __shfl_sync(kAll, v, g * l.share);
+      const uint64_t other = __shfl_sync(kAll, v, g * l.share);
       rank += other > v || (other == v && g < mine);
     }
-    const bool real = mine < l.groups, stays = real && rank < a.kept;
-    if (k32 && !exact) {
-      const int last = __ffs(__ballot_sync(kAll, real && rank == a.kept - 1)) - 1;
-      const F vl = __shfl_sync(kAll, v, last), l1 = __shfl_sync(kAll, b1, last), l2 = __shfl_sync(kAll, b2, last);
-      const bool close = real && !(fabs(v - vl) > 2 * tell(vl)) && v > none;
-      const bool same = !biased && b1 == l1 && b2 == l2;
-      *near = __any_sync(kAll, close && !stays) && __any_sync(kAll, close && !same);
-    }
-    if (!stays) {
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) key[i] = none;
-    }
+    stays = mine < l.groups && rank < a.kept;
   }
-
   int id = -1;
-  F before = 0;
-  float x_before = 0.f, b_before = 0.f;
-  const bool compare = k32 && biased;
-  for (int j = 0; j < a.k + (compare ? 1 : 0); ++j) {
-    F best = key[0];
-#pragma unroll
-    for (int i = 1; i < kPer; ++i) best = fmax(best, key[i]);
-    const F m = warp_max(best);
-    if (!(m > none)) break;
-    const unsigned from = __ballot_sync(kAll, best == m);
-    const int win = __ffs(from) - 1;
-    int at = 0;
-    float xv = 0.f;
-    bool found = false;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const bool hit = !found && lane == win && key[i] == m;
-      if (hit) at = i, xv = x[i], key[i] = none;
-      found |= hit;
-    }
+  for (int j = 0; j < a.k; ++j) {
+    uint64_t best = 0;
+    int at = -1;
+#pragma unroll kUnroll
+    for (int i = 0; i < kPer; ++i)
+      if (stays && key[i] > best) best = key[i], at = i;
+    const uint64_t m = warp_max(best);
+    if (m == 0) break;
+    const int win = __ffs(__ballot_sync(kAll, best == m)) - 1;
+#pragma unroll kUnroll
+    for (int i = 0; i < kPer; ++i)
+      if (lane == win && i == at) key[i] = 0;
     const int e = __shfl_sync(kAll, e0 + at, win);
-    if (lane == j && j < a.k) id = e;
-    if (compare) {
-      xv = __shfl_sync(kAll, xv, win);
-      const float b = ld(a.bias + e);
-      if (j > 0 && !(before - m > 2 * tell(before)) && !(xv == x_before && b == b_before)) *near = true;
-      before = m, x_before = xv, b_before = b;
-    }
+    if (lane == j) id = e;
   }
   return id;
 }
 
+// A lane's logits of one row as they lie in memory: vectors of up to 16 bytes where they are aligned to those (kWide).
 template <class T, int kPer>
-__device__ __forceinline__ void load_row(const T *row, const Lanes &l, float (&x)[kPer]) {
-  const int lane = threadIdx.x & 31, e0 = first_of(l, lane), n = count_of(l, lane);
+struct Logits {
+  static constexpr bool kCanWide = kPer >= 2 && (kPer & (kPer - 1)) == 0;
+  [[maybe_unused]] static constexpr int kWords = kPer * int(sizeof(T)) / 4;
+  uint32_t w[kPer];
+  __device__ __forceinline__ void load(const T *p, int n, bool full, bool wide) {
+    if constexpr (kCanWide) {
+      if (wide) {
+        if constexpr (kWords == 1) {
+          w[0] = ld(reinterpret_cast<const uint32_t *>(p));
+        } else if constexpr (kWords == 2) {
+          const uint2 v = ld(reinterpret_cast<const uint2 *>(p));
+          w[0] = v.x, w[1] = v.y;
+        } else {
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) x[i] = i < n ? value(row + e0 + i) + 0.f : -INFINITY;  // -0 and 0 are one key
-}
-
-// The choice in fp64, the row read again: few rows come here, and none of their registers are held for it.
-template <class T, int kPer>
-__device__ __noinline__ int choose_again(const RouteArgs *a, const Lanes *l, const T *row, float top) {
-  float x[kPer];
-  load_row<T, kPer>(row, *l, x);
-  bool near;
-  return choose<double, kPer>(*a, *l, x, top, &near);
-}
-
-template <class T, int kPer>
-__global__ void __launch_bounds__(kWarps * 32) route_fwd_kernel(const __grid_constant__ RouteArgs a,
-                                                                const __grid_constant__ Lanes l) {
-  grid_wait();
-  const int lane = threadIdx.x & 31;
-  const bool soft = a.score == SAO_SCORE_SOFTMAX;
-  for (int64_t row = int64_t(blockIdx.x) * kWarps + threadIdx.x / 32; row < a.N; row += int64_t(gridDim.x) * kWarps) {
-    int32_t *ids = a.ids + row * a.k;
-    float *weights = a.weights + row * a.k;
-    if (a.mask && ld(a.mask + row) == 0) {
-      if (lane < a.k) {
-        if (!a.replay) ids[lane] = -1;
-        weights[lane] = 0.f;
+          for (int i = 0; i < kWords; i += 4) {
+            const uint4 v = ld(reinterpret_cast<const uint4 *>(p) + i / 4);
+            w[i] = v.x, w[i + 1] = v.y, w[i + 2] = v.z, w[i + 3] = v.w;
+          }
+        }
+        return;
       }
-      continue;
     }
-    const T *from = static_cast<const T *>(a.x) + row * a.E;
-    float x[kPer];
-    load_row<T, kPer>(from, l, x);
-    bool bad = false;
-    float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      bad |= !(x[i] < INFINITY) && (soft || x[i] != x[i]);
-      top = fmaxf(top, x[i]);
+      w[i] = 0u;
+      if (full || i < n) {
+        if constexpr (sizeof(T) == 2)
+          w[i] = ld(reinterpret_cast<const uint16_t *>(p) + i);
+        else
+          w[i] = ld(reinterpret_cast<const uint32_t *>(p) + i);
+      }
     }
-    top = warp_max(top);
-    bad = __any_sync(kAll, bad);
-    if (bad && lane == 0) raise_device_error(a.err, SAO_DEVERR_LOGITS);
+  }
+  __device__ __forceinline__ void get(float (&x)[kPer], bool wide) const {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      if constexpr (sizeof(T) == 4) {
+        x[i] = __uint_as_float(w[i]);
+      } else {
+        if (kCanWide && wide)
+          x[i] = __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+        else
+          x[i] = __uint_as_float(w[i] << 16);
+      }
+    }
+  }
+};
+
+// exp and sigmoid for keys alone. With |x| 2^-23.4 for the product's rounding and 2^-22.5 for the exponential's error (of
+// itself), a sigmoid is off by s (1 - s) of those, its sum's 2^-24 and the reciprocal's 2^-23: less than 2^-21.
+__device__ __forceinline__ float exp_fast(float x) {
+  float e;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x * 1.4426950408889634f));
+  return e;
+}
+__device__ __forceinline__ float sigmoid_fast(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + exp_fast(-x)));
+  return r;
+}
+// How near two keys may be for their order in fp32 to be doubted, but for rounding with their own size: twice a score's
+// error. Under softmax that has the sum's, 2^-18 of the row's largest score.
+constexpr float kDoubtSigmoid = 0x1p-20f, kDoubtSoftmax = 0x1p-17f;
+
+// How a call's rows are taken.
+struct Plan {
+  int batch;      // consecutive rows of a warp at a time: their choices fill its lanes
+  uint32_t mask;  // the bits of a packed key that hold the expert
+  int wide;       // rows are aligned for vectors
+};
+
+// A warp takes `batch` rows, one after another up to the choices, which come to lie in lane r k + j; their weights
+// are then computed and written for all of them at once.
+//
+// Keys are packed: bits in the order of integers, the lowest of them replaced by the expert's index (inverted: the
+// lower of equal ones is the larger), so that a pick is one integer maximum over the warp and gives key and index, and
+// the next one is the largest below it: p - m, as unsigned numbers, is larger for each p < m than for any other. A bf16
+// logit has room for the index. Other keys are packed by their distance d from the row's largest, whose leading bits say
+// most where it counts: those of the picks are small. Neighbours that differ in the replaced bits alone, or by less than
+// their errors, are looked at again (choose_exactly) unless they are of one logit and bias.
+//
+// kFull: 32 kPer experts, no lane with fewer than another.
+template <class T, int kPer, bool kFull, bool kBiased>
+__global__ void __launch_bounds__(kWarps * 32, kPer <= 4 ? 5 : kPer <= 8 ? 3 : 1)
+    route_fwd_kernel(const __grid_constant__ RouteArgs a, const __grid_constant__ Lanes l, Plan plan) {
+  grid_wait();
+  constexpr bool kExact = !kBiased && sizeof(T) == 2;
+  const int lane = threadIdx.x & 31;
+  const int e0 = kFull ? lane * kPer : first_of(l, lane), n = kFull ? kPer : count_of(l, lane);
+  const bool soft = a.score == SAO_SCORE_SOFTMAX, wide = kFull && plan.wide;
+  const bool sums = soft && (kBiased || !a.renorm), need_top = sums || (soft && a.two && l.groups > 1);
+  const uint32_t mask = kExact ? 0xffffu : plan.mask, low = mask - uint32_t(e0);
+  const auto index = [&](int i) { return kFull ? low - i : (low - i) & mask; };
+  // no packed key of an expert that can be chosen is below it (-inf, or a distance of inf)
+  const uint32_t none = (kExact ? 0x007fffffu : 0x00ffffffu) | mask;
+  const int mine = lane / a.k, j = lane - mine * a.k, first = mine * a.k;
+  const bool even = (a.k & (a.k - 1)) == 0;
+  float b[kPer];
+  if (kBiased) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      b[i] = -INFINITY;
+      if (kFull || i < n) b[i] = fmaxf(ld(a.bias + e0 + i), -INFINITY);  // (a NaN is out as well)
+    }
+  }
+  const int64_t step = int64_t(gridDim.x) * kWarps * plan.batch;
+  for (int64_t row0 = (int64_t(blockIdx.x) * kWarps + threadIdx.x / 32) * plan.batch; row0 < a.N; row0 += step) {
+    const int rows = int(a.N - row0 < plan.batch ? a.N - row0 : plan.batch);
+    unsigned on = rows == 32 ? kAll : (1u << rows) - 1u;
+    if (a.mask) on &= __ballot_sync(kAll, lane < rows && ld(a.mask + row0 + (lane < rows ? lane : 0)) != 0);
+    unsigned good = 0u;             // rows with scores
+    unsigned doubt = 0u;            // rows whose groups are in doubt, or whose keys have no distances
+    uint32_t pick = 0u, next = 0u;  // this lane's choice; the key after the row's last one
+    float peak = 0.f, total = 1.f;  // of this lane's row, where they are needed: largest logit, sum of exponentials
+    const T *from = static_cast<const T *>(a.x) + row0 * a.E + e0;
+    Logits<T, kPer> ahead;
+    ahead.load(from, n, kFull, wide);
+    for (int r = 0; r < rows; ++r) {
+      float x[kPer];
+      ahead.get(x, wide);
+      from += a.E;
+      if (r + 1 < rows) ahead.load(from, n, kFull, wide);
+      if (!(on >> r & 1u)) continue;
+      float probe = 0.f;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) probe = fmaf(x[i], 0.f, probe);
+      bool out = false;  // some logit is -inf
+      if (__any_sync(kAll, probe != 0.f)) {  // a NaN or an infinity
+        bool bad = false;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) bad |= !(x[i] < INFINITY) && (soft || x[i] != x[i]);
+        if (__any_sync(kAll, bad)) {
+          if (lane == 0) raise_device_error(a.err, SAO_DEVERR_LOGITS);
+          continue;
+        }
+        out = true;
+      }
+      if (!kFull) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) x[i] = i < n ? x[i] : -INFINITY;
+      }
+      float top = 0.f, inverse = 1.f;
+      if (need_top || out) {
+        top = x[0];
+#pragma unroll
+        for (int i = 1; i < kPer; ++i) top = fmaxf(top, x[i]);
+        top = warp_max(top);
+        if (!(top > -INFINITY)) continue;
+      }
+      good |= 1u << r;
+      float key[kPer];
+      if (sums) {
+        float sum = 0.f;
+        if (a.renorm) {
+#pragma unroll
+          for (int i = 0; i < kPer; ++i) sum += key[i] = exp_fast(x[i] - top);
+        } else {  // the weights have this sum's error
+#pragma unroll
+          for (int i = 0; i < kPer; ++i) sum += key[i] = expf(x[i] - top);
+        }
+        sum = warp_sum(sum);
+        inverse = 1.f / sum;
+        if (mine == r) peak = top, total = sum;
+      }
+      if (a.replay) continue;
+      if (kBiased) {
+        if (soft) {
+#pragma unroll
+          for (int i = 0; i < kPer; ++i) key[i] = fmaf(key[i], inverse, b[i]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < kPer; ++i) key[i] = sigmoid_fast(x[i]) + b[i];
+        }
+        if (out) {
+#pragma unroll
+          for (int i = 0; i < kPer; ++i) key[i] = x[i] > -INFINITY ? key[i] : -INFINITY;
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) key[i] = x[i] + 0.f;  // -0 and 0 are one key
+      }
+      float b1 = -INFINITY;
+      if (l.groups > 1) {
+        float b2 = -INFINITY;
+        if (a.two) {
+#pragma unroll
+          for (int i = 0; i < kPer; ++i) {
+            b2 = fmaxf(b2, fminf(b1, key[i]));
+            b1 = fmaxf(b1, key[i]);
+          }
+          for (int o = 1; o < l.share; o <<= 1) {
+            const float c1 = __shfl_xor_sync(kAll, b1, o), c2 = __shfl_xor_sync(kAll, b2, o);
+            merge_two(b1, b2, c1, c2);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < kPer; ++i) b1 = fmaxf(b1, key[i]);
+          for (int o = 1; o < l.share; o <<= 1) b1 = fmaxf(b1, __shfl_xor_sync(kAll, b1, o));
+        }
+        float v = b1;
+        if (a.two && b1 > -INFINITY) {
+          if (kBiased)
+            v = b2 > -INFINITY ? b1 + b2 : b1;
+          else
+            v = soft ? exp_fast(b1 - top) + exp_fast(b2 - top) : sigmoid_fast(b1) + sigmoid_fast(b2);
+        }
+        // picked like experts, the group in the last five bits
+        const int group = lane / l.share;
+        const uint32_t u = v > -INFINITY && group < l.groups ? (ordered(v) & ~31u) | (31u - group) : 0u;
+        uint32_t last = __reduce_max_sync(kAll, u);
+        for (int i = 1; i < a.kept; ++i) last = __reduce_max_sync(kAll, u < last ? u : 0u);
+        if (!kExact || a.two) {
+          const uint32_t after = __reduce_max_sync(kAll, u < last ? u : 0u);
+          if (after != 0u) {
+            const float p = unordered(last & ~31u), q = unordered(after & ~31u), size = fabsf(p) + fabsf(q);
+            float error = 0x1p-18f * size;  // of the five bits
+            if (kBiased || a.two)
+              error += 2.f * (soft ? kDoubtSoftmax * (kBiased ? inverse : 1.f) : kDoubtSigmoid) + 0x1p-22f * size;
+            if (!(p - q > error)) doubt |= 1u << r;
+          }
+        }
+        if (u < last) {
+          b1 = -INFINITY;
+#pragma unroll
+          for (int i = 0; i < kPer; ++i) key[i] = -INFINITY;
+        }
+      }
+      uint32_t p[kPer];
+      if (kExact) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) p[i] = (ordered(key[i]) & ~mask) | index(i);
+      } else {
+        if (l.groups == 1) {
+#pragma unroll
+          for (int i = 0; i < kPer; ++i) b1 = fmaxf(b1, key[i]);
+        }
+        const float largest = warp_max(b1);
+        if (!(fabsf(largest) < INFINITY)) {  // no expert, or one whose distances from the others say nothing
+          doubt |= 1u << r;
+          continue;
+        }
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) p[i] = (~(__float_as_uint(largest - key[i]) << 1) & ~mask) | index(i);
+      }
+      uint32_t m = 0u;
+      const auto below = [&] {  // the largest packed key below m
+        uint32_t best = p[0] - m;
+#pragma unroll
+        for (int i = 1; i < kPer; ++i) best = max(best, p[i] - m);
+        return m + __reduce_max_sync(kAll, best);
+      };
+      const int its = lane - r * a.k;
+#pragma unroll 4
+      for (int c = 0; c < a.k; ++c) {
+        m = below();
+        if (its == c) pick = m;
+      }
+      if (!kExact) {
+        const uint32_t found = below();
+        if (mine == r && found < m) next = found;  // (not where all experts are picked)
+      }
+    }
+
+    // the choices of all rows
+    const bool there = lane < rows * a.k;
+    const int64_t row = row0 + (there ? mine : 0);
+    from = static_cast<const T *>(a.x) + row * a.E;
     int id = -1;
-    const bool scores = !bad && top > -INFINITY;
+    const bool scores = there && (good >> mine & 1u);
     if (a.replay) {
-      if (lane < a.k) id = ld(ids + lane);
+      if (there && (on >> mine & 1u)) id = ld(a.ids + row0 * a.k + lane);
       if (id >= a.E) raise_device_error(a.err, SAO_DEVERR_EXPERT_ID);
       if (id >= a.E || !scores) id = -1;
-    } else {
-      if (scores) {
-        bool near;
-        id = choose<float, kPer>(a, l, x, top, &near);
-        if (__any_sync(kAll, near)) id = choose_again<T, kPer>(&a, &l, from, top);
+    } else if (scores && pick > none) {
+      id = int(mask - (pick & mask));
+    }
+    float chosen = id >= 0 ? value(from + id) : -INFINITY;
+    if (!a.replay && (!kExact || doubt != 0u)) {
+      // (a row that ran out of experts may only have run out of distances below inf)
+      bool near = scores && ((doubt >> mine & 1u) || (!kExact && id < 0));
+      if (!kExact) {
+        uint32_t after = __shfl_down_sync(kAll, pick, 1);
+        float x_after = __shfl_down_sync(kAll, chosen, 1);
+        if (j == a.k - 1) {
+          after = next;
+          x_after = after > none && id >= 0 ? value(from + int(mask - (after & mask))) : 0.f;
+        }
+        if (id >= 0 && after > none) {
+          bool apart = (pick & ~mask) > (after & ~mask), same = chosen == x_after;
+          if (kBiased) {
+            const float b_pick = ld(a.bias + id), b_after = ld(a.bias + int(mask - (after & mask)));
+            const float d = __uint_as_float((~pick & ~mask) >> 1), d_after = __uint_as_float((~after & ~mask) >> 1);
+            const float error = (soft ? kDoubtSoftmax / total : kDoubtSigmoid) +
+                                0x1p-23f * (2.f + fabsf(b_pick) + fabsf(b_after)) + 0x1p-23f * float(mask + 2u) * d_after;
+            apart = d_after - d > error;
+            same &= b_pick == b_after;
+          }
+          near |= !apart && !same;
+        }
       }
-      if (lane < a.k) ids[lane] = id;
+      unsigned again = __ballot_sync(kAll, near);
+      while (again != 0u) {
+        const int r = (__ffs(again) - 1) / a.k;
+        const int found = choose_exactly<T, kPer, kBiased>(&a, &l, static_cast<const T *>(a.x) + (row0 + r) * a.E);
+        const int its = __shfl_sync(kAll, found, j);
+        if (there && mine == r) {
+          id = its;
+          chosen = id >= 0 ? value(from + id) : -INFINITY;
+        }
+        again &= ~__ballot_sync(kAll, mine == r);
+      }
     }
     float w = 0.f;
-    const float chosen = id >= 0 ? value(from + id) : -INFINITY;
     if (a.renorm) {
       // sigmoid(x) = exp(min(x, 0)) / (1 + exp(-|x|)): relative to the largest, no sum vanishes
-      const float low = soft ? chosen : fminf(chosen, 0.f), m = warp_max(low);
-      if (m > -INFINITY) {
-        float s = expf(low - m);
-        if (!soft) s /= 1.f + expf(-fabsf(chosen));
-        w = s / warp_sum(s);
-      }
+      const float lower = soft ? chosen : fminf(chosen, 0.f), m = share_max(lower, first, a.k, even);
+      float s = m > -INFINITY ? expf(lower - m) : 0.f;
+      if (!soft) s /= 1.f + expf(-fabsf(chosen));
+      const float sum = share_sum(s, first, a.k, even);
+      if (sum > 0.f) w = s / sum;
     } else if (!soft) {
       w = sigmoid(chosen);
-    } else {
-      float sum = 0.f;
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) sum += scores ? expf(x[i] - top) : 0.f;
-      sum = warp_sum(sum);
-      if (scores) w = expf(chosen - top) / sum;
+    } else if (id >= 0) {
+      w = expf(chosen - peak) / total;
     }
-    if (lane < a.k) weights[lane] = a.scale * w;
-  }
-}
-
-template <class T, int kPer>
-__global__ void __launch_bounds__(kWarps * 32) route_bwd_kernel(const __grid_constant__ RouteBwdArgs a, int per) {
-  grid_wait();
-  const int lane = threadIdx.x & 31;
-  const Lanes l{32, per, a.E, 1};
-  const int e0 = first_of(l, lane), n = count_of(l, lane);
-  const bool soft = a.score == SAO_SCORE_SOFTMAX, dense = soft && !a.renorm;
-  for (int64_t row = int64_t(blockIdx.x) * kWarps + threadIdx.x / 32; row < a.N; row += int64_t(gridDim.x) * kWarps) {
-    const T *x = static_cast<const T *>(a.x) + row * a.E;
-    T *dx = static_cast<T *>(a.dx) + row * a.E;
-    const bool on = a.scale != 0.f && (a.mask == nullptr || ld(a.mask + row) != 0);
-    int id = -1;
-    float w = 0.f, g = 0.f;
-    if (on && lane < a.k) {
-      id = ld(a.ids + row * a.k + lane);
-      if (id >= a.E) raise_device_error(a.err, SAO_DEVERR_EXPERT_ID), id = -1;
-      if (id >= 0) w = ld(a.weights + row * a.k + lane), g = ld(a.grad + row * a.k + lane);
-    }
-    const float c = warp_sum(g * w);
-    float d = 0.f;  // of choice j in lane j
-    if (dense)
-      d = a.scale * g;
-    else if (w != 0.f) {
-      d = a.renorm ? w * (g - c / a.scale) : w * g;
-      if (!soft) d *= sigmoid(-value(x + id));
-    }
-    float v[kPer];
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) v[i] = 0.f;
-    for (int j = 0; j < a.k; ++j) {
-      const int at = __shfl_sync(kAll, id, j) - e0;
-      const float dj = __shfl_sync(kAll, d, j);
-#pragma unroll
-      for (int i = 0; i < kPer; ++i)
-        if (at == i) v[i] += dj;
-    }
-    if (dense) {
-      float p[kPer], sum = 0.f, top = -INFINITY;
-      const bool any = __any_sync(kAll, id >= 0);
-      if (any) load_row<T, kPer>(x, l, p);
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        if (!any) p[i] = 0.f;
-        top = fmaxf(top, p[i]);
-      }
-      top = warp_max(top);
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) sum += p[i] = expf(p[i] - top);
-      const float inverse = 1.f / warp_sum(sum);
-      const bool scores = any && top > -INFINITY && inverse > 0.f;  // a NaN, +inf: the sum is NaN
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) v[i] = scores ? p[i] * inverse * (v[i] - c) : 0.f;
-    }
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      if (i >= n) continue;
-      if (a.accumulate) v[i] += value(dx + e0 + i);
-      if constexpr (sizeof(T) == 2)
-        dx[e0 + i] = __float2bfloat16_rn(v[i]);
-      else
-        dx[e0 + i] = v[i];
+    if (there) {
+      if (!a.replay) a.ids[row0 * a.k + lane] = id;
+      a.weights[row0 * a.k + lane] = id >= 0 ? a.scale * w : 0.f;
     }
   }
 }
 
+// f(the least count of a table that is `per` or more, whether the experts are 32 of it)
 template <class F>
-sao_status by_count(int per, F f) {
-  if (per <= 1) return f(std::integral_constant<int, 1>());
-  if (per <= 2) return f(std::integral_constant<int, 2>());
-  if (per <= 4) return f(std::integral_constant<int, 4>());
-  if (per <= 5) return f(std::integral_constant<int, 5>());
-  if (per <= 8) return f(std::integral_constant<int, 8>());
-  if (per <= 16) return f(std::integral_constant<int, 16>());
-  if (per <= 32) return f(std::integral_constant<int, 32>());
-  return f(std::integral_constant<int, 64>());  // 17 to 31 groups, a lane each: up to 60 experts
-}
-
-template <class F>
-sao_status by_type(sao_dtype dt, F f) {
-  return dt == SAO_BF16 ? f(__nv_bfloat16()) : f(float());
-}
-
-sao_status grid_of(int64_t N, unsigned *grid) {
-  DeviceInfo di;
-  SAO_TRY(device_info(&di));
-  const int64_t most = int64_t(di.sm_count) * 16, g = (N + kWarps - 1) / kWarps;
-  *grid = unsigned(g < most ? g : most);
-  return SAO_OK;
+sao_status by_count(int E, int per, F f) {
+  const auto full = [&](auto count) { return f(count, std::integral_constant<bool, true>()); };
+  const auto part = [&](auto count) { return f(count, std::integral_constant<bool, false>()); };
+  using std::integral_constant;
+  if (E == 32 * per) {
+    if (per == 1) return full(integral_constant<int, 1>());
+    if (per == 2) return full(integral_constant<int, 2>());
+    if (per == 4) return full(integral_constant<int, 4>());
+    if (per == 5) return full(integral_constant<int, 5>());
+    if (per == 8) return full(integral_constant<int, 8>());
+    if (per == 16) return full(integral_constant<int, 16>());
+  }
+  if (per <= 1) return part(integral_constant<int, 1>());
+  if (per <= 2) return part(integral_constant<int, 2>());
+  if (per <= 4) return part(integral_constant<int, 4>());
+  if (per <= 6) return part(integral_constant<int, 6>());
+  if (per <= 8) return part(integral_constant<int, 8>());
+  if (per <= 12) return part(integral_constant<int, 12>());
+  if (per <= 16) return part(integral_constant<int, 16>());
+  if (per <= 32) return part(integral_constant<int, 32>());
+  return part(integral_constant<int, 64>());  // 17 to 31 groups, a lane each: up to 60 experts
 }
 
 }  // namespace
 
 sao_status route_fwd_launch(const RouteArgs &args, sao_dtype dt, cudaStream_t s) {
+  DeviceInfo di;
+  SAO_TRY(device_info(&di));
   RouteArgs a = args;
   if (a.groups == a.kept || a.replay) a.groups = a.kept = 1;
+  if (a.replay) a.bias = nullptr;
   Lanes l{32, 0, a.E / a.groups, a.groups};
   while (l.share * a.groups > 32) l.share /= 2;
   l.per = (l.size + l.share - 1) / l.share;
-  unsigned grid;
-  SAO_TRY(grid_of(a.N, &grid));
+  // as many rows to a warp as its lanes have room for, while there are rows for every warp
+  const int64_t spread = a.N / (int64_t(di.sm_count) * 4 * kWarps);
+  Plan p{int(least(32 / a.k, spread < 1 ? 1 : spread)), 0u, 0};
+  while (p.mask < unsigned(a.E) - 1u) p.mask = 2 * p.mask + 1u;
+  const int bytes = l.per * (dt == SAO_BF16 ? 2 : 4);
+  p.wide = reinterpret_cast<uintptr_t>(a.x) % unsigned(bytes < 16 ? bytes : 16) == 0;
+  const int64_t grid = least((a.N + kWarps * p.batch - 1) / (kWarps * p.batch), int64_t(di.sm_count) * 128);
   const int slot = launch_begin("route_fwd", s);
   SAO_TRY(by_type(dt, [&](auto t) {
-    return by_count(l.per, [&](auto per) {
-      pdl(route_fwd_kernel<decltype(t), decltype(per)::value>, grid, kWarps * 32, 0, s)(a, l);
-      return SAO_OK;
-    });
-  }));
-  return launch_end(slot, s);
-}
-
-sao_status route_bwd_launch(const RouteBwdArgs &a, sao_dtype dt, cudaStream_t s) {
-  const int per = (a.E + 31) / 32;
-  unsigned grid;
-  SAO_TRY(grid_of(a.N, &grid));
-  const int slot = launch_begin("route_bwd", s);
-  SAO_TRY(by_type(dt, [&](auto t) {
-    return by_count(per, [&](auto count) {
-      pdl(route_bwd_kernel<decltype(t), decltype(count)::value>, grid, kWarps * 32, 0, s)(a, per);
+    return by_count(a.E, l.per, [&](auto per, auto full) {
+      using T = decltype(t);
+      constexpr int kPer = decltype(per)::value;
+      constexpr bool kFull = decltype(full)::value;
+      const auto kernel = a.bias ? route_fwd_kernel<T, kPer, kFull, true> : route_fwd_kernel<T, kPer, kFull, false>;
+      pdl(kernel, unsigned(grid), kWarps * 32, 0, s)(a, l, p);
       return SAO_OK;
     });
   }));
