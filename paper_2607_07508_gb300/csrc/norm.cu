@@ -159,7 +159,7 @@ __device__ __forceinline__ uint32_t power_of(float amax, float *inverse) {
 }
 
 template <class T, class WT, int kVec, int kLoads>
-__global__ void __launch_bounds__(kMaxThreads) norm_fwd_kernel(NormFwd a, int warps) {
+__global__ void __launch_bounds__(kMaxThreads, kVec == 1 && kLoads > 16 ? 1 : 2) norm_fwd_kernel(NormFwd a, int warps) {
   grid_wait();
   __shared__ float slots[2 * kMaxWarps];
   Team team(warps, slots);
@@ -198,46 +198,39 @@ __global__ void __launch_bounds__(kMaxThreads) norm_fwd_kernel(NormFwd a, int wa
       for (int j = 0; j < kVec; ++j) s[j & 1] = fmaf(r[i].at(j), r[i].at(j), s[j & 1]);
     const float rstd = 1.f / sqrtf(fmaf(team.sum(s[0] + s[1]), mean, a.eps));
     if (a.rstd && team.warp == 0 && lane == 0) a.rstd[row] = rstd;
-    const auto normed = [&](int i, float(&y)[kVec]) {
+    float y[kLoads][kVec];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) y[i][j] = 0.f;
+      if (column(i) >= a.h) continue;
       float w[kVec];
       weights<WT, kVec>(a.weight, column(i), w);
 #pragma unroll
-      for (int j = 0; j < kVec; ++j) y[j] = r[i].at(j) * rstd * w[j];
-    };
-    if (a.y) {
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i)
-        if (column(i) < a.h) {
-          float y[kVec];
-          normed(i, y);
-          Pack<T, kVec> p;
-          p.set(y);
-          p.store(static_cast<T *>(a.y) + at + column(i));
-        }
+      for (int j = 0; j < kVec; ++j) y[i][j] = r[i].at(j) * rstd * w[j];
+      if (a.y) {
+        Pack<T, kVec> p;
+        p.set(y[i]);
+        p.store(static_cast<T *>(a.y) + at + column(i));
+      }
     }
     if (!a.y8) continue;
     const auto amax_of = [&](int i) {
       float m = 0.f;
-      if (column(i) < a.h) {
-        float y[kVec];
-        normed(i, y);
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) m = max_nan(m, fabsf(y[j]));
-      }
+      for (int j = 0; j < kVec; ++j) m = max_nan(m, fabsf(y[i][j]));
       return m;
     };
     const auto put = [&](int i, float inverse) {
       if (column(i) >= a.h) return;
-      float y[kVec];
-      normed(i, y);
       uint8_t *p = a.y8 + at + column(i);
       if constexpr (kVec == 1) {
-        *p = __nv_cvt_float_to_fp8(y[0] * inverse, __NV_SATFINITE, __NV_E4M3);
+        *p = __nv_cvt_float_to_fp8(y[i][0] * inverse, __NV_SATFINITE, __NV_E4M3);
       } else {
         uint16_t q[kVec / 2];
 #pragma unroll
         for (int j = 0; j < kVec / 2; ++j)
-          q[j] = __nv_cvt_float2_to_fp8x2(make_float2(y[2 * j] * inverse, y[2 * j + 1] * inverse), __NV_SATFINITE,
+          q[j] = __nv_cvt_float2_to_fp8x2(make_float2(y[i][2 * j] * inverse, y[i][2 * j + 1] * inverse), __NV_SATFINITE,
                                           __NV_E4M3);
         const uint32_t low = q[0] | uint32_t(q[1]) << 16;
         if constexpr (kVec == 8)
@@ -417,9 +410,11 @@ int teams_of(int warps) { return warps < kThreads / 32 ? kThreads / 32 / warps :
 
 template <class T, class WT, int kVec>
 sao_status fwd(const NormFwd &a, int sms, cudaStream_t s) {
-  // few rows: up to a CTA's warps each (latency); else few warps with many loads
-  constexpr int kFewLoads = kVec == 1 ? 4 : 1, kMostLoads = kVec == 8 ? 8 : 32 / kVec;
-  const Shape p = shape_of(a.h, kVec, kFewLoads, kMostLoads, a.N <= sms ? kThreads / 32 : 1);
+  // few rows: few loads a lane, for latency. Many: 16 columns a lane up to 8 warps to a row, else 32, which keeps 64
+  // registers and half an SM's warps (65,536 x 2,048 161 us with 16, 168 with 32; 16,384 x 6,144 in 8 bits 166 and 153)
+  constexpr int kFewLoads = kVec == 1 ? 4 : 1, kMostLoads = 32 / kVec;
+  const Shape p = a.N <= sms ? shape_of(a.h, kVec, kFewLoads, kMostLoads, kThreads / 32)
+                             : shape_of(a.h, kVec, kVec == 1 ? 8 : 16 / kVec, kMostLoads, kThreads / 32);
   const int teams = teams_of(p.warps);
   int64_t grid = (a.N + teams - 1) / teams;
   grid = grid < 64 * int64_t(sms) ? grid : 64 * int64_t(sms);
@@ -435,7 +430,8 @@ sao_status fwd(const NormFwd &a, int sms, cudaStream_t s) {
 template <class T, class WT, int kVec>
 sao_status bwd(const NormBwd &a, int sms, float *partial, cudaStream_t s) {
   constexpr int kFewLoads = kVec == 1 ? 4 : 8 / kVec, kMostLoads = 32 / kVec;
-  const Shape p = shape_of(a.h, kVec, kFewLoads, kMostLoads, a.N <= sms ? kThreads / 32 : 1);
+  const int wish = a.N <= sms ? kThreads / 32 : kVec == 1 ? 4 : 1;  // (single columns: fewer lanes past the row's end)
+  const Shape p = shape_of(a.h, kVec, kFewLoads, kMostLoads, wish);
   const int teams = teams_of(p.warps);
   int64_t grid = (a.N + teams - 1) / teams;
   const int most = 2 * sms < kBwdCtas ? 2 * sms : kBwdCtas;
