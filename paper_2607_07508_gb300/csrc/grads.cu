@@ -29,6 +29,10 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kLoads = 8;                                 // of 16 bytes, in flight in a thread
 constexpr int kChunkBytes = kThreads * kLoads * 16;       // 32 KB of a tensor
+// clip_kernel writes what it loads: 512 threads of 64 registers, two CTAs to an SM, which took 544 us for 3.7 GB where
+// 256 threads of 156 registers took 710 and three CTAs 715
+constexpr int kClipThreads = 512;
+constexpr int kClipLoads = kChunkBytes / (kClipThreads * 16);
 constexpr int kMaxGrid = 8 * 160;                         // CTAs of a launch, at most
 
 // The tensors of one launch. n: elements, with the types in its top bits.
@@ -199,19 +203,19 @@ __device__ __forceinline__ void chunk_scale(const void *src, void *dst, int n, f
   const bool wide = ((reinterpret_cast<uintptr_t>(src) | reinterpret_cast<uintptr_t>(dst)) & 15u) == 0;
   const int vectors = wide ? n / kPer : 0;
   if (vectors > 0) {
-    uint4 v[kLoads];
+    uint4 v[kClipLoads];
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int at = threadIdx.x + i * kThreads;
+    for (int i = 0; i < kClipLoads; ++i) {
+      const int at = threadIdx.x + i * kClipThreads;
       if (at < vectors) v[i] = ld(static_cast<const uint4 *>(src) + at);
     }
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int at = threadIdx.x + i * kThreads;
+    for (int i = 0; i < kClipLoads; ++i) {
+      const int at = threadIdx.x + i * kClipThreads;
       if (at >= vectors) continue;
       if constexpr (kBf16Src_ == kBf16Dst_) {
         if (coef == 1.f) {
-          static_cast<uint4 *>(dst)[at] = v[i];
+          __stcs(static_cast<uint4 *>(dst) + at, v[i]);
           continue;
         }
       }
@@ -234,18 +238,18 @@ __device__ __forceinline__ void chunk_scale(const void *src, void *dst, int n, f
           o[j] = *reinterpret_cast<const uint32_t *>(&b);
         }
         if constexpr (kPer == 8)
-          static_cast<uint4 *>(dst)[at] = make_uint4(o[0], o[1], o[2], o[3]);
+          __stcs(static_cast<uint4 *>(dst) + at, make_uint4(o[0], o[1], o[2], o[3]));
         else
-          static_cast<uint2 *>(dst)[at] = make_uint2(o[0], o[1]);
+          __stcs(static_cast<uint2 *>(dst) + at, make_uint2(o[0], o[1]));
       } else {
 #pragma unroll
         for (int j = 0; j < kPer / 4; ++j)
-          static_cast<float4 *>(dst)[at * (kPer / 4) + j] =
-              make_float4(f[4 * j], f[4 * j + 1], f[4 * j + 2], f[4 * j + 3]);
+          __stcs(static_cast<float4 *>(dst) + at * (kPer / 4) + j,
+                 make_float4(f[4 * j], f[4 * j + 1], f[4 * j + 2], f[4 * j + 3]));
       }
     }
   }
-  for (int at = vectors * kPer + threadIdx.x; at < n; at += kThreads) {
+  for (int at = vectors * kPer + threadIdx.x; at < n; at += kClipThreads) {
     const uint32_t w = load_one<kBf16Src_>(src, at).x;
     const float f = __uint_as_float(kBf16Src_ ? w << 16 : w) * coef;
     if (kBf16Src_ && kBf16Dst_ && coef == 1.f)
@@ -258,7 +262,7 @@ __device__ __forceinline__ void chunk_scale(const void *src, void *dst, int n, f
 }
 
 template <int kCap>
-__global__ void __launch_bounds__(kThreads) clip_kernel(const __grid_constant__ List<kCap> l, const double *sumsq,
+__global__ void __launch_bounds__(kClipThreads, 2) clip_kernel(const __grid_constant__ List<kCap> l, const double *sumsq,
                                                         float max_norm, int in_place, float *norm, float *coef) {
   grid_wait();
   __shared__ float factor;
@@ -359,7 +363,7 @@ sao_status clip_of(const sao_tensor *grads, const sao_tensor *out, int32_t count
     int grid;
     SAO_TRY(grid_of(chunks, &grid));
     const int slot = launch_begin("grad_clip", s);
-    pdl(clip_kernel<kCap>, unsigned(grid), kThreads, 0, s)(l, sumsq, max_norm, in_place, norm, coef);
+    pdl(clip_kernel<kCap>, unsigned(grid), kClipThreads, 0, s)(l, sumsq, max_norm, in_place, norm, coef);
     any = true;
     return launch_end(slot, s);
   };

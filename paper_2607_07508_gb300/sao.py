@@ -536,6 +536,12 @@ def _current(device) -> None:
         raise ValueError(f"the tensors lie on device {device}, the current one is {_device()}")
 
 
+def _on_current(t: torch.Tensor) -> None:
+    device = t.get_device()
+    if device >= 0:  # (others are refused where their pointers are taken)
+        _current(device)
+
+
 def sao_route_workspace_bytes(N: int, E: int) -> int:
     return int(load().sao_route_workspace_bytes(int(N), int(E)))
 
@@ -550,7 +556,7 @@ def _router(logits, expert_ids):
     N, E = logits.shape
     if expert_ids.dim() != 2 or expert_ids.shape[0] != N:
         raise ValueError("expert_ids must be [N, k]")
-    _current(logits.get_device() if logits.is_cuda else None)
+    _on_current(logits)
     return N, E, expert_ids.shape[1]
 
 
@@ -586,48 +592,55 @@ def norm_workspace(N: int, h: int, device=None) -> torch.Tensor:
     return torch.empty(max(sao_norm_workspace_bytes(N, h), 256), dtype=torch.uint8, device=device or "cuda")
 
 
-_SCALINGS = {"none": (0, 0, None), "row": (1, 0, _F32), "block": (2, 128, _F32), "mx": (3, 32, _E8M0)}
+_SCALINGS = {"none": (0, 0, (None,)), "row": (1, 0, (_F32,)), "block": (2, 128, (_F32,)), "mx": (3, 32, (_E8M0, _U8))}
+_BYTES = (_E4M3, _U8)
 
 
 def _scales(scaling, h):
-    """(code, scales to a row, their type) of a scaling's name."""
+    """(code, scales to a row, their types) of a scaling's name."""
     if scaling not in _SCALINGS:
         raise ValueError(f"scaling is one of {', '.join(_SCALINGS)}, got {scaling!r}")
-    code, size, dtype = _SCALINGS[scaling]
-    return code, 1 if size == 0 else -(-h // size), dtype
+    code, size, dtypes = _SCALINGS[scaling]
+    return code, 1 if size == 0 else -(-h // size), dtypes
+
+
+def _arg_of(t: Optional[torch.Tensor], dtypes, n: int, name: str) -> Optional[int]:
+    """_arg of a tensor of any of `dtypes`."""
+    if t is None:
+        return None
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name} must be {dtypes[0]}, got {t.dtype}")
+    return _arg(t, t.dtype, n, name)
 
 
 def norm_out8(N: int, h: int, scaling: str, device=None):
     """Allocate the 8-bit rows [N, h] (e4m3) and their scales of sao_rms_norm_fwd: [N, 1] fp32 for "row", [N, ceil(h /
     128)] fp32 for "block", [N, ceil(h / 32)] e8m0 for "mx"."""
-    code, n, dtype = _scales(scaling, h)
+    code, n, dtypes = _scales(scaling, h)
     if code == 0:
         raise ValueError("no 8-bit rows without a scaling")
     return (torch.empty(N, h, dtype=_E4M3, device=device or "cuda"),
-            torch.empty(N, n, dtype=dtype, device=device or "cuda"))
+            torch.empty(N, n, dtype=dtypes[0], device=device or "cuda"))
 
 
 def _norm(x, weight):
     """(N, h, code of x, code of the weight)"""
-    if x.dim() != 2 or weight.numel() != x.shape[1]:
+    N, h = x.shape
+    if weight.numel() != h:
         raise ValueError("x must be [N, h], weight [h]")
-    _current(x.get_device() if x.is_cuda else None)
-    return (*x.shape, _dtype_code(x), _dtype_code(weight))
+    _on_current(x)
+    return N, h, _dtype_code(x), _dtype_code(weight)
 
 
 def sao_rms_norm_fwd(x, weight, eps, ws, residual=None, sum=None, y=None, rstd=None, y8=None, scales=None,
                      scaling="none", stream=None):
     """y8, scales: of norm_out8, or uint8 tensors of their sizes."""
     N, h, code, w_code = _norm(x, weight)
-    scale_code, n, dtype = _scales(scaling, h)
-    y8 = y8 if y8 is None or y8.dtype is _U8 else y8.view(_U8) if y8.dtype is _E4M3 else y8
-    if scales is not None and scales.dtype is _E8M0:
-        scales = scales.view(_U8)
-    dtype = _U8 if dtype is _E8M0 else dtype
+    scale_code, n, dtypes = _scales(scaling, h)
     _check(load().sao_rms_norm_fwd(_ptr(x), _arg(residual, x.dtype, N * h, "residual"), code, _ptr(weight), w_code,
                                    float(eps), N, h, _arg(sum, x.dtype, N * h, "sum"), _arg(y, x.dtype, N * h, "y"),
-                                   _arg(rstd, _F32, N, "rstd"), _arg(y8, _U8, N * h, "y8"),
-                                   _arg(scales, dtype, N * n, "scales"), scale_code, _ptr(ws), ws.numel(),
+                                   _arg(rstd, _F32, N, "rstd"), _arg_of(y8, _BYTES, N * h, "y8"),
+                                   _arg_of(scales, dtypes, N * n, "scales"), scale_code, _ptr(ws), ws.numel(),
                                    _stream(stream)))
 
 
