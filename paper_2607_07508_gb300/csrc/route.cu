@@ -3,145 +3,25 @@
 //   s_e = softmax(x)_e or sigmoid(x_e),  key_e = s_e + bias_e,  the k largest keys of the groups that stay
 //   w_j = scale s_j, over the sum of the chosen s where weights are renormalised
 //
-// Softmax and sigmoid keep the logits' order: without a bias experts are picked by their logits, which is exact, and
-// renormalised weights need the chosen logits alone. Keys with a bias (and sums of two keys) are formed in fp32; a row in
-// which two of them are nearer to one another than their errors, and not of the same logit and bias, is chosen again in
-// fp64.
-#include "route_common.cuh"
+// Softmax and sigmoid keep the logits' order: without a bias experts are picked by their logits, which is exact,
+// and renormalised weights need the chosen logits alone. Keys with a bias (and sums of two keys) are formed in
+// fp32; a row in which two of them are nearer to one another than their errors, and not of the same logit and
+// bias, is chosen again in fp64.
+#include "route_exact.cuh"
 
 namespace sao {
 namespace {
 
 using namespace route;
 
-// Where a lane's experts lie: consecutive ones of one group, `per` of them or fewer.
-struct Lanes {
-  int share;  // lanes to a group (a power of two)
-  int per;    // experts to a lane
-  int size;   // experts to a group
-  int groups;
-};
-__device__ __forceinline__ int first_of(const Lanes &l, int lane) {
-  return lane / l.share * l.size + lane % l.share * l.per;
-}
-__device__ __forceinline__ int count_of(const Lanes &l, int lane) {
-  if (lane / l.share >= l.groups) return 0;
-  const int left = l.size - lane % l.share * l.per;
-  return left < l.per ? (left > 0 ? left : 0) : l.per;
-}
-
-// Values in the order of unsigned integers.
-__device__ __forceinline__ uint32_t ordered(float v) {
-  const uint32_t u = __float_as_uint(v);
-  return u ^ (uint32_t(int32_t(u) >> 31) | 0x80000000u);
-}
-__device__ __forceinline__ float unordered(uint32_t u) {
-  return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u);
-}
-__device__ __forceinline__ uint64_t ordered(double v) {
-  const uint64_t u = uint64_t(__double_as_longlong(v));
-  return u ^ (uint64_t(int64_t(u) >> 63) | 0x8000000000000000ull);
-}
-__device__ __forceinline__ float warp_max(float v) { return unordered(__reduce_max_sync(kAll, ordered(v))); }
-__device__ __forceinline__ uint64_t warp_max(uint64_t v) {
-  const uint32_t high = __reduce_max_sync(kAll, uint32_t(v >> 32));
-  const uint32_t low = __reduce_max_sync(kAll, uint32_t(v >> 32) == high ? uint32_t(v) : 0u);
-  return uint64_t(high) << 32 | low;
-}
-
-template <class F>
-__device__ __forceinline__ void merge_two(F &a1, F &a2, F b1, F b2) {
-  a2 = fmax(fmin(a1, b1), fmax(a2, b2));
-  a1 = fmax(a1, b1);
-}
-
-// The choice of one row in fp64 (without a bias: by its logits, and sums of scores in fp64). Lane j gets choice j, -1 if
-// there is none. Few rows come here; keys are compared as integers, as the fp64 units are few.
-template <class T, int kPer, bool kBiased>
-__device__ __noinline__ int choose_exactly(const RouteArgs *args, const Lanes *lanes, const T *row) {
-  const RouteArgs &a = *args;
-  const Lanes &l = *lanes;
-  const int lane = threadIdx.x & 31, e0 = first_of(l, lane), n = count_of(l, lane);
-  const bool soft = a.score == SAO_SCORE_SOFTMAX;
-  constexpr int kUnroll = kPer <= 8 ? kPer : 1;  // (else in local memory, which costs the kernel no registers)
-  float top = -INFINITY;
-#pragma unroll 1
-  for (int i = 0; i < n; ++i) top = fmaxf(top, value(row + e0 + i));
-  top = warp_max(top);
-  double inverse = 1.0;
-  if (kBiased && soft) {
-    double sum = 0.0;
-#pragma unroll 1
-    for (int i = 0; i < n; ++i) sum += exp(double(value(row + e0 + i)) - double(top));
-    inverse = 1.0 / warp_sum(sum);
-  }
-  uint64_t key[kPer];  // 0: none
-#pragma unroll kUnroll
-  for (int i = 0; i < kPer; ++i) {
-    key[i] = 0;
-    if (i >= n) continue;
-    const float x = value(row + e0 + i) + 0.f, b = kBiased ? ld(a.bias + e0 + i) : 0.f;  // -0 and 0 are one key
-    if (!(x > -INFINITY && b > -INFINITY)) continue;
-    double k = double(x);
-    if (kBiased) k = (soft ? exp(double(x) - double(top)) * inverse : sigmoid(double(x))) + double(b) + 0.0;
-    key[i] = ordered(k);
-  }
-  bool stays = true;
-  if (l.groups > 1) {
-    uint64_t b1 = 0, b2 = 0;
-#pragma unroll kUnroll
-    for (int i = 0; i < kPer; ++i) {
-      b2 = max(b2, min(b1, key[i]));
-      b1 = max(b1, key[i]);
-    }
-    for (int o = 1; o < l.share; o <<= 1) {
-      const uint64_t c1 = __shfl_xor_sync(kAll, b1, o), c2 = __shfl_xor_sync(kAll, b2, o);
-      b2 = max(min(b1, c1), max(b2, c2));
-      b1 = max(b1, c1);
-    }
-    uint64_t v = b1;
-    if (a.two && b1 != 0) {
-      const auto plain = [&](uint64_t u) {  // its score, or key with the bias
-        const double k = __longlong_as_double(int64_t(u & 0x8000000000000000ull ? u ^ 0x8000000000000000ull : ~u));
-        return u == 0 ? 0.0 : kBiased ? k : soft ? exp(k - double(top)) : sigmoid(k);
-      };
-      v = ordered(plain(b1) + plain(b2) + 0.0);
-    }
-    const int mine = lane / l.share;
-    int rank = 0;
-    for (int g = 0; g < l.groups; ++g) {
-      const uint64_t other = __shfl_sync(kAll, v, g * l.share);
-      rank += other > v || (other == v && g < mine);
-    }
-    stays = mine < l.groups && rank < a.kept;
-  }
-  int id = -1;
-  for (int j = 0; j < a.k; ++j) {
-    uint64_t best = 0;
-    int at = -1;
-#pragma unroll kUnroll
-    for (int i = 0; i < kPer; ++i)
-      if (stays && key[i] > best) best = key[i], at = i;
-    const uint64_t m = warp_max(best);
-    if (m == 0) break;
-    const int win = __ffs(__ballot_sync(kAll, best == m)) - 1;
-#pragma unroll kUnroll
-    for (int i = 0; i < kPer; ++i)
-      if (lane == win && i == at) key[i] = 0;
-    const int e = __shfl_sync(kAll, e0 + at, win);
-    if (lane == j) id = e;
-  }
-  return id;
-}
-
 // A lane's logits of one row as they lie in memory: vectors of up to 16 bytes where they are aligned to those (kWide).
 template <class T, int kPer>
 struct Logits {
   static constexpr bool kCanWide = kPer >= 2 && (kPer & (kPer - 1)) == 0;
-  [[maybe_unused]] static constexpr int kWords = kPer * int(sizeof(T)) / 4;
   uint32_t w[kPer];
   __device__ __forceinline__ void load(const T *p, int n, bool full, bool wide) {
     if constexpr (kCanWide) {
+      constexpr int kWords = kPer * int(sizeof(T)) / 4;
       if (wide) {
         if constexpr (kWords == 1) {
           w[0] = ld(reinterpret_cast<const uint32_t *>(p));
@@ -184,22 +64,6 @@ struct Logits {
   }
 };
 
-// exp and sigmoid for keys alone. With |x| 2^-23.4 for the product's rounding and 2^-22.5 for the exponential's error (of
-// itself), a sigmoid is off by s (1 - s) of those, its sum's 2^-24 and the reciprocal's 2^-23: less than 2^-21.
-__device__ __forceinline__ float exp_fast(float x) {
-  float e;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(x * 1.4426950408889634f));
-  return e;
-}
-__device__ __forceinline__ float sigmoid_fast(float x) {
-  float r;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + exp_fast(-x)));
-  return r;
-}
-// How near two keys may be for their order in fp32 to be doubted, but for rounding with their own size: twice a score's
-// error. Under softmax that has the sum's, 2^-18 of the row's largest score.
-constexpr float kDoubtSigmoid = 0x1p-20f, kDoubtSoftmax = 0x1p-17f;
-
 // How a call's rows are taken.
 struct Plan {
   int batch;      // consecutive rows of a warp at a time: their choices fill its lanes
@@ -210,12 +74,13 @@ struct Plan {
 // A warp takes `batch` rows, one after another up to the choices, which come to lie in lane r k + j; their weights
 // are then computed and written for all of them at once.
 //
-// Keys are packed: bits in the order of integers, the lowest of them replaced by the expert's index (inverted: the
-// lower of equal ones is the larger), so that a pick is one integer maximum over the warp and gives key and index, and
-// the next one is the largest below it: p - m, as unsigned numbers, is larger for each p < m than for any other. A bf16
-// logit has room for the index. Other keys are packed by their distance d from the row's largest, whose leading bits say
-// most where it counts: those of the picks are small. Neighbours that differ in the replaced bits alone, or by less than
-// their errors, are looked at again (choose_exactly) unless they are of one logit and bias.
+// Keys are packed: bits in the order of integers, the lowest of them replaced by the expert's index (inverted:
+// the lower of equal ones is the larger), so that a pick is one integer maximum over the warp and gives key and
+// index, and the next one is the largest below it: p - m, as unsigned numbers, is larger for each p < m than for
+// any other. A bf16 logit has room for the index. Other keys are packed by their distance d from the row's
+// largest, whose leading bits say most where it counts: those of the picks are small. Neighbours that differ in
+// the replaced bits alone, or by less than their errors, are looked at again (choose_exactly) unless they are of
+// one logit and bias.
 //
 // kFull: 32 kPer experts, no lane with fewer than another.
 template <class T, int kPer, bool kFull, bool kBiased>
@@ -428,8 +293,8 @@ __global__ void __launch_bounds__(kWarps * 32, kPer <= 4 ? 5 : kPer <= 8 ? 3 : 1
           if (kBiased) {
             const float b_pick = ld(a.bias + id), b_after = ld(a.bias + int(mask - (after & mask)));
             const float d = __uint_as_float((~pick & ~mask) >> 1), d_after = __uint_as_float((~after & ~mask) >> 1);
-            const float error = (soft ? kDoubtSoftmax / total : kDoubtSigmoid) +
-                                0x1p-23f * (2.f + fabsf(b_pick) + fabsf(b_after)) + 0x1p-23f * float(mask + 2u) * d_after;
+            const float size = 2.f + fabsf(b_pick) + fabsf(b_after) + float(mask + 2u) * d_after;
+            const float error = (soft ? kDoubtSoftmax / total : kDoubtSigmoid) + 0x1p-23f * size;
             apart = d_after - d > error;
             same &= b_pick == b_after;
           }
@@ -439,7 +304,8 @@ __global__ void __launch_bounds__(kWarps * 32, kPer <= 4 ? 5 : kPer <= 8 ? 3 : 1
       unsigned again = __ballot_sync(kAll, near);
       while (again != 0u) {
         const int r = (__ffs(again) - 1) / a.k;
-        const int found = choose_exactly<T, kPer, kBiased>(&a, &l, static_cast<const T *>(a.x) + (row0 + r) * a.E);
+        const T *its_row = static_cast<const T *>(a.x) + (row0 + r) * a.E;
+        const int found = choose_exactly<T, kPer, kBiased>({a.bias, a.k, a.kept, soft, a.two != 0}, l, its_row);
         const int its = __shfl_sync(kAll, found, j);
         if (there && mine == r) {
           id = its;
@@ -504,6 +370,7 @@ sao_status route_fwd_launch(const RouteArgs &args, sao_dtype dt, cudaStream_t s)
   Lanes l{32, 0, a.E / a.groups, a.groups};
   while (l.share * a.groups > 32) l.share /= 2;
   l.per = (l.size + l.share - 1) / l.share;
+  if (route_lists_take(a, di.sm_count)) return route_lists_launch(a, l, dt, di.sm_count, s);
   // as many rows to a warp as its lanes have room for, while there are rows for every warp
   const int64_t spread = a.N / (int64_t(di.sm_count) * 4 * kWarps);
   Plan p{int(least(32 / a.k, spread < 1 ? 1 : spread)), 0u, 0};

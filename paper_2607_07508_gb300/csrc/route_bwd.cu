@@ -1,7 +1,7 @@
 // Routing to experts: the gradient of the router's logits.
 //
-// Bound by HBM: it writes every logit's gradient, most of them 0 (renormalised weights, and sigmoid scores, depend on the
-// chosen logits alone).
+// Bound by HBM: it writes every logit's gradient, most of them 0 (renormalised weights, and sigmoid scores,
+// depend on the chosen logits alone).
 #include "bulk.cuh"
 #include "route_common.cuh"
 
@@ -25,10 +25,11 @@ struct BwdPlan {
   int wide;   // dx (and x) on 16 bytes
 };
 
-// A warp writes the gradient of `rows` rows at a time, made up in shared memory and sent off in one bulk copy (the rows
-// lie one after another): zeros with the chosen experts' gradients put between them, or, kDense, the softmax gradient of
-// every logit. Lane r k + j has choice j of row r, 32 / k rows at a time; an id that a row has twice is found with
-// match_any and written once, by its first lane. kEach (kDense): a lane's logits of a row, at most.
+// A warp writes the gradient of `rows` rows at a time, made up in shared memory and sent off in one bulk copy
+// (the rows lie one after another): zeros with the chosen experts' gradients put between them, or, kDense, the
+// softmax gradient of every logit. Lane r k + j has choice j of row r, 32 / k rows at a time; an id that a row
+// has twice is found with match_any and written once, by its first lane. kEach (kDense): a lane's logits of a
+// row, at most.
 template <class T, bool kDense, int kEach>
 __global__ void __launch_bounds__(128) route_bwd_kernel(const __grid_constant__ RouteBwdArgs a, BwdPlan plan) {
   grid_wait();

@@ -126,6 +126,75 @@ def test_groups(E, groups, kept, k, dtype, score, two):
         check(x, k, score, bias, groups=groups, kept=kept, two=two, renorm=bias is None)
 
 
+# With many tokens rows are taken by eight lanes each, up to 512 experts and eight a token.
+MANY = [(16, 1, 1, 1), (17, 1, 1, 5), (63, 1, 1, 6), (64, 1, 1, 8), (96, 2, 1, 3), (100, 4, 3, 8), (128, 1, 1, 8),
+        (160, 8, 3, 8), (256, 8, 4, 8), (256, 2, 1, 7), (257, 1, 1, 8), (384, 4, 1, 2), (512, 8, 7, 8), (24, 8, 2, 6)]
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("E,groups,kept,k", MANY)
+def test_many_tokens(E, groups, kept, k, dtype, score):
+    N = 5003
+    x = _logits(N, E, dtype, seed=E + k)
+    mask = (torch.rand(N, generator=torch.Generator().manual_seed(E)) < 0.7).to(torch.uint8).cuda()
+    for bias in (None, _bias(E), _bias(E) * 30 - 100):
+        for two in (False, True) if groups > 1 else (False,):
+            check(x, k, score, bias, mask if E % 2 else None, groups, kept, two, renorm=two or bias is None or k == 6)
+    check(x, k, score, None, mask, groups, kept, False, renorm=False)
+
+
+@pytest.mark.parametrize("k", [8, 5])
+@pytest.mark.parametrize("groups,kept,two", [(1, 1, False), (8, 3, False), (8, 3, True), (2, 1, True)])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_many_tokens_with_equal_and_near_keys(score, groups, kept, two, k):
+    """Few different logits; logits that differ in their last bits; keys with a bias that differ by its rounding."""
+    N, E = 4000, 128
+    g = torch.Generator().manual_seed(k)
+    for levels in (1, 3, 40):
+        x = (torch.randint(0, levels, (N, E), generator=g).float() * 0.3 - 0.6).cuda()
+        for dtype in ("f32", "bf16"):
+            for bias in (None, torch.zeros(E, device="cuda"), (torch.randint(0, 2, (E,), generator=g) * 0.25).cuda()):
+                check(x.to(DT[dtype]), k, score, bias, groups=groups, kept=kept, two=two, train=False)
+    base = _logits(1, E, seed=3).repeat(N, 1)
+    moved = (base.view(torch.int32) + torch.randint(-40, 40, (N, E), generator=g, dtype=torch.int32).cuda()).view(torch.float32)
+    x = torch.where(torch.rand(N, E, generator=g).cuda() < 0.5, moved, base[:, :1]).contiguous()
+    bias = (0.75 - R.scores(base[:1].double(), score)[0]).float()
+    near = torch.where(torch.rand(N, E, generator=g).cuda() < 0.5, moved, base).contiguous()
+    for rows, b in ((x, None), (moved, None), (near, bias)):
+        check(rows, k, score, b, groups=groups, kept=kept, two=two, train=False)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("groups,kept", [(1, 1), (4, 2)])
+def test_many_tokens_out_of_the_ordinary(groups, kept, dtype, score):
+    """NaN, infinities, rows with few experts or none, the type's lowest value, far and large logits, biases that are out."""
+    N, E, inf = 3000, 64, math.inf
+    x = _logits(N, E, dtype, seed=21)
+    g = torch.Generator().manual_seed(22)
+    kind = torch.randint(0, 12, (N,), generator=g).cuda()
+    at = torch.randint(0, E, (N,), generator=g).cuda()
+    x[torch.arange(N).cuda(), at] = torch.where(kind < 3, torch.tensor([math.nan, inf, -inf]).cuda()[kind.clamp(max=2)],
+                                                x[torch.arange(N).cuda(), at].float()).to(x.dtype)
+    x[kind == 3] = -inf
+    x[kind == 4, 3:] = -inf
+    x[kind == 5, 2:] = torch.finfo(x.dtype).min
+    x[kind == 6] *= 40
+    x[kind == 7] -= 200
+    x[kind == 8] *= 1e30
+    bias = _bias(E)
+    bias[5], bias[6] = -inf, math.nan
+    large = bias.clone()
+    large[9] = 1e4
+    top = bias.clone()
+    top[9] = inf
+    for b in (None, bias, large, top):
+        for two in (False, True):
+            check(x, 6, score, b, groups=groups, kept=kept, two=two, renorm=True, train=False)
+    check(x, 8, score, None, groups=groups, kept=kept, renorm=False, train=False)
+
+
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 @pytest.mark.parametrize("levels", [1, 2, 3, 40])
 @pytest.mark.parametrize("groups,kept", [(1, 1), (8, 3), (16, 5)])
