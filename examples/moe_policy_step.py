@@ -7,7 +7,11 @@ The rows of one packed batch serve three objectives at once, as in a run that di
   balance       load balance of the router, each trajectory by itself, over all tokens
 
 The LM head's gradient is one fp32 buffer: the RL backward writes it, the distillation backward adds to it; the
-hidden states' gradients are summed. Run it as `python -m examples.moe_policy_step`.
+hidden states' gradients are summed.
+
+`whole_step` has what lies in front of and behind those losses too: the router's choice of experts, whose outputs join
+the residual stream, the norm in front of the head, their gradients, and the clipping of all of them by their norm.
+Run it as `python -m examples.moe_policy_step`.
 """
 from __future__ import annotations
 
@@ -16,6 +20,7 @@ import torch
 from paper_2607_07508_gb300 import sao, synthetic as S
 
 DISTILL_WEIGHT, BALANCE_WEIGHT = 0.5, 0.01
+EPS, MAX_NORM, ROUTE_SCALE = 1e-6, 0.1, 2.5
 TEMPERATURE, TOP, EXPERTS, CHOSEN = 2.0, 20, 16, 2
 
 
@@ -80,14 +85,64 @@ def step(b):
             "dW": dW, "d_router": d_router}
 
 
+def layer(b, seed=8):
+    """The last layer in front of the head: the stream, a balance bias, what each token's chosen experts answer (here
+    drawn, for any choice: the experts' products are not the step's subject) and the norm's weight."""
+    wl, E = b["wl"], b["router"].shape[1]
+    g = torch.Generator().manual_seed(seed)
+    dev = b["H"].device
+    return {"residual": wl.H.to(dev), "bias": (0.1 * torch.randn(E, generator=g)).to(dev),
+            "answers": torch.randn(wl.N, CHOSEN, wl.h, generator=g).to(b["H"].dtype).to(dev),
+            "norm_weight": (1 + 0.2 * torch.randn(wl.h, generator=g)).to(dev)}
+
+
+def whole_step(b, l):
+    """Router, norm, the losses of `step`, and back: the gradients clipped by their global norm."""
+    N, E, h = b["router"].shape[0], b["router"].shape[1], l["residual"].shape[1]
+    f = lambda *shape, dtype=torch.float32: torch.empty(*shape, dtype=dtype, device=l["residual"].device)
+    sigmoid = sao.SAO_SCORE_SIGMOID
+
+    # forward: experts and their weights, the stream with their answers, its norm
+    route_ws, norm_ws = sao.route_workspace(N, E), sao.norm_workspace(N, h)
+    experts, weights = f(N, CHOSEN, dtype=torch.int32), f(N, CHOSEN)
+    sao.sao_route_fwd(b["router"], sigmoid, experts, weights, route_ws, bias=l["bias"], groups=4, groups_kept=2,
+                      group_score=sao.SAO_GROUP_TOP2, scale=ROUTE_SCALE)
+    answer = (weights[:, :, None] * l["answers"].float()).sum(1).to(l["residual"].dtype)
+    stream, H, rstd = torch.empty_like(answer), torch.empty_like(answer), f(N)
+    sao.sao_rms_norm_fwd(answer, l["norm_weight"], EPS, norm_ws, residual=l["residual"], sum=stream, y=H, rstd=rstd)
+
+    out = step({**b, "H": H, "experts": experts})
+
+    # backward: the stream's gradient, the norm's weight's, the router's (onto the balance loss's)
+    dH = out["dH"].to(H.dtype)
+    d_stream, d_norm = torch.empty_like(H), f(h)
+    sao.sao_rms_norm_bwd(stream, l["norm_weight"], rstd, dH, d_stream, d_norm, norm_ws)
+    d_weights = (d_stream.float()[:, None] * l["answers"].float()).sum(2)
+    balance_router, d_router = out["d_router"], out["d_router"].clone()
+    sao.sao_route_bwd(b["router"], sigmoid, experts, weights, d_weights, d_router, route_ws, scale=ROUTE_SCALE,
+                      accumulate=True)
+
+    # one step over all of them
+    grads, grad_ws = [out["dW"], d_norm, d_router], sao.grad_workspace()
+    clipped = [torch.empty_like(g) for g in grads]
+    sumsq, norm, coef = f(1, dtype=torch.float64), f(1), f(1)
+    sao.sao_grad_sumsq(grads, sumsq, grad_ws)
+    sao.sao_grad_clip(grads, sumsq, MAX_NORM, norm, coef, grad_ws, out=clipped)
+    return {**out, "experts": experts, "weights": weights, "answer": answer, "stream": stream, "H": H, "dH_rounded": dH,
+            "d_stream": d_stream, "d_weights": d_weights, "d_norm": d_norm, "balance_router": balance_router,
+            "d_router": d_router, "norm": norm, "coef": coef, "clipped": clipped}
+
+
 def main():
-    out = step(batch())
+    b = batch()
+    out = whole_step(b, layer(b))
     torch.cuda.synchronize()
     print("policy loss %.6f  distillation %.6f  balance %.6f" % (out["policy"].item(), out["distill"].item(),
                                                                out["balance"].item()))
     print("tokens per expert", out["load"].sum(0).tolist())
     print("gradient norms: hidden states %.4f  LM head %.4f  router %.6f" % tuple(
         out[k].float().norm().item() for k in ("dH", "dW", "d_router")))
+    print("global norm %.4f, clipped by %.4f" % (out["norm"].item(), out["coef"].item()))
 
 
 if __name__ == "__main__":
