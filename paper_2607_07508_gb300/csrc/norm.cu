@@ -159,7 +159,7 @@ __device__ __forceinline__ uint32_t power_of(float amax, float *inverse) {
 }
 
 template <class T, class WT, int kVec, int kLoads>
-__global__ void __launch_bounds__(kMaxThreads, kVec == 1 && kLoads > 16 ? 1 : 2) norm_fwd_kernel(NormFwd a, int warps) {
+__global__ void __launch_bounds__(kMaxThreads, kVec < 8 && kVec * kLoads == 32 ? 1 : 2) norm_fwd_kernel(NormFwd a, int warps) {
   grid_wait();
   __shared__ float slots[2 * kMaxWarps];
   Team team(warps, slots);
@@ -379,7 +379,13 @@ __global__ void __launch_bounds__(32 * kSumWarps) norm_dw_kernel(const float *pa
   dw[c] = accumulate ? dw[c] + s : s;
 }
 
-constexpr int kBwdCtas = 2 * 160;  // partials of dw, at most
+sao_status sum_parts(const NormBwd &a, const float *partial, int parts, cudaStream_t s) {
+  const int slot = launch_begin("norm_dw", s);
+  pdl(norm_dw_kernel, unsigned((a.h + 31) / 32), 32 * kSumWarps, 0, s)(partial, parts, a.h, a.dweight, a.accumulate);
+  return launch_end(slot, s);
+}
+
+constexpr int kBwdCtas = 2 * 160, kTileCtas = 6 * 160;  // partials of dw, at most
 
 // Loads a lane (each a power of two) and warps a row: f(integral constants) for the least of
 // kFew, 2 kFew .. kMost that leaves at most `wish` warps to a row.
@@ -429,8 +435,9 @@ sao_status fwd(const NormFwd &a, int sms, cudaStream_t s) {
 
 template <class T, class WT, int kVec>
 sao_status bwd(const NormBwd &a, int sms, float *partial, cudaStream_t s) {
-  constexpr int kFewLoads = kVec == 1 ? 4 : 8 / kVec, kMostLoads = 32 / kVec;
-  const int wish = a.N <= sms ? kThreads / 32 : kVec == 1 ? 4 : 1;  // (single columns: fewer lanes past the row's end)
+  constexpr int kFewLoads = kVec == 1 ? 8 : kVec == 4 ? 4 : 1, kMostLoads = 32 / kVec;
+  // many rows: 32 bf16 columns a lane, fewer fp32 or single ones, for registers
+  const int wish = a.N <= sms ? kThreads / 32 : kVec < 8 ? kMaxWarps : 1;
   const Shape p = shape_of(a.h, kVec, kFewLoads, kMostLoads, wish);
   const int teams = teams_of(p.warps);
   int64_t grid = (a.N + teams - 1) / teams;
@@ -443,11 +450,7 @@ sao_status bwd(const NormBwd &a, int sms, float *partial, cudaStream_t s) {
           teams > 1 ? size_t(a.h) * sizeof(float) : 0, s)(a, p.warps, a.dweight ? partial : nullptr);
   });
   SAO_TRY(launch_end(slot, s));
-  if (!a.dweight) return SAO_OK;
-  const int sum_slot = launch_begin("norm_dw", s);
-  pdl(norm_dw_kernel, unsigned((a.h + 31) / 32), 32 * kSumWarps, 0, s)(partial, int(grid), a.h, a.dweight,
-                                                                       a.accumulate);
-  return launch_end(sum_slot, s);
+  return a.dweight ? sum_parts(a, partial, int(grid), s) : SAO_OK;
 }
 
 // f(type of the arrays, of the weight, columns of a load)
@@ -465,10 +468,19 @@ sao_status by_types(sao_dtype dt, sao_dtype w_dt, bool wide, F f) {
   return wide ? f(float(), float(), Wide32()) : f(float(), float(), One());
 }
 
+// Whether rows go by tiles: those that leave most of a warp idle, and in the forward those that are no whole vectors,
+// but for fp32 ones of up to 1,024 columns. (Forward by tiles and by single columns: 300,000 x 20 bf16 21 and 93 us,
+// 4,099 x 515 9 and 13.5, in fp32 16 and 13.5, 20,001 x 4,099 190 and 256, in fp32 269 and 322. Backward: 300,000 x 20
+// 34 and 121; it reads its tiles three times, 60,001 x 1,001 318 and 181.)
+bool short_rows(int h, sao_dtype dt) { return h * (dt == SAO_BF16 ? 2 : 4) <= 256; }
+bool fwd_by_tiles(int h, sao_dtype dt, bool wide) {
+  return short_rows(h, dt) || (!wide && (dt == SAO_BF16 || h > 1024));
+}
+
 }  // namespace
 
 size_t norm_ws_bytes(int64_t N, int32_t h) {
-  const int64_t parts = N < kBwdCtas ? N : kBwdCtas;
+  const int64_t parts = N < kTileCtas ? N : kTileCtas;
   return round256(size_t(parts) * size_t(h) * sizeof(float));
 }
 
@@ -477,6 +489,8 @@ sao_status norm_fwd_launch(const NormFwd &a, sao_dtype dt, sao_dtype w_dt, cudaS
   SAO_TRY(device_info(&di));
   const bool wide = a.h % (dt == SAO_BF16 ? 8 : 4) == 0 && aligned16(a.x) && aligned16(a.residual) &&
                     aligned16(a.sum) && aligned16(a.y) && aligned16(a.weight) && aligned16(a.y8);
+  const bool tiles = aligned16(a.x) && aligned16(a.residual) && aligned16(a.sum) && aligned16(a.y) && a.y8 == nullptr;
+  if (tiles && fwd_by_tiles(a.h, dt, wide)) return norm_fwd_tiles_launch(a, dt, w_dt, s);
   return by_types(dt, w_dt, wide, [&](auto t, auto w, auto vec) {
     return fwd<decltype(t), decltype(w), decltype(vec)::value>(a, di.sm_count, s);
   });
@@ -486,10 +500,16 @@ sao_status norm_bwd_launch(const NormBwd &a, sao_dtype dt, sao_dtype w_dt, void 
   DeviceInfo di;
   SAO_TRY(device_info(&di));
   Carver c(ws, ws_bytes);
-  float *partial = c.take<float>(size_t(a.N < kBwdCtas ? a.N : kBwdCtas) * size_t(a.h));
+  float *partial = c.take<float>(size_t(a.N < kTileCtas ? a.N : kTileCtas) * size_t(a.h));
   if (a.dweight && !c.ok()) return fail(SAO_ERR_WORKSPACE, "workspace of the norm's backward too small");
   const bool wide = a.h % (dt == SAO_BF16 ? 8 : 4) == 0 && aligned16(a.x) && aligned16(a.dy) && aligned16(a.dsum) &&
                     aligned16(a.dx) && aligned16(a.weight);
+  if (aligned16(a.x) && aligned16(a.dy) && aligned16(a.dsum) && aligned16(a.dx) && short_rows(a.h, dt)) {
+    int parts;
+    const int most = 6 * di.sm_count < kTileCtas ? 6 * di.sm_count : kTileCtas;
+    SAO_TRY(norm_bwd_tiles_launch(a, dt, w_dt, partial, int(a.N < most ? a.N : most), &parts, s));
+    return a.dweight ? sum_parts(a, partial, parts, s) : SAO_OK;
+  }
   return by_types(dt, w_dt, wide, [&](auto t, auto w, auto vec) {
     return bwd<decltype(t), decltype(w), decltype(vec)::value>(a, di.sm_count, partial, s);
   });
