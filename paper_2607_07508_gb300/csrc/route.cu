@@ -281,6 +281,8 @@ __global__ void __launch_bounds__(kWarps * 32, kPer <= 4 ? 5 : kPer <= 8 ? 3 : 1
     if (!a.replay && (!kExact || doubt != 0u)) {
       // (a row that ran out of experts may only have run out of distances below inf)
       bool near = scores && ((doubt >> mine & 1u) || (!kExact && id < 0));
+      float b_pick = 0.f;
+      float window = -1.f;  // the last choice and the key behind it are of one logit and bias: how far about to look
       if (!kExact) {
         uint32_t after = __shfl_down_sync(kAll, pick, 1);
         float x_after = __shfl_down_sync(kAll, chosen, 1);
@@ -289,19 +291,41 @@ __global__ void __launch_bounds__(kWarps * 32, kPer <= 4 ? 5 : kPer <= 8 ? 3 : 1
           x_after = after > none && id >= 0 ? value(from + int(mask - (after & mask))) : 0.f;
         }
         if (id >= 0 && after > none) {
+          const float d = __uint_as_float((~pick & ~mask) >> 1), d_after = __uint_as_float((~after & ~mask) >> 1);
+          float error = 0x1p-23f * float(mask + 2u) * d_after;
           bool apart = (pick & ~mask) > (after & ~mask), same = chosen == x_after;
           if (kBiased) {
-            const float b_pick = ld(a.bias + id), b_after = ld(a.bias + int(mask - (after & mask)));
-            const float d = __uint_as_float((~pick & ~mask) >> 1), d_after = __uint_as_float((~after & ~mask) >> 1);
-            const float size = 2.f + fabsf(b_pick) + fabsf(b_after) + float(mask + 2u) * d_after;
-            const float error = (soft ? kDoubtSoftmax / total : kDoubtSigmoid) + 0x1p-23f * size;
+            b_pick = ld(a.bias + id);
+            const float b_after = ld(a.bias + int(mask - (after & mask)));
+            error += (soft ? kDoubtSoftmax / total : kDoubtSigmoid) + 0x1p-23f * (2.f + fabsf(b_pick) + fabsf(b_after));
             apart = d_after - d > error;
             same &= b_pick == b_after;
           }
           near |= !apart && !same;
+          if (j == a.k - 1 && !apart && same) window = 2.f * error;
         }
       }
       unsigned again = __ballot_sync(kAll, near);
+      // equal ones go by their index, unless some other key is as near to them
+      unsigned equal = __ballot_sync(kAll, window >= 0.f);
+      while (equal != 0u) {
+        const int at = __ffs(equal) - 1;
+        equal &= equal - 1u;
+        const float x_last = __shfl_sync(kAll, chosen, at), b_last = __shfl_sync(kAll, b_pick, at);
+        const float reach = __shfl_sync(kAll, window, at), its_peak = __shfl_sync(kAll, peak, at);
+        const float its_total = __shfl_sync(kAll, total, at);
+        const auto key_of = [&](float x, float b) {
+          return !kBiased ? x : (soft ? exp_fast(x - its_peak) / its_total : sigmoid_fast(x)) + b;
+        };
+        const T *its_row = static_cast<const T *>(a.x) + (row0 + at / a.k) * a.E;
+        const float last = key_of(x_last, b_last);
+        bool other = false;
+        for (int e = lane; e < a.E; e += 32) {
+          const float x = value(its_row + e), b = kBiased ? ld(a.bias + e) : 0.f;
+          other |= fabsf(key_of(x, b) - last) <= reach && !(x == x_last && b == b_last);
+        }
+        if (__any_sync(kAll, other)) again |= 1u << at;
+      }
       while (again != 0u) {
         const int r = (__ffs(again) - 1) / a.k;
         const T *its_row = static_cast<const T *>(a.x) + (row0 + r) * a.E;

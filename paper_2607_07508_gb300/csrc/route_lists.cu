@@ -60,37 +60,59 @@ struct ListPlan {
 constexpr uint32_t kFractionMask = 511u;  // of a fraction: its 23 bits fill the others
 constexpr float kFractionLeast = 1.f + 0x1p-10f;
 
-// Eight logits from p on, `n` of them there (others: -inf).
+// Eight logits from p on as they lie in memory, `n` of them there (others: -inf).
 template <class T>
-__device__ __forceinline__ void load8(const T *p, int n, int unit, float (&x)[8]) {
-  constexpr int kSize = int(sizeof(T));
-  const auto put = [&](int at, uint32_t w) {
-    if constexpr (kSize == 4)
-      x[at] = __uint_as_float(w);
-    else
-      x[at] = __uint_as_float(w << 16), x[at + 1] = __uint_as_float(w & 0xffff0000u);
-  };
-  if (unit == 16 && n >= 8) {
+struct Block {
+  static constexpr int kSize = int(sizeof(T)), kWords = 2 * kSize;
+  uint32_t w[kWords];
+  __device__ __forceinline__ void load(const T *p, int n, int unit) {
+    if (unit == 16 && n >= 8) {
 #pragma unroll
-    for (int i = 0; i < 8; i += 16 / kSize) {
-      const uint4 v = ld(reinterpret_cast<const uint4 *>(p + i));
-      put(i, v.x), put(i + 4 / kSize, v.y), put(i + 8 / kSize, v.z), put(i + 12 / kSize, v.w);
-    }
-  } else if (unit >= 8) {
+      for (int i = 0; i < kWords; i += 4) {
+        const uint4 v = ld(reinterpret_cast<const uint4 *>(p) + i / 4);
+        w[i] = v.x, w[i + 1] = v.y, w[i + 2] = v.z, w[i + 3] = v.w;
+      }
+    } else if (unit >= 8 && (n >= 8 || n * kSize % 8 == 0)) {
+      constexpr uint32_t kNone = kSize == 4 ? 0xff800000u : 0xff80ff80u;
 #pragma unroll
-    for (int i = 0; i < 8; i += 8 / kSize) {
-      if (i + 8 / kSize <= n) {
-        const uint2 v = ld(reinterpret_cast<const uint2 *>(p + i));
-        put(i, v.x), put(i + 4 / kSize, v.y);
-      } else {
+      for (int i = 0; i < kWords; i += 2) {
+        uint2 v = make_uint2(kNone, kNone);
+        if ((i + 2) * 4 <= n * kSize) v = ld(reinterpret_cast<const uint2 *>(p) + i / 2);
+        w[i] = v.x, w[i + 1] = v.y;
+      }
+    } else {
 #pragma unroll
-        for (int j = 0; j < 8 / kSize; ++j) x[i + j] = i + j < n ? value(p + i + j) : -INFINITY;
+      for (int i = 0; i < 8; ++i) {
+        if constexpr (kSize == 4) {
+          w[i] = i < n ? ld(reinterpret_cast<const uint32_t *>(p) + i) : 0xff800000u;
+        } else {
+          const uint32_t u = i < n ? ld(reinterpret_cast<const uint16_t *>(p) + i) : 0xff80u;
+          w[i / 2] = i & 1 ? w[i / 2] | u << 16 : u;
+        }
       }
     }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = i < n ? value(p + i) : -INFINITY;
   }
+  __device__ __forceinline__ float at(int i) const {
+    if constexpr (kSize == 4) return __uint_as_float(w[i]);
+    return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+  }
+};
+
+// The packed keys of a block of bf16 logits, the first of which has index `low` (the next ones lower): two at a time.
+__device__ __forceinline__ void pack(const Block<__nv_bfloat16> &x, uint32_t low, uint32_t, uint32_t (&p)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 zero = __floats2bfloat162_rn(0.f, 0.f);
+    const __nv_bfloat162 sum = __hadd2(*reinterpret_cast<const __nv_bfloat162 *>(&x.w[i]), zero);  // (-0: 0)
+    uint32_t u = *reinterpret_cast<const uint32_t *>(&sum);
+    u ^= (u >> 15 & 0x00010001u) * 0x7fffu + 0x80008000u;  // both halves in the order of integers
+    p[2 * i] = u * 0x10000u + (low - 2 * i);
+    p[2 * i + 1] = (u & 0xffff0000u) + (low - 2 * i - 1);
+  }
+}
+__device__ __forceinline__ void pack(const Block<float> &x, uint32_t low, uint32_t mask, uint32_t (&p)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) p[i] = (ordered(x.at(i) + 0.f) & ~mask) + (low - i);
 }
 
 // Over the kShare lanes of a row.
@@ -129,8 +151,8 @@ __global__ void __launch_bounds__(kListWarps * 32)
     // a key is (s + b - least) units + 1 + 2^-10: in [1, 2), with room for its errors
     units = (1.f - 0x1p-9f) / (1.f + (high - low));
     all_exactly = most == INFINITY || !(units >= 0x1p-20f);  // biases that leave no digits to scores
-    for (int e = threadIdx.x; e < a.E; e += kListWarps * 32) {
-      const float b = ld(a.bias + e);
+    for (int e = threadIdx.x; e < 512; e += kListWarps * 32) {
+      const float b = e < a.E ? ld(a.bias + e) : -INFINITY;
       offset[e] = fabsf(b) < INFINITY ? fmaf(b - low, units, kFractionLeast) : -INFINITY;
     }
     __syncthreads();
@@ -142,12 +164,12 @@ __global__ void __launch_bounds__(kListWarps * 32)
   const int e0 = s / l.share * l.size + s % l.share * plan.per;
   int n = l.size - s % l.share * plan.per;
   n = n < plan.per ? (n > 0 ? n : 0) : plan.per;
-  const auto packed = [&](float x, int e, bool there) {
+  const auto packed = [&](float x, int e) {  // as the blocks below, one expert
     if (kBiased) {
-      const float f = fmaf(sigmoid_fast(x), units, there ? offset[e] : -INFINITY);
+      const float f = fmaf(sigmoid_fast(x), units, offset[e]);
       return f >= 1.f && x > -INFINITY ? __float_as_uint(f) << 9 | (kFractionMask - e) : 0u;
     }
-    return (ordered(x + 0.f) & ~mask) | ((mask - e) & mask);  // -0 and 0 are one key; -inf comes to `none` or less
+    return (ordered(x + 0.f) & ~mask) | (mask - e);  // -0 and 0 are one key; -inf comes to `none` or less
   };
   const int64_t step = int64_t(gridDim.x) * kListWarps * kRows;
   for (int64_t row0 = (int64_t(blockIdx.x) * kListWarps + warp) * kRows; row0 < a.N; row0 += step) {
@@ -160,19 +182,40 @@ __global__ void __launch_bounds__(kListWarps * 32)
     }
     const T *logits = static_cast<const T *>(a.x) + (real ? row : a.N - 1) * a.E, *from = logits + e0;
     uint32_t v[8], rest = 0u;
-    float probe = 0.f;
+    bool odd = false;  // perhaps an infinity or a NaN
 #pragma unroll 1
     for (int block = 0; block < plan.blocks; ++block) {
-      const int here = on ? n - block * 8 : 0;
-      float x[8];
-      load8(from + block * 8, here, plan.unit, x);
+      const int here = on ? n - block * 8 : 0, e = e0 + block * 8;
+      Block<T> x;
+      x.load(from + block * 8, here, plan.unit);
       uint32_t w[8];
+      if constexpr (kBiased) {
+        float probe = 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        probe = fmaf(i < here ? x[i] : 0.f, 0.f, probe);
-        w[i] = packed(x[i], e0 + block * 8 + i, i < here);
+        for (int i = 0; i < 8; ++i) {
+          probe = fmaf(x.at(i), 0.f, probe);
+          // (1: an expert that is out, as is one of a NaN)
+          const float f = fmaxf(fmaf(sigmoid_fast(x.at(i)), units, offset[e + i]), 1.f);
+          w[i] = __float_as_uint(f) * 512u + (kFractionMask - e - i);
+        }
+        if (probe != 0.f) {  // (places past the last expert are -inf too)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            if (!(x.at(i) > -INFINITY)) w[i] = 0u;
+            odd |= i < here && !(fabsf(x.at(i)) < INFINITY);
+          }
+        }
+        sort8(w);
+      } else {
+        pack(x, mask - e, mask, w);
+        sort8(w);
+        if (here >= 8) {
+          odd |= w[0] >= (0xff800000u & ~mask) || w[7] <= none;
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) odd |= i < here && !(fabsf(x.at(i)) < INFINITY);
+        }
       }
-      sort8(w);
       if (block == 0) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = w[i];
@@ -181,7 +224,7 @@ __global__ void __launch_bounds__(kListWarps * 32)
       }
     }
     bool scores = on;
-    if (__any_sync(kAll, probe != 0.f)) {  // an infinity or a NaN
+    if (__any_sync(kAll, on && odd)) {
       bool bad = false;
       for (int i = 0; i < (on ? n : 0); ++i) {
         const float x = value(from + i);
@@ -205,6 +248,12 @@ __global__ void __launch_bounds__(kListWarps * 32)
       for (int o = l.share; o < kShare; o <<= 1) first = max(first, __shfl_xor_sync(kAll, first, o));
       if (first > none) top = value(logits + (mask - (first & mask)));
     }
+    // whether two keys, the first of them not the smaller one, may be in another order than their exact values
+    const auto near = [&](uint32_t p, uint32_t q) {
+      if (kExact) return false;
+      return p > none && q > none && (kBiased ? (p >> 9) - (q >> 9) <= apart : ((p ^ q) & ~mask) == 0u);
+    };
+    const auto exactly = [&](float x, float b) { return kBiased ? sigmoid(double(x)) + double(b) : double(x); };
     bool again = all_exactly, stays = true;  // again: choose_exactly
     if (l.groups > 1) {
       const bool one = v[0] > none, both = v[1] > none;
@@ -239,19 +288,37 @@ __global__ void __launch_bounds__(kListWarps * 32)
                             : a.two ? 0x1p-18f
                                     : 0.f;
         const bool doubt = highest > -INFINITY && !(lowest - highest > error);
-        if (__any_sync(kAll, doubt)) {
-          // groups about the border of the same logits and biases are equal, and in their order
+        if (__any_sync(kAll, doubt)) {  // ranked again by fp64, a group's best one or two being certain
           const int id0 = one ? int(mask - (v[0] & mask)) : -1, id1 = a.two && both ? int(mask - (v[1] & mask)) : -1;
-          const float x0 = id0 >= 0 ? value(logits + id0) : 0.f, x1 = id1 >= 0 ? value(logits + id1) : -INFINITY;
+          const float x0 = id0 >= 0 ? value(logits + id0) : 0.f, x1 = id1 >= 0 ? value(logits + id1) : 0.f;
           const float b0 = kBiased && id0 >= 0 ? ld(a.bias + id0) : 0.f;
           const float b1 = kBiased && id1 >= 0 ? ld(a.bias + id1) : 0.f;
+          const auto term = [&](float x, float b) {
+            if (kBiased || !a.two) return exactly(x, b);
+            return soft ? exp(double(x) - double(top)) : sigmoid(double(x));
+          };
+          const double fine = one ? term(x0, b0) + (id1 >= 0 ? term(x1, b1) : 0.0) : -INFINITY;
           const bool border = fabsf(worth - lowest) <= 2.f * error || fabsf(worth - highest) <= 2.f * error;
-          const int at = base + __ffs(__ballot_sync(kAll, rank == a.kept - 1) >> base & 0xffu) - 1;
-          // (every lane shuffles: none of this behind an &&)
-          const float its_x0 = __shfl_sync(kAll, x0, at), its_x1 = __shfl_sync(kAll, x1, at);
-          const float its_b0 = __shfl_sync(kAll, b0, at), its_b1 = __shfl_sync(kAll, b1, at);
-          const bool same = x0 == its_x0 && x1 == its_x1 && b0 == its_b0 && b1 == its_b1;
-          again |= row_any(doubt && border && !same);
+          // uncertain: keys about the last of those, unless they are of one logit and bias
+          const uint32_t least_of = a.two ? v[1] : v[0];
+          const float x_of = a.two ? x1 : x0, b_of = a.two ? b1 : b0;
+          const bool unsure = doubt && border && near(least_of, a.two ? v[2] : v[1]);
+          if (__any_sync(kAll, unsure)) {
+            int mixed = 0;
+            for (int i = 0; i < (unsure ? n : 0); ++i) {
+              const float x = value(from + i);
+              const uint32_t p = packed(x, e0 + i);
+              if (!(p > none && (p > least_of ? near(p, least_of) : near(least_of, p)))) continue;
+              mixed |= !(x == x_of && (!kBiased || ld(a.bias + e0 + i) == b_of));
+            }
+            again |= row_any(mixed != 0);
+          }
+          rank = 0;
+          for (int o = l.share; o < kShare; o += l.share) {
+            const double other = __shfl_xor_sync(kAll, fine, o);
+            rank += other > fine || (other == fine && (s ^ o) < s);
+          }
+          if (doubt) stays = rank < a.kept;
         }
       }
       if (!stays) {
@@ -273,42 +340,57 @@ __global__ void __launch_bounds__(kListWarps * 32)
     int id = scores && s < a.k && pick > none ? int(mask - (pick & mask)) : -1;
     float chosen = id >= 0 ? value(logits + id) : -INFINITY;
     if (!kExact) {
-      const auto near = [&](uint32_t p, uint32_t q) {
-        return p > none && q > none && (kBiased ? (p >> 9) - (q >> 9) <= apart : ((p ^ q) & ~mask) == 0u);
-      };
       const float bias = kBiased && id >= 0 ? ld(a.bias + id) : 0.f;
       // picks among one another
       const uint32_t after = __shfl_down_sync(kAll, pick, 1);
       const float x_after = __shfl_down_sync(kAll, chosen, 1), b_after = __shfl_down_sync(kAll, bias, 1);
       const bool swap = id >= 0 && s < a.k - 1 && near(pick, after) && !(chosen == x_after && bias == b_after);
-      if (__any_sync(kAll, swap)) {
-        double key = -INFINITY;
-        if (id >= 0) key = kBiased ? sigmoid(double(chosen)) + double(bias) : double(chosen);
-        int rank = 0;
-        for (int o = 1; o < kShare; ++o) {
-          const double other = __shfl_xor_sync(kAll, key, o);
-          const int its = __shfl_xor_sync(kAll, id, o);
-          rank += other > key || (other == key && (id < 0 ? (s ^ o) < s : its >= 0 && its < id));
-        }
-        int source = lane;
-        for (int i = 0; i < kShare; ++i)
-          if (__shfl_sync(kAll, rank, base + i) == s) source = base + i;
-        id = __shfl_sync(kAll, id, source);
-        chosen = __shfl_sync(kAll, chosen, source);
-      }
-      // the last one and what was left out: in doubt unless all keys about it are of one logit and bias
+      // the last one and what was left out: nothing to do if all keys about it are of one logit and bias
       const bool border = scores && near(last, next);
+      bool compare = false;  // the one key left out that is about the last one may have to be a pick
       if (__any_sync(kAll, border)) {
         const int at = int(mask - (last & mask));
         const float x_last = border ? value(logits + at) : 0.f, b_last = kBiased && border ? ld(a.bias + at) : 0.f;
         bool mixed = false;
+        int left = 0;
         for (int i = 0; i < (border && stays ? n : 0); ++i) {
           const float x = value(from + i);
-          const uint32_t p = packed(x, e0 + i, true);
-          const bool about = p > none && (p > last ? near(p, last) : near(last, p));
-          mixed |= about && !(x == x_last && (!kBiased || ld(a.bias + e0 + i) == b_last));
+          const uint32_t p = packed(x, e0 + i);
+          if (!(p > none && (p > last ? near(p, last) : near(last, p)))) continue;
+          left += p < last;
+          mixed |= !(x == x_last && (!kBiased || ld(a.bias + e0 + i) == b_last));
         }
-        again |= row_any(mixed);
+        for (int o = 1; o < kShare; o <<= 1) left += __shfl_xor_sync(kAll, left, o);
+        mixed = row_any(mixed);
+        compare = mixed && left == 1;
+        again |= mixed && left != 1;
+      }
+      if (__any_sync(kAll, swap || compare)) {
+        double key = id >= 0 ? exactly(chosen, bias) : -INFINITY;
+        const auto rank_of = [&] {
+          int rank = 0;
+          for (int o = 1; o < kShare; ++o) {
+            const double other = __shfl_xor_sync(kAll, key, o);
+            const int its = __shfl_xor_sync(kAll, id, o);
+            rank += other > key || (other == key && (id < 0 ? (s ^ o) < s : its >= 0 && its < id));
+          }
+          return rank;
+        };
+        int rank = rank_of();
+        if (__any_sync(kAll, compare)) {
+          const int its = compare ? int(mask - (next & mask)) : 0;
+          const float x = compare ? value(logits + its) : 0.f, b = kBiased && compare ? ld(a.bias + its) : 0.f;
+          const double k = exactly(x, b);
+          if (compare && rank == a.k - 1 && (k > key || (k == key && its < id))) id = its, chosen = x, key = k;
+          rank = rank_of();
+        }
+        int source = lane;
+        for (int i = 0; i < kShare; ++i) {
+          const int its = __shfl_sync(kAll, rank, base + i);
+          if (its == s) source = base + i;
+        }
+        id = __shfl_sync(kAll, id, source);
+        chosen = __shfl_sync(kAll, chosen, source);
       }
     }
     unsigned todo = __ballot_sync(kAll, again && scores);
@@ -361,12 +443,17 @@ sao_status route_lists_launch(const RouteArgs &a, const Lanes &l32, sao_dtype dt
   ListPlan p{};
   p.per = (l.size + l.share - 1) / l.share;
   p.blocks = (p.per + 7) / 8;
-  while (p.mask < unsigned(a.E) - 1u) p.mask = 2 * p.mask + 1u;
+  // (the last lane's blocks may reach past the last expert: 511 at most)
+  const int e_most = (kShare - 1) / l.share * l.size + (kShare - 1) % l.share * p.per + p.blocks * 8 - 1;
+  while (p.mask < unsigned(e_most)) p.mask = 2 * p.mask + 1u;
   p.unit = 16;  // where rows, groups and lanes start on it
   while (p.unit >= 8 && (reinterpret_cast<uintptr_t>(a.x) % p.unit != 0 || a.E * size % p.unit != 0 ||
                          l.size * size % p.unit != 0 || (l.share > 1 && p.per * size % p.unit != 0)))
     p.unit /= 2;
-  const int64_t grid = least((a.N + kRows * kListWarps - 1) / (kRows * kListWarps), int64_t(sms) * 16);
+  // as many CTAs as there is work for, or, with a bias to set up, few that take equal shares
+  const int64_t tiles = (a.N + kRows * kListWarps - 1) / (kRows * kListWarps);
+  const int64_t most = int64_t(sms) * (a.bias ? 6 : 128), turns = (tiles + most - 1) / most;
+  const int64_t grid = (tiles + turns - 1) / turns;
   const int slot = launch_begin("route_lists", s);
   const auto launch = [&](auto kernel) { pdl(kernel, unsigned(grid), kListWarps * 32, 0, s)(a, l, l32, p); };
   const bool rest = a.k == kList;

@@ -165,6 +165,26 @@ def test_many_tokens_with_equal_and_near_keys(score, groups, kept, two, k):
         check(rows, k, score, b, groups=groups, kept=kept, two=two, train=False)
 
 
+@pytest.mark.parametrize("k", [1, 3, 4, 7, 8])
+@pytest.mark.parametrize("groups,kept,two", [(1, 1, False), (4, 3, False), (8, 5, True)])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("N", [900, 4000])
+def test_experts_in_pairs(N, score, groups, kept, two, k):
+    """Experts in pairs, or threes, whose logits differ by a few of their last bits, one or the other of them the larger:
+    the last choice falls between such, or within a group that is such a copy of another."""
+    E = 96
+    g = torch.Generator().manual_seed(k)
+    for copies in (2, 3):
+        x = (torch.randn(N, E // copies, generator=g) * 1.5).cuda().repeat(1, copies)
+        x = (x.view(torch.int32) + torch.randint(-6, 7, (N, E), generator=g, dtype=torch.int32).cuda()).view(torch.float32)
+        bias = _bias(E // copies, seed=copies).repeat(copies)
+        order = torch.randperm(E, generator=g).cuda()
+        for b in (None, bias):
+            check(x.contiguous(), k, score, b, groups=groups, kept=kept, two=two, train=False)
+            check(x[:, order].contiguous(), k, score, None if b is None else b[order].contiguous(), groups=groups, kept=kept,
+                  two=two, train=False)
+
+
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("groups,kept", [(1, 1), (4, 2)])
