@@ -363,15 +363,17 @@ __global__ void __launch_bounds__(kMaxThreads) norm_bwd_kernel(NormBwd a, int wa
 }
 
 // dw = (dw +) the partials' sums: 32 columns to a CTA, its warps side by side in the partials.
-constexpr int kSumWarps = 16;
+constexpr int kSumWarps = 32;
 __global__ void __launch_bounds__(32 * kSumWarps) norm_dw_kernel(const float *partial, int parts, int h, float *dw,
                                                                  int accumulate) {
   grid_wait();
   __shared__ float warp_sum[kSumWarps][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, c = blockIdx.x * 32 + lane;
   float s = 0.f;
-  if (c < h)
+  if (c < h) {
+#pragma unroll 8
     for (int p = warp; p < parts; p += kSumWarps) s += ld(partial + int64_t(p) * h + c);
+  }
   warp_sum[warp][lane] = s;
   __syncthreads();
   if (warp != 0 || c >= h) return;
@@ -441,7 +443,9 @@ sao_status bwd(const NormBwd &a, int sms, float *partial, cudaStream_t s) {
   const Shape p = shape_of(a.h, kVec, kFewLoads, kMostLoads, wish);
   const int teams = teams_of(p.warps);
   int64_t grid = (a.N + teams - 1) / teams;
-  const int most = 2 * sms < kBwdCtas ? 2 * sms : kBwdCtas;
+  // (few single columns: few registers, and few loads in flight without the warps)
+  const bool light = kVec == 1 && p.loads <= 8;
+  const int most = light ? (6 * sms < kTileCtas ? 6 * sms : kTileCtas) : 2 * sms < kBwdCtas ? 2 * sms : kBwdCtas;
   grid = grid < most ? grid : most;
   const int slot = launch_begin("norm_bwd", s);
   by_loads(p.loads, [&](auto loads) {
@@ -468,14 +472,12 @@ sao_status by_types(sao_dtype dt, sao_dtype w_dt, bool wide, F f) {
   return wide ? f(float(), float(), Wide32()) : f(float(), float(), One());
 }
 
-// Whether rows go by tiles: those that leave most of a warp idle, and in the forward those that are no whole vectors,
-// but for fp32 ones of up to 1,024 columns. (Forward by tiles and by single columns: 300,000 x 20 bf16 21 and 93 us,
-// 4,099 x 515 9 and 13.5, in fp32 16 and 13.5, 20,001 x 4,099 190 and 256, in fp32 269 and 322. Backward: 300,000 x 20
-// 34 and 121; it reads its tiles three times, 60,001 x 1,001 318 and 181.)
-bool short_rows(int h, sao_dtype dt) { return h * (dt == SAO_BF16 ? 2 : 4) <= 256; }
-bool fwd_by_tiles(int h, sao_dtype dt, bool wide) {
-  return short_rows(h, dt) || (!wide && (dt == SAO_BF16 || h > 1024));
-}
+// Whether rows go by tiles: short ones, which leave most of a warp idle, and in the forward those that are no whole
+// vectors, but for fp32 ones of up to 1,024 columns. (Forward by tiles and else: 300,000 x 20 bf16 21 and 93 us, 400,003 x
+// 64 76 and 113, x 128 142 and 118; 4,099 x 515 9 and 13.5, in fp32 16 and 14, 20,001 x 4,099 190 and 256, in fp32 270 and
+// 322. Backward: 300,000 x 20 34 and 111, 400,003 x 64 140 and 161, x 77 192 and 171; it reads its tiles three times.)
+constexpr int kShortRow = 64;
+bool fwd_by_tiles(int h, sao_dtype dt, bool wide) { return h <= kShortRow || (!wide && (dt == SAO_BF16 || h > 1024)); }
 
 }  // namespace
 
@@ -504,7 +506,7 @@ sao_status norm_bwd_launch(const NormBwd &a, sao_dtype dt, sao_dtype w_dt, void 
   if (a.dweight && !c.ok()) return fail(SAO_ERR_WORKSPACE, "workspace of the norm's backward too small");
   const bool wide = a.h % (dt == SAO_BF16 ? 8 : 4) == 0 && aligned16(a.x) && aligned16(a.dy) && aligned16(a.dsum) &&
                     aligned16(a.dx) && aligned16(a.weight);
-  if (aligned16(a.x) && aligned16(a.dy) && aligned16(a.dsum) && aligned16(a.dx) && short_rows(a.h, dt)) {
+  if (aligned16(a.x) && aligned16(a.dy) && aligned16(a.dsum) && aligned16(a.dx) && a.h <= kShortRow) {
     int parts;
     const int most = 6 * di.sm_count < kTileCtas ? 6 * di.sm_count : kTileCtas;
     SAO_TRY(norm_bwd_tiles_launch(a, dt, w_dt, partial, int(a.N < most ? a.N : most), &parts, s));
