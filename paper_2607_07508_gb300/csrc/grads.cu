@@ -262,8 +262,9 @@ __device__ __forceinline__ void chunk_scale(const void *src, void *dst, int n, f
 }
 
 template <int kCap>
-__global__ void __launch_bounds__(kClipThreads, 2) clip_kernel(const __grid_constant__ List<kCap> l, const double *sumsq,
-                                                        float max_norm, int in_place, float *norm, float *coef) {
+__global__ void __launch_bounds__(kClipThreads, 2)
+    clip_kernel(const __grid_constant__ List<kCap> l, const double *sumsq, float max_norm, int in_place, float *norm,
+                float *coef) {
   grid_wait();
   __shared__ float factor;
   if (threadIdx.x == 0) {

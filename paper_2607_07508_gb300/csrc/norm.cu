@@ -159,7 +159,8 @@ __device__ __forceinline__ uint32_t power_of(float amax, float *inverse) {
 }
 
 template <class T, class WT, int kVec, int kLoads>
-__global__ void __launch_bounds__(kMaxThreads, kVec < 8 && kVec * kLoads == 32 ? 1 : 2) norm_fwd_kernel(NormFwd a, int warps) {
+__global__ void __launch_bounds__(kMaxThreads, kVec < 8 && kVec * kLoads == 32 ? 1 : 2)
+    norm_fwd_kernel(NormFwd a, int warps) {
   grid_wait();
   __shared__ float slots[2 * kMaxWarps];
   Team team(warps, slots);
@@ -472,10 +473,11 @@ sao_status by_types(sao_dtype dt, sao_dtype w_dt, bool wide, F f) {
   return wide ? f(float(), float(), Wide32()) : f(float(), float(), One());
 }
 
-// Whether rows go by tiles: short ones, which leave most of a warp idle, and in the forward those that are no whole
-// vectors, but for fp32 ones of up to 1,024 columns. (Forward by tiles and else: 300,000 x 20 bf16 21 and 93 us, 400,003 x
-// 64 76 and 113, x 128 142 and 118; 4,099 x 515 9 and 13.5, in fp32 16 and 14, 20,001 x 4,099 190 and 256, in fp32 270 and
-// 322. Backward: 300,000 x 20 34 and 111, 400,003 x 64 140 and 161, x 77 192 and 171; it reads its tiles three times.)
+// Whether rows go by tiles: short ones, which leave most of a warp idle, and in the forward those that are no
+// whole vectors, but for fp32 ones of up to 1,024 columns. (Forward by tiles and else: 300,000 x 20 bf16 21 and 93
+// us, 400,003 x 64 76 and 113, x 128 142 and 118; 4,099 x 515 9 and 13.5, in fp32 16 and 14, 20,001 x 4,099 190
+// and 256, in fp32 270 and 322. Backward: 300,000 x 20 34 and 111, 400,003 x 64 140 and 161, x 77 192 and 171; it
+// reads its tiles three times.)
 constexpr int kShortRow = 64;
 bool fwd_by_tiles(int h, sao_dtype dt, bool wide) { return h <= kShortRow || (!wide && (dt == SAO_BF16 || h > 1024)); }
 

@@ -1,4 +1,5 @@
-// Root-mean-square norm of rows that are no whole number of 16-byte vectors, or short: by tiles of rows in shared memory.
+// Root-mean-square norm of rows that are no whole number of 16-byte vectors, or short: by tiles of rows in shared
+// memory.
 //
 // Rows lie one after another, so a tile of them is one run of memory, whatever their length: it is loaded and stored by
 // vectors (but for its first and last few elements), every lane busy, and only shared memory is read column by column,
@@ -34,9 +35,9 @@ struct TilePlan {
   int bytes;  // of a tile, with room for what its alignment leaves in front and behind
 };
 
-// The elements [from, from + count) of an array and a tile that holds them: the tile's first vector is the one of memory
-// that holds element `from`, so that vectors of both lie on 16 bytes. f(at, vector) with the tile's vectors, one(i) with
-// single elements of the tile.
+// The elements [from, from + count) of an array and a tile that holds them: the tile's first vector is the one of
+// memory that holds element `from`, so that vectors of both lie on 16 bytes. f(at, vector) with the tile's
+// vectors, one(i) with single elements of the tile.
 template <class T, class Vector, class One>
 __device__ __forceinline__ void flat(int64_t from, int count, Vector vector, One one) {
   constexpr int kVec = 16 / int(sizeof(T)), kBatch = 4;
@@ -195,8 +196,9 @@ __global__ void __launch_bounds__(kThreads, 4) norm_fwd_tiles(const __grid_const
   }
 }
 
-// A CTA's sums for dw go to row blockIdx.x of `partial`. Shared memory: the tiles of the stream and of dy, then sums for
-// dw (kThreads / h of each column where rows are shorter than that), then each row's rstd and factor of the stream.
+// A CTA's sums for dw go to row blockIdx.x of `partial`. Shared memory: the tiles of the stream and of dy, then
+// sums for dw (kThreads / h of each column where rows are shorter than that), then each row's rstd and factor of
+// the stream.
 template <class T>
 __global__ void __launch_bounds__(kThreads, 4) norm_bwd_tiles(const __grid_constant__ NormBwd a, bool w_bf16,
                                                            TilePlan plan, float *partial) {
@@ -239,7 +241,8 @@ __global__ void __launch_bounds__(kThreads, 4) norm_bwd_tiles(const __grid_const
         const int part = threadIdx.x / a.h, c = threadIdx.x - part * a.h;
         if (part < parts) {
           float s = 0.f;
-          for (int r = part; r < rows; r += parts) s = fmaf(get(d + r * a.h + c), get(x + r * a.h + c) * row_rstd[r], s);
+          for (int r = part; r < rows; r += parts)
+            s = fmaf(get(d + r * a.h + c), get(x + r * a.h + c) * row_rstd[r], s);
           sums[threadIdx.x] += s;
         }
       } else {

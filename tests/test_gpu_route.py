@@ -147,9 +147,10 @@ def test_many_tokens(E, groups, kept, k, dtype, score):
 @pytest.mark.parametrize("k", [8, 5])
 @pytest.mark.parametrize("groups,kept,two", [(1, 1, False), (8, 3, False), (8, 3, True), (2, 1, True)])
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
-def test_many_tokens_with_equal_and_near_keys(score, groups, kept, two, k):
+@pytest.mark.parametrize("N", [700, 4000])
+def test_equal_and_near_keys(N, score, groups, kept, two, k):
     """Few different logits; logits that differ in their last bits; keys with a bias that differ by its rounding."""
-    N, E = 4000, 128
+    E = 128
     g = torch.Generator().manual_seed(k)
     for levels in (1, 3, 40):
         x = (torch.randint(0, levels, (N, E), generator=g).float() * 0.3 - 0.6).cuda()
@@ -188,9 +189,10 @@ def test_experts_in_pairs(N, score, groups, kept, two, k):
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("groups,kept", [(1, 1), (4, 2)])
-def test_many_tokens_out_of_the_ordinary(groups, kept, dtype, score):
+@pytest.mark.parametrize("N", [300, 3000])
+def test_rows_out_of_the_ordinary(N, groups, kept, dtype, score):
     """NaN, infinities, rows with few experts or none, the type's lowest value, far and large logits, biases that are out."""
-    N, E, inf = 3000, 64, math.inf
+    E, inf = 64, math.inf
     x = _logits(N, E, dtype, seed=21)
     g = torch.Generator().manual_seed(22)
     kind = torch.randint(0, 12, (N,), generator=g).cuda()
