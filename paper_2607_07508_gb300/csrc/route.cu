@@ -3,10 +3,14 @@
 //   s_e = softmax(x)_e or sigmoid(x_e),  key_e = s_e + bias_e,  the k largest keys of the groups that stay
 //   w_j = scale s_j, over the sum of the chosen s where weights are renormalised
 //
-// Softmax and sigmoid keep the logits' order: without a bias experts are picked by their logits, which is exact,
-// and renormalised weights need the chosen logits alone. Keys with a bias (and sums of two keys) are formed in
-// fp32; a row in which two of them are nearer to one another than their errors, and not of the same logit and
-// bias, is chosen again in fp64.
+// Softmax and sigmoid keep the logits' order: without a bias experts are picked by their logits, which is exact, and
+// renormalised weights need the chosen logits alone. Keys with a bias (and sums of two keys) are formed in fp32; where
+// two of them are nearer to one another than their errors, and not of the same logit and bias, fp64 decides.
+//
+// This form takes what route_lists.cu does not: few tokens, more than eight experts a token or 512 in all, softmax with a
+// bias, any number of groups, replayed choices. It is bound by instructions, 11 to 20 a pick and lane: a warp to a row keeps
+// latency low (7 x 256 in groups 7.7 us with nothing in the caches), and 65,536 x 256 with 10 experts a token take 35
+// us in bf16 and 41 in fp32, 3 to 5 times their bytes at the rate of HBM.
 #include "route_exact.cuh"
 
 namespace sao {

@@ -1,7 +1,12 @@
 // Routing to experts: the gradient of the router's logits.
 //
-// Bound by HBM: it writes every logit's gradient, most of them 0 (renormalised weights, and sigmoid scores,
-// depend on the chosen logits alone).
+//   renormalised  d x_j = w_j (g_j - c / scale), sigmoid times 1 - s_j;  else softmax d x_e = s_e (scale g_e - c),
+//   sigmoid d x_j = w_j g_j (1 - s_j);  c = sum_j g_j w_j
+//
+// It writes every logit's gradient, most of them 0 (renormalised weights, and sigmoid scores, depend on the chosen
+// logits alone), and is bound by that with many tokens: 2^20 x 160 bf16 91 us, 4.8 TB/s; 65,536 x 128 fp32 10 us (34 MB
+// written, half of it latency). The gradient of every logit of a softmax takes an exponential's instructions a logit:
+// 98,301 x 63 bf16 22 us.
 #include "bulk.cuh"
 #include "route_common.cuh"
 

@@ -1,9 +1,12 @@
 // Routing to experts, the form for many tokens: eight lanes take a row, each an eighth of its experts, and keep the
 // largest eight keys of those in a sorted list; three exchanges merge the lists.
 //
-// What bounds it is the number of instructions: a list costs 9 of them a key (a block of eight is sorted by a
-// network of 19 exchanges and merged with eight maxima and 12 exchanges), where picking one expert after another
-// from a warp's 32 lanes costs 11 to 20 a pick and lane, and nothing is summed or compared over a whole warp.
+// What bounds it is the number of instructions, minima and maxima above all (their units are 70 to 86 % busy): a list
+// costs 9 of them a key (a block of eight is sorted by a network of 19 exchanges and merged with eight maxima and 12
+// exchanges), where picking one expert after another from a warp's 32 lanes costs 11 to 20 a pick and lane, and nothing
+// is summed or compared over a whole warp. 8 of 65,536 x 128 fp32 22 us (205 instructions a row; by warps 23 us, 300), of
+// 65,536 x 256 bf16 in groups with a bias 38 (410; 57, 675), of 2^20 x 160 bf16 in groups 282 (258; 419, 357): 335 MB of
+// logits at 1.2 TB/s.
 //
 // Keys are packed in 32 bits, the expert's index (inverted: the lower of equal keys is the larger) below
 //   a bf16 logit, which leaves room for it;
