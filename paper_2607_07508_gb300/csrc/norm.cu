@@ -254,40 +254,47 @@ __global__ void __launch_bounds__(kMaxThreads, kVec < 8 && kVec * kLoads == 32 ?
       for (int i = 0; i < kLoads; ++i) put(i, inverse);
       continue;
     }
-    const bool mx = a.scaling == SAO_SCALE_MX32;
-    const int size = mx ? 32 : 128, blocks = (a.h + size - 1) / size;
-    // loads that a block spans (single columns: 4 of 32), and lanes of a load that share one
-    const int lanes = size / kVec < 32 ? size / kVec : 32;
-    constexpr int kStep = kVec == 1 ? 4 : 1;
+    const auto by_blocks = [&](auto size) {
+      constexpr int kSize = decltype(size)::value;
+      constexpr bool kMx = kSize == 32;
+      const int blocks = (a.h + kSize - 1) / kSize;
+      // loads that a block spans (single columns: 4 of 32), and lanes of a load that share one
+      constexpr int kStep = kVec == 1 ? 4 : 1, kLanes = kSize / kVec < 32 ? kSize / kVec : 32;
 #pragma unroll
-    for (int i = 0; i < kLoads; i += kStep) {
-      float m[kStep];
+      for (int i = 0; i < kLoads; i += kStep) {
+        float m[kStep];
 #pragma unroll
-      for (int k = 0; k < kStep; ++k) {
-        m[k] = amax_of(i + k);
-        for (int o = 1; o < lanes; o <<= 1) m[k] = max_nan(m[k], __shfl_xor_sync(0xffffffffu, m[k], o));
-      }
-      if (kStep > 1 && !mx) {
-        float all = m[0];
+        for (int k = 0; k < kStep; ++k) {
+          m[k] = amax_of(i + k);
 #pragma unroll
-        for (int k = 1; k < kStep; ++k) all = max_nan(all, m[k]);
-#pragma unroll
-        for (int k = 0; k < kStep; ++k) m[k] = all;
-      }
-#pragma unroll
-      for (int k = 0; k < kStep; ++k) {
-        const int c = column(i + k);
-        const bool first = c < a.h && c % size == 0;
-        if (mx) {
-          const uint32_t b = power_of(m[k], &inverse);
-          if (first) static_cast<uint8_t *>(a.scales)[row * blocks + c / size] = uint8_t(b);
-        } else {
-          const float scale = scale_of(m[k], &inverse);
-          if (first) static_cast<float *>(a.scales)[row * blocks + c / size] = scale;
+          for (int o = 1; o < kLanes; o <<= 1) m[k] = max_nan(m[k], __shfl_xor_sync(0xffffffffu, m[k], o));
         }
-        put(i + k, inverse);
+        if (kStep > 1 && !kMx) {
+          float all = m[0];
+#pragma unroll
+          for (int k = 1; k < kStep; ++k) all = max_nan(all, m[k]);
+#pragma unroll
+          for (int k = 0; k < kStep; ++k) m[k] = all;
+        }
+#pragma unroll
+        for (int k = 0; k < kStep; ++k) {
+          const int c = column(i + k);
+          const bool first = c < a.h && (c & (kSize - 1)) == 0;
+          if (kMx) {
+            const uint32_t b = power_of(m[k], &inverse);
+            if (first) static_cast<uint8_t *>(a.scales)[row * blocks + c / kSize] = uint8_t(b);
+          } else {
+            const float scale = scale_of(m[k], &inverse);
+            if (first) static_cast<float *>(a.scales)[row * blocks + c / kSize] = scale;
+          }
+          put(i + k, inverse);
+        }
       }
-    }
+    };
+    if (a.scaling == SAO_SCALE_MX32)
+      by_blocks(std::integral_constant<int, 32>());
+    else
+      by_blocks(std::integral_constant<int, 128>());
   }
 }
 

@@ -152,8 +152,10 @@ __global__ void __launch_bounds__(128) route_bwd_kernel(const __grid_constant__ 
         }
       }
       __syncwarp();
-      for (int i = lane; i < rows * a.k; i += 32) {
-        const int id = chosen_id[i], r = i / a.k, at = r * a.E + id;
+      for (int r0 = 0; r0 < rows; r0 += at_once) {
+        const int r = r0 + mine, i = r0 * a.k + lane;
+        if (mine >= at_once || r >= rows) continue;
+        const int id = chosen_id[i], at = r * a.E + id;
         if (id < 0 || !(inverse[r] > 0.f)) continue;
         const float before = a.accumulate ? value(dx + at) : 0.f;
         put(tile + at, fmaf(expf(value(x + at) - peak[r]) * inverse[r], chosen_d[i] - row_c[r], before));
