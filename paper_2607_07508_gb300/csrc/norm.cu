@@ -29,6 +29,8 @@
 namespace sao {
 namespace {
 
+using namespace norm;
+
 constexpr int kThreads = 256;   // of a CTA, or one row's where they are more
 constexpr int kMaxThreads = 512;
 constexpr int kMaxWarps = kMaxThreads / 32;
@@ -107,13 +109,6 @@ __device__ __forceinline__ void weights(const void *weight, int c, float (&w)[kV
   }
 }
 
-// The maximum, NaN if one of them is (an 8-bit scale that hides a NaN would be a number).
-__device__ __forceinline__ float max_nan(float a, float b) {
-  float m;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
-  return m;
-}
-
 // The warps of a CTA that share a row: `warps` of them, this thread's one being `warp`.
 struct Team {
   int warps, warp, team;
@@ -144,22 +139,6 @@ struct Team {
     return all(v, [](float a, float b) { return max_nan(a, b); });
   }
 };
-
-// A block's scale and what its values are multiplied by. amax / 448 is the largest e4m3 value's.
-__device__ __forceinline__ float scale_of(float amax, float *inverse) {
-  const float s = max_nan(amax / 448.f, FLT_MIN);  // a block of zeros has a scale all the same
-  *inverse = 1.f / s;
-  return s;
-}
-// The least power of two 2^(b - 127) that amax / 448 does not pass (b = 255: NaN). 448 is 1.75 2^8: the exponent less 8,
-// and one more where the mantissa is past 1.75.
-__device__ __forceinline__ uint32_t power_of(float amax, float *inverse) {
-  const uint32_t u = __float_as_uint(amax);
-  const int e = int((u + 0x1fffffu) >> 23) - 8;
-  const uint32_t b = u >= 0x7f800000u ? 255u : e > 0 ? uint32_t(e) : 0u;
-  *inverse = b == 255u ? NAN : __uint_as_float((254u - b) << 23);
-  return b;
-}
 
 template <class T, class WT, int kVec, int kLoads>
 __global__ void __launch_bounds__(kMaxThreads, kVec < 8 && kVec * kLoads == 32 ? 1 : 2)
@@ -489,7 +468,9 @@ sao_status by_types(sao_dtype dt, sao_dtype w_dt, bool wide, F f) {
 // and 256, in fp32 270 and 322. Backward: 300,000 x 20 34 and 111, 400,003 x 64 140 and 161, x 77 192 and 171; it
 // reads its tiles three times.)
 constexpr int kShortRow = 64;
-bool fwd_by_tiles(int h, sao_dtype dt, bool wide) { return h <= kShortRow || (!wide && (dt == SAO_BF16 || h > 1024)); }
+bool fwd_by_tiles(int h, sao_dtype dt, bool wide, bool to8) {
+  return h <= kShortRow || (!wide && (to8 || dt == SAO_BF16 || h > 1024));
+}
 
 }  // namespace
 
@@ -503,8 +484,8 @@ sao_status norm_fwd_launch(const NormFwd &a, sao_dtype dt, sao_dtype w_dt, cudaS
   SAO_TRY(device_info(&di));
   const bool wide = a.h % (dt == SAO_BF16 ? 8 : 4) == 0 && aligned16(a.x) && aligned16(a.residual) &&
                     aligned16(a.sum) && aligned16(a.y) && aligned16(a.weight) && aligned16(a.y8);
-  const bool tiles = aligned16(a.x) && aligned16(a.residual) && aligned16(a.sum) && aligned16(a.y) && a.y8 == nullptr;
-  if (tiles && fwd_by_tiles(a.h, dt, wide)) return norm_fwd_tiles_launch(a, dt, w_dt, s);
+  const bool tiles = aligned16(a.x) && aligned16(a.residual) && aligned16(a.sum) && aligned16(a.y) && aligned16(a.y8);
+  if (tiles && fwd_by_tiles(a.h, dt, wide, a.y8 != nullptr)) return norm_fwd_tiles_launch(a, dt, w_dt, s);
   return by_types(dt, w_dt, wide, [&](auto t, auto w, auto vec) {
     return fwd<decltype(t), decltype(w), decltype(vec)::value>(a, di.sm_count, s);
   });

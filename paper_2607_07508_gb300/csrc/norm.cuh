@@ -2,6 +2,8 @@
 #pragma once
 
 #include <cuda_runtime.h>
+#include <float.h>
+#include <math.h>
 #include <stdint.h>
 
 #include "../../include/sao.h"
@@ -31,11 +33,38 @@ struct NormBwd {
   int h;
 };
 
+namespace norm {
+
+// The maximum, NaN if one of them is (an 8-bit scale that hides a NaN would be a number).
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float m;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
+  return m;
+}
+
+// A block's scale and what its values are multiplied by. amax / 448 is the largest e4m3 value's.
+__device__ __forceinline__ float scale_of(float amax, float *inverse) {
+  const float s = max_nan(amax / 448.f, FLT_MIN);  // a block of zeros has a scale all the same
+  *inverse = 1.f / s;
+  return s;
+}
+// The least power of two 2^(b - 127) that amax / 448 does not pass (b = 255: NaN). 448 is 1.75 2^8: the exponent less 8,
+// and one more where the mantissa is past 1.75.
+__device__ __forceinline__ uint32_t power_of(float amax, float *inverse) {
+  const uint32_t u = __float_as_uint(amax);
+  const int e = int((u + 0x1fffffu) >> 23) - 8;
+  const uint32_t b = u >= 0x7f800000u ? 255u : e > 0 ? uint32_t(e) : 0u;
+  *inverse = b == 255u ? NAN : __uint_as_float((254u - b) << 23);
+  return b;
+}
+
+}  // namespace norm
+
 size_t norm_ws_bytes(int64_t N, int32_t h);
 sao_status norm_fwd_launch(const NormFwd &a, sao_dtype dt, sao_dtype w_dt, cudaStream_t s);
 sao_status norm_bwd_launch(const NormBwd &a, sao_dtype dt, sao_dtype w_dt, void *ws, size_t ws_bytes, cudaStream_t s);
 
-// norm_tiles.cu: the same for rows of any length, arrays on 16 bytes, no 8-bit rows. The backward has at most
+// norm_tiles.cu: the same for rows of any length, arrays on 16 bytes. The backward has at most
 // `most` CTAs, and writes how many (`parts`) have sums for dw in `partial`.
 sao_status norm_fwd_tiles_launch(const NormFwd &a, sao_dtype dt, sao_dtype w_dt, cudaStream_t s);
 sao_status norm_bwd_tiles_launch(const NormBwd &a, sao_dtype dt, sao_dtype w_dt, float *partial, int most, int *parts,

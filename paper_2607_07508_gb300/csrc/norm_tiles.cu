@@ -8,6 +8,7 @@
 // 93 and 111), forward of 20,001 x 4,099 190 us (0.66 GB, 3.5 TB/s; single columns from memory 256, vectors that the
 // rows' ends cut 191). Which calls come here: fwd_by_tiles in norm.cu.
 #include <cuda_bf16.h>
+#include <cuda_fp8.h>
 #include <math.h>
 #include <stdint.h>
 
@@ -17,6 +18,8 @@
 
 namespace sao {
 namespace {
+
+using namespace norm;
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr unsigned kAll = 0xffffffffu;
@@ -143,20 +146,90 @@ struct Share {
     column = warps > 1 ? warp % warps * 32 + lane : lane & (lanes - 1);
     step = warps > 1 ? warps * 32 : lanes;
   }
-  // The row's sum, in all of its threads. All threads of the CTA call it (those without a row too).
-  __device__ __forceinline__ float sum(float v) {
-    for (int o = lanes / 2; o > 0; o >>= 1) v += __shfl_xor_sync(kAll, v, o);
+  // Over the row, in all of its threads. All threads of the CTA call it (those without a row too).
+  template <class Op>
+  __device__ __forceinline__ float all(float v, Op op) {
+    for (int o = lanes / 2; o > 0; o >>= 1) v = op(v, __shfl_xor_sync(kAll, v, o));
     if (warps == 1) return v;
     float *mine = slots + (turn++ & 1u) * kWarps;
     const int warp = threadIdx.x / 32, first = warp / warps * warps;
     if ((threadIdx.x & 31) == 0) mine[warp] = v;
     __syncthreads();
     v = mine[first];
-    for (int i = 1; i < warps; ++i) v += mine[first + i];
+    for (int i = 1; i < warps; ++i) v = op(v, mine[first + i]);
     return v;
+  }
+  __device__ __forceinline__ float sum(float v) {
+    return all(v, [](float a, float b) { return a + b; });
+  }
+  __device__ __forceinline__ float max(float v) {
+    return all(v, [](float a, float b) { return max_nan(a, b); });
   }
 };
 
+__device__ __forceinline__ uint8_t to8(float v) { return __nv_cvt_float_to_fp8(v, __NV_SATFINITE, __NV_E4M3); }
+
+// A row in 8 bits to `out`, from its columns' values: blocks of kSize columns (0: the row) by a part of a warp or, of a
+// row of several warps, one of them each. All threads of the CTA call it; those without a row write nothing.
+template <int kSize, class Value>
+__device__ __forceinline__ void quantise(Share &share, const NormFwd &a, int64_t row, bool real, uint8_t *out,
+                                         Value value) {
+  float inverse;
+  if constexpr (kSize == 0) {
+    float m = 0.f;
+    for (int c = share.column; c < (real ? a.h : 0); c += share.step) m = max_nan(m, fabsf(value(c)));
+    const float scale = scale_of(share.max(m), &inverse);
+    if (real && share.column == 0) static_cast<float *>(a.scales)[row] = scale;
+    for (int c = share.column; c < (real ? a.h : 0); c += share.step) out[c] = to8(value(c) * inverse);
+  } else {
+    const int lane = share.warps > 1 ? threadIdx.x & 31 : share.column, blocks = (a.h + kSize - 1) / kSize;
+    const int first = share.warps > 1 ? threadIdx.x / 32 % share.warps : 0;
+    const auto scale = [&](int b, float m, bool writes) {
+      if (kSize == 32) {
+        const uint32_t power = power_of(m, &inverse);
+        if (writes) static_cast<uint8_t *>(a.scales)[row * blocks + b] = uint8_t(power);
+      } else {
+        const float f = scale_of(m, &inverse);
+        if (writes) static_cast<float *>(a.scales)[row * blocks + b] = f;
+      }
+    };
+    if (share.lanes == 32) {  // a warp's 128 columns at a time: four blocks of 32, or one, with their values in registers
+      constexpr int kBlocks = 128 / kSize;
+      for (int b0 = first * kBlocks; b0 < blocks; b0 += share.warps * kBlocks) {
+        float v[4];
+        uint32_t m[kBlocks] = {};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int c = b0 * kSize + i * 32 + lane;
+          v[i] = real && c < a.h ? value(c) : 0.f;
+          uint32_t &its = m[i * kBlocks / 4];
+          its = max(its, __float_as_uint(v[i]) & 0x7fffffffu);  // (a NaN is the largest)
+        }
+#pragma unroll
+        for (int i = 0; i < kBlocks; ++i) m[i] = __reduce_max_sync(kAll, m[i]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int c = b0 * kSize + i * 32 + lane, b = b0 + i * kBlocks / 4;
+          if (i % (4 / kBlocks) == 0) scale(b, __uint_as_float(m[i * kBlocks / 4]), real && lane == 0 && b < blocks);
+          if (real && c < a.h) out[c] = to8(v[i] * inverse);
+        }
+      }
+      return;
+    }
+    for (int b = 0; b < blocks; ++b) {
+      const int end = !real ? 0 : (b + 1) * kSize < a.h ? (b + 1) * kSize : a.h;
+      float m = 0.f;
+#pragma unroll 4
+      for (int c = b * kSize + lane; c < end; c += share.lanes) m = max_nan(m, fabsf(value(c)));
+      for (int o = share.lanes / 2; o > 0; o >>= 1) m = max_nan(m, __shfl_xor_sync(kAll, m, o));
+      scale(b, m, real && lane == 0);
+#pragma unroll 4
+      for (int c = b * kSize + lane; c < end; c += share.lanes) out[c] = to8(value(c) * inverse);
+    }
+  }
+}
+
+// Shared memory: the tile of the stream, then that of the 8-bit rows if there are any.
 template <class T>
 __global__ void __launch_bounds__(kThreads, 4) norm_fwd_tiles(const __grid_constant__ NormFwd a, bool w_bf16,
                                                            TilePlan plan) {
@@ -164,6 +237,7 @@ __global__ void __launch_bounds__(kThreads, 4) norm_fwd_tiles(const __grid_const
   extern __shared__ __align__(16) unsigned char shared[];
   __shared__ float slots[2 * kWarps];
   T *tile = reinterpret_cast<T *>(shared);
+  uint8_t *tile8 = shared + plan.bytes;
   constexpr int kVec = 16 / int(sizeof(T));
   Share share(plan, slots);
   const float mean = 1.f / float(a.h);
@@ -186,14 +260,26 @@ __global__ void __launch_bounds__(kThreads, 4) norm_fwd_tiles(const __grid_const
 #pragma unroll 4
       for (int c = share.column; c < (real ? a.h : 0); c += share.step) s = fmaf(get(row + c), get(row + c), s);
       const float rstd = 1.f / sqrtf(fmaf(share.sum(s), mean, a.eps));
-      if (!real) continue;
-      if (a.rstd && share.column == 0) a.rstd[row0 + r] = rstd;
+      if (real && a.rstd && share.column == 0) a.rstd[row0 + r] = rstd;
+      const auto value = [&](int c) { return get(row + c) * rstd * column_weight(a.weight, w_bf16, c); };
+      if (a.y8) {
+        uint8_t *out = tile8 + from % 16 + (real ? r : 0) * a.h;
+        if (a.scaling == SAO_SCALE_ROW)
+          quantise<0>(share, a, row0 + r, real, out, value);
+        else if (a.scaling == SAO_SCALE_BLOCK128)
+          quantise<128>(share, a, row0 + r, real, out, value);
+        else
+          quantise<32>(share, a, row0 + r, real, out, value);
+        // y takes the place of the stream, which other threads of the row have read
+        if (a.y) share.warps > 1 ? __syncthreads() : __syncwarp();
+      }
+      if (!real || !a.y) continue;
 #pragma unroll 4
-      for (int c = share.column; c < a.h; c += share.step)
-        put(row + c, get(row + c) * rstd * column_weight(a.weight, w_bf16, c));
+      for (int c = share.column; c < a.h; c += share.step) put(row + c, value(c));
     }
     __syncthreads();
-    store_tile<T>(tile, static_cast<T *>(a.y), from, count);
+    if (a.y) store_tile<T>(tile, static_cast<T *>(a.y), from, count);
+    if (a.y8) store_tile<uint8_t>(tile8, a.y8, from, count);
     __syncthreads();
   }
 }
@@ -314,9 +400,10 @@ template <class T>
 sao_status fwd(const NormFwd &a, bool w_bf16, const DeviceInfo &di, cudaStream_t s) {
   SAO_TRY(allow<T>(di.device, kMostShared));
   const TilePlan p = plan_of(a.h, sizeof(T));
-  const int64_t tiles = (a.N + p.rows - 1) / p.rows, most = int64_t(di.sm_count) * 4 * ctas_of(p.bytes, 6);
+  const size_t bytes = p.bytes + (a.y8 ? size_t(p.rows) * a.h + 32 : 0);
+  const int64_t tiles = (a.N + p.rows - 1) / p.rows, most = int64_t(di.sm_count) * 4 * ctas_of(bytes, 6);
   const int slot = launch_begin("norm_fwd", s);
-  pdl(norm_fwd_tiles<T>, unsigned(tiles < most ? tiles : most), kThreads, p.bytes, s)(a, w_bf16, p);
+  pdl(norm_fwd_tiles<T>, unsigned(tiles < most ? tiles : most), kThreads, bytes, s)(a, w_bf16, p);
   return launch_end(slot, s);
 }
 

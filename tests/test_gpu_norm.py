@@ -143,6 +143,15 @@ def test_eight_bits(N, h, dtype, scaling):
     check_forward(c, forward(c, scaling=scaling, want_y=h % 2 == 0, rstd=False), scaling=scaling)
 
 
+@pytest.mark.parametrize("scaling", ["row", "block", "mx"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,h", [(3000, 5), (700, 24), (1001, 47), (400, 64), (333, 129), (90, 771), (61, 2259), (7, 9001)])
+def test_eight_bits_beside_y(N, h, dtype, scaling):
+    for residual in (True, False):
+        c = _case(N, h, dtype, residual=residual, seed=h)
+        check_forward(c, forward(c, scaling=scaling), scaling=scaling)
+
+
 @pytest.mark.parametrize("h", [640, 2048])
 @pytest.mark.parametrize("dtype,offset", [("f32", 1), ("f32", 2), ("bf16", 1), ("bf16", 4), ("bf16", 8)])
 def test_alignment(dtype, offset, h):
