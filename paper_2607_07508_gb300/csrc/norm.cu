@@ -282,7 +282,7 @@ template <class T, class WT, int kVec, int kLoads>
 __global__ void __launch_bounds__(kMaxThreads) norm_bwd_kernel(NormBwd a, int warps, float *partial) {
   grid_wait();
   __shared__ float slots[2 * kMaxWarps];
-  extern __shared__ float sums[];  // [h], with more than one team
+  extern __shared__ float sums[];  // a place for each of a lane's columns, with more than one team
   Team team(warps, slots);
   const int lane = threadIdx.x & 31, teams = blockDim.x / (32 * warps);
   const int c0 = (team.warp * kLoads * 32 + lane) * kVec;
@@ -333,22 +333,30 @@ __global__ void __launch_bounds__(kMaxThreads) norm_bwd_kernel(NormBwd a, int wa
       }
   }
   if (partial == nullptr) return;
-  float *out = partial + int64_t(blockIdx.x) * a.h;
-  for (int t = 0; t < teams; ++t) {  // the teams' sums in their order
+  // The teams' sums in their order, a thread's where no other's banks are (by columns this took 10 us of a call).
+  const int width = 32 * warps, place = team.warp * 32 + lane;
+  for (int t = 0; t < teams; ++t) {
     if (t > 0) __syncthreads();
     if (t != team.team) continue;
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i)
+    for (int i = 0; i < kLoads * kVec; ++i) {
+      if (t > 0) dw[i] += sums[i * width + place];
+      if (t < teams - 1) sums[i * width + place] = dw[i];
+    }
+  }
+  if (team.team != teams - 1) return;
+  float *out = partial + int64_t(blockIdx.x) * a.h;
 #pragma unroll
-      for (int j = 0; j < kVec; ++j) {
-        const int c = column(i) + j;
-        if (c >= a.h) continue;
-        const float v = t == 0 ? dw[i * kVec + j] : sums[c] + dw[i * kVec + j];
-        if (t == teams - 1)
-          out[c] = v;
-        else
-          sums[c] = v;
-      }
+  for (int i = 0; i < kLoads; ++i) {
+    if (column(i) >= a.h) continue;
+    if constexpr (kVec == 1) {
+      out[column(i)] = dw[i];
+    } else {
+#pragma unroll
+      for (int j = 0; j < kVec; j += 4)
+        *reinterpret_cast<float4 *>(out + column(i) + j) =
+            make_float4(dw[i * kVec + j], dw[i * kVec + j + 1], dw[i * kVec + j + 2], dw[i * kVec + j + 3]);
+    }
   }
 }
 
@@ -411,7 +419,7 @@ sao_status fwd(const NormFwd &a, int sms, cudaStream_t s) {
   // few rows: few loads a lane, for latency. Many: 16 columns a lane up to 8 warps to a row, else 32, which keeps 64
   // registers and half an SM's warps (65,536 x 2,048 161 us with 16, 168 with 32; 16,384 x 6,144 in 8 bits 166 and 153)
   constexpr int kFewLoads = kVec == 1 ? 4 : 1, kMostLoads = 32 / kVec;
-  const Shape p = a.N <= sms ? shape_of(a.h, kVec, kFewLoads, kMostLoads, kThreads / 32)
+  const Shape p = a.N <= 4 * sms ? shape_of(a.h, kVec, kFewLoads, kMostLoads, kThreads / 32)
                              : shape_of(a.h, kVec, kVec == 1 ? 8 : 16 / kVec, kMostLoads, kThreads / 32);
   const int teams = teams_of(p.warps);
   int64_t grid = (a.N + teams - 1) / teams;
@@ -429,7 +437,7 @@ template <class T, class WT, int kVec>
 sao_status bwd(const NormBwd &a, int sms, float *partial, cudaStream_t s) {
   constexpr int kFewLoads = kVec == 1 ? 8 : kVec == 4 ? 4 : 1, kMostLoads = 32 / kVec;
   // many rows: 32 bf16 columns a lane, fewer fp32 or single ones, for registers
-  const int wish = a.N <= sms ? kThreads / 32 : kVec < 8 ? kMaxWarps : 1;
+  const int wish = a.N <= 4 * sms ? kThreads / 32 : kVec < 8 ? kMaxWarps : 1;
   const Shape p = shape_of(a.h, kVec, kFewLoads, kMostLoads, wish);
   const int teams = teams_of(p.warps);
   int64_t grid = (a.N + teams - 1) / teams;
@@ -441,7 +449,8 @@ sao_status bwd(const NormBwd &a, int sms, float *partial, cudaStream_t s) {
   by_loads(p.loads, [&](auto loads) {
     if constexpr (decltype(loads)::value >= kFewLoads && decltype(loads)::value <= kMostLoads)
       pdl(norm_bwd_kernel<T, WT, kVec, decltype(loads)::value>, unsigned(grid), unsigned(teams * p.warps * 32),
-          teams > 1 ? size_t(a.h) * sizeof(float) : 0, s)(a, p.warps, a.dweight ? partial : nullptr);
+          teams > 1 ? size_t(p.loads) * kVec * 32 * p.warps * sizeof(float) : 0, s)(
+          a, p.warps, a.dweight ? partial : nullptr);
   });
   SAO_TRY(launch_end(slot, s));
   return a.dweight ? sum_parts(a, partial, int(grid), s) : SAO_OK;

@@ -367,10 +367,11 @@ __global__ void __launch_bounds__(kThreads, 4) norm_bwd_tiles(const __grid_const
   }
 }
 
-// Rows of a tile and how they are shared out. A tile has about 16 KB; from eight rows on a warp or less takes one.
-TilePlan plan_of(int h, int size) {
+// Rows of a tile and how they are shared out. A tile has about 16 KB, or less to have two for each SM; from eight rows
+// on a warp or less takes one.
+TilePlan plan_of(int64_t N, int h, int size, int sms) {
   TilePlan p{1, 32, kWarps, 0};
-  while (p.rows < 512 && 2 * p.rows * h * size <= (16 << 10)) p.rows *= 2;
+  while (p.rows < 512 && 2 * p.rows * h * size <= (16 << 10) && 2 * p.rows * int64_t(sms) < N) p.rows *= 2;
   p.warps = p.rows >= kWarps ? 1 : kWarps / p.rows;
   while (p.lanes > 4 && p.lanes * 4 > h && p.rows >= kWarps * (64 / p.lanes)) p.lanes /= 2;
   p.bytes = (p.rows * h * size + 2 * 16 + 15) / 16 * 16;
@@ -399,7 +400,7 @@ int ctas_of(size_t bytes, int most) {
 template <class T>
 sao_status fwd(const NormFwd &a, bool w_bf16, const DeviceInfo &di, cudaStream_t s) {
   SAO_TRY(allow<T>(di.device, kMostShared));
-  const TilePlan p = plan_of(a.h, sizeof(T));
+  const TilePlan p = plan_of(a.N, a.h, sizeof(T), di.sm_count);
   const size_t bytes = p.bytes + (a.y8 ? size_t(p.rows) * a.h + 32 : 0);
   const int64_t tiles = (a.N + p.rows - 1) / p.rows, most = int64_t(di.sm_count) * 4 * ctas_of(bytes, 6);
   const int slot = launch_begin("norm_fwd", s);
@@ -411,7 +412,7 @@ template <class T>
 sao_status bwd(const NormBwd &a, bool w_bf16, const DeviceInfo &di, float *partial, int most, int *parts,
                cudaStream_t s) {
   SAO_TRY(allow<T>(di.device, kMostShared));
-  const TilePlan p = plan_of(a.h, sizeof(T));
+  const TilePlan p = plan_of(a.N, a.h, sizeof(T), di.sm_count);
   const size_t bytes = 2 * size_t(p.bytes) + sizeof(float) * (size_t(a.h < kThreads ? kThreads : a.h) + 2 * p.rows);
   const int64_t tiles = (a.N + p.rows - 1) / p.rows;
   *parts = int(tiles < most ? tiles : most);
