@@ -432,15 +432,190 @@ __global__ void __launch_bounds__(kListWarps * 32)
   }
 }
 
+// The same for up to 32 experts in one group: a thread to a row, all of it in registers, nothing to merge or to sum with
+// another lane. Choices and weights go through shared memory, so that a warp's 32 rows are stored together.
+// 395,545 x 15 bf16 with a softmax and a bias SMALL_A us, 65,536 x 8 fp32 SMALL_B (a warp to a row 105 and 15).
+//
+// kBlocks: of eight experts.
+template <class T, int kBlocks, bool kBiased>
+__global__ void __launch_bounds__(kListWarps * 32)
+    route_small_kernel(const __grid_constant__ RouteArgs a, const __grid_constant__ Lanes l32, ListPlan plan) {
+  grid_wait();
+  constexpr bool kExact = !kBiased && sizeof(T) == 2;
+  __shared__ float offset[kListWarps][8 * kBlocks];
+  __shared__ int all_ids[kListWarps][32 * kList];
+  __shared__ float all_weights[kListWarps][32 * kList];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+  int *its_ids = all_ids[warp];
+  float *its_weights = all_weights[warp];
+  const bool soft = a.score == SAO_SCORE_SOFTMAX, sums = soft && (kBiased || !a.renorm);
+  float units = 1.f;
+  bool all_exactly = false;
+  if (kBiased) {  // keys as fractions, as above
+    const float b = lane < a.E ? ld(a.bias + lane) : -INFINITY;
+    const bool there = fabsf(b) < INFINITY;
+    float low = -warp_max(there ? -b : -INFINITY), high = warp_max(there ? b : -INFINITY);
+    if (high < low) low = high = 0.f;
+    units = (1.f - 0x1p-9f) / (1.f + (high - low));
+    all_exactly = __any_sync(kAll, b == INFINITY) || !(units >= 0x1p-20f);
+    if (lane < 8 * kBlocks) offset[warp][lane] = there ? fmaf(b - low, units, kFractionLeast) : -INFINITY;
+    __syncwarp();
+  }
+  const uint32_t mask = kExact ? 0xffffu : kBiased ? kFractionMask : plan.mask;
+  const uint32_t none = kExact ? 0x007fffffu : kBiased ? kFractionMask : 0x007fffffu | mask;
+  const int64_t step = int64_t(gridDim.x) * kListWarps * 32;
+  for (int64_t row0 = (int64_t(blockIdx.x) * kListWarps + warp) * 32; row0 < a.N; row0 += step) {
+    const int rows = int(a.N - row0 < 32 ? a.N - row0 : 32);
+    const bool on = lane < rows && (a.mask == nullptr || ld(a.mask + row0 + lane) != 0);
+    const T *logits = static_cast<const T *>(a.x) + (row0 + (lane < rows ? lane : 0)) * a.E;
+    Block<T> x[kBlocks];
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) x[b].load(logits + 8 * b, on ? a.E - 8 * b : 0, plan.unit);
+    bool bad = false;
+    float top = -INFINITY, total = 1.f, inverse = 1.f;
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float v = x[b].at(i);
+        bad |= !(v < INFINITY) && (soft || v != v);
+        top = fmaxf(top, v);
+      }
+    if (__any_sync(kAll, bad) && bad) raise_device_error(a.err, SAO_DEVERR_LOGITS);
+    const bool scores = on && !bad && top > -INFINITY;
+    uint32_t v[8], rest = 0u;
+    float e[kBlocks][8];
+    if (sums) {
+      total = 0.f;
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {  // (where weights have this sum's error it is that of expf)
+          const float d = x[b].at(i) - top;
+          total += e[b][i] = a.renorm ? exp_fast(d) : expf(d);
+        }
+      inverse = 1.f / total;
+    }
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) {
+      uint32_t w[8];
+      if constexpr (kBiased) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float s = soft ? e[b][i] * inverse : sigmoid_fast(x[b].at(i));
+          const float f = fmaxf(fmaf(s, units, offset[warp][8 * b + i]), 1.f);
+          w[i] = x[b].at(i) > -INFINITY ? __float_as_uint(f) * 512u + (kFractionMask - 8 * b - i) : 0u;
+        }
+      } else {
+        pack(x[b], mask - 8 * b, mask, w);
+      }
+      sort8(w);
+      if (b == 0) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = w[i];
+      } else {
+        merge8<!kExact>(v, w, rest);
+      }
+    }
+    // two fractions are off by twice a score's error (of a softmax 2^-18 of its largest, which `inverse` is) and 3 2^-23
+    const uint32_t apart = !kBiased ? 0u : uint32_t((soft ? 64.f * inverse : 8.f) * units) + 5u;
+    bool again = all_exactly;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (i >= a.k) continue;
+      const int id = scores && v[i] > none ? int(mask - (v[i] & mask)) : -1;
+      its_ids[lane * a.k + i] = id;
+      if (!kExact) {
+        const uint32_t p = v[i], q = i < 7 ? v[i < 7 ? i + 1 : 7] : rest;
+        if (p > none && q > none && (kBiased ? (p >> 9) - (q >> 9) <= apart : ((p ^ q) & ~mask) == 0u)) {
+          // those of one logit and bias are equal, but at the border of the choice a third one may be as near
+          const int next = int(mask - (q & mask));
+          bool same = i < a.k - 1 && id >= 0 && value(logits + id) == value(logits + next);
+          if (kBiased) same = same && ld(a.bias + id) == ld(a.bias + next);
+          again |= !same;
+        }
+      }
+    }
+    __syncwarp();
+    unsigned todo = __ballot_sync(kAll, again && scores);
+    while (todo != 0u) {
+      const int r = __ffs(todo) - 1;
+      todo &= todo - 1u;
+      const T *its_row = static_cast<const T *>(a.x) + (row0 + r) * a.E;
+      const int found = choose_exactly<T, 1, kBiased>({a.bias, a.k, a.kept, soft, a.two != 0}, l32, its_row);
+      if (lane < a.k) its_ids[r * a.k + lane] = found;
+      __syncwarp();
+    }
+    float c[8], m = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int id = i < a.k ? its_ids[lane * a.k + i] : -1;
+      c[i] = id >= 0 ? value(logits + id) : -INFINITY;
+      m = fmaxf(m, soft ? c[i] : fminf(c[i], 0.f));
+    }
+    if (a.renorm) {
+      // sigmoid(x) = exp(min(x, 0)) / (1 + exp(-|x|)): relative to the largest, no sum vanishes
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float t = m > -INFINITY ? expf((soft ? c[i] : fminf(c[i], 0.f)) - m) : 0.f;
+        if (!soft) t /= 1.f + expf(-fabsf(c[i]));
+        sum += c[i] = t;
+      }
+      const float f = sum > 0.f ? 1.f / sum : 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) c[i] *= f;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        c[i] = !soft ? sigmoid(c[i]) : c[i] > -INFINITY ? expf(c[i] - top) * inverse : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < a.k) its_weights[lane * a.k + i] = its_ids[lane * a.k + i] >= 0 ? a.scale * c[i] : 0.f;
+    __syncwarp();
+    for (int t = lane; t < rows * a.k; t += 32) {
+      a.ids[row0 * a.k + t] = its_ids[t];
+      a.weights[row0 * a.k + t] = its_weights[t];
+    }
+    __syncwarp();
+  }
+}
+
 }  // namespace
 
+bool route_small_take(const RouteArgs &a, int sms) {
+  return !a.replay && a.k <= kList && a.E <= 32 && a.groups == 1 && a.N >= int64_t(sms) * 32;
+}
+
 bool route_lists_take(const RouteArgs &a, int sms) {
+  if (route_small_take(a, sms)) return true;
   if (a.replay || a.k > kList || a.E < 16 || a.E > 512 || a.groups > kShare || (a.groups & (a.groups - 1)) != 0)
     return false;
   return !(a.bias && a.score == SAO_SCORE_SOFTMAX) && a.N >= int64_t(sms) * kRows * kListWarps;
 }
 
+sao_status route_small_launch(const RouteArgs &a, const Lanes &l32, sao_dtype dt, int sms, cudaStream_t s) {
+  const int size = dt == SAO_BF16 ? 2 : 4;
+  ListPlan p{a.E, (a.E + 7) / 8, 16, 7u};
+  while (p.mask + 1u < 8u * (p.blocks > 2 ? 4 : p.blocks)) p.mask = 2 * p.mask + 1u;
+  while (p.unit >= 8 && (reinterpret_cast<uintptr_t>(a.x) % p.unit != 0 || a.E * size % p.unit != 0)) p.unit /= 2;
+  const int64_t tiles = (a.N + 32 * kListWarps - 1) / (32 * kListWarps), most = int64_t(sms) * 128;
+  const int slot = launch_begin("route_small", s);
+  SAO_TRY(by_type(dt, [&](auto t) {
+    using T = decltype(t);
+    const auto launch = [&](auto kernel) {
+      pdl(kernel, unsigned(least(tiles, most)), kListWarps * 32, 0, s)(a, l32, p);
+      return SAO_OK;
+    };
+    if (p.blocks == 1) return launch(a.bias ? route_small_kernel<T, 1, true> : route_small_kernel<T, 1, false>);
+    if (p.blocks == 2) return launch(a.bias ? route_small_kernel<T, 2, true> : route_small_kernel<T, 2, false>);
+    return launch(a.bias ? route_small_kernel<T, 4, true> : route_small_kernel<T, 4, false>);
+  }));
+  return launch_end(slot, s);
+}
+
 sao_status route_lists_launch(const RouteArgs &a, const Lanes &l32, sao_dtype dt, int sms, cudaStream_t s) {
+  if (route_small_take(a, sms)) return route_small_launch(a, l32, dt, sms, s);
   const Lanes l{kShare / a.groups, 0, a.E / a.groups, a.groups};
   const int size = dt == SAO_BF16 ? 2 : 4;
   ListPlan p{};

@@ -144,6 +144,48 @@ def test_many_tokens(E, groups, kept, k, dtype, score):
     check(x, k, score, None, mask, groups, kept, False, renorm=False)
 
 
+# Up to 32 experts in one group, eight a token: a thread to a row.
+FEW = [(1, 1), (2, 1), (5, 2), (8, 2), (8, 8), (9, 3), (15, 5), (16, 4), (17, 8), (23, 7), (31, 1), (32, 8)]
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("E,k", FEW)
+def test_few_experts(E, k, dtype, score):
+    N = 9001
+    x = _logits(N, E, dtype, seed=E + k)
+    mask = (torch.rand(N, generator=torch.Generator().manual_seed(E)) < 0.7).to(torch.uint8).cuda()
+    for bias in (None, _bias(E), _bias(E) * 30 - 100):
+        for renorm in (True, False):
+            check(x, k, score, bias, mask if renorm else None, renorm=renorm)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("E,k", [(6, 2), (16, 8), (30, 5)])
+def test_few_experts_of_near_and_extraordinary_keys(E, k, dtype, score):
+    """Copies that differ in their last bits, few different logits, NaN, infinities, the lowest value, biases that are out."""
+    N, inf = 6000, math.inf
+    g = torch.Generator().manual_seed(E)
+    x = torch.randn(N, (E + 1) // 2, generator=g).repeat(1, 2)[:, :E].contiguous()
+    x = (x.view(torch.int32) + torch.randint(-3, 4, (N, E), generator=g, dtype=torch.int32)).view(torch.float32)
+    few = torch.randint(0, 3, (N, E), generator=g).float() * 0.3
+    x = torch.where((torch.arange(N) % 3 == 0)[:, None], few, x).to(DT[dtype]).cuda()
+    kind = torch.randint(0, 12, (N,), generator=g).cuda()
+    x[kind == 0, 1], x[kind == 1, 2], x[kind == 2, 0] = math.nan, inf, -inf
+    x[kind == 3], x[kind == 4, 1:] = -inf, -inf
+    x[kind == 5, 2:] = torch.finfo(x.dtype).min
+    x[kind == 6] *= 60
+    bias = _bias((E + 1) // 2).repeat(2)[:E].contiguous()
+    out = bias.clone()
+    out[1], out[3] = -inf, math.nan
+    top = bias.clone()
+    top[2] = inf
+    for b in (None, bias, torch.zeros(E, device="cuda"), out, bias * 1e6, top):
+        check(x, k, score, b, renorm=True, train=False)
+        check(x[:5000].contiguous(), k, score, b, renorm=False, train=False)
+
+
 @pytest.mark.parametrize("k", [8, 5])
 @pytest.mark.parametrize("groups,kept,two", [(1, 1, False), (8, 3, False), (8, 3, True), (2, 1, True)])
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
