@@ -1,5 +1,5 @@
-// Routing to experts, the form for many tokens: eight lanes take a row, each an eighth of its experts, and keep the
-// largest eight keys of those in a sorted list; three exchanges merge the lists.
+// Routing to experts, the forms for many tokens: eight lanes take a row, each an eighth of its experts, and keep the
+// largest eight keys of those in a sorted list; three exchanges merge the lists. Or a thread takes a row (below).
 //
 // What bounds it is the number of instructions, minima and maxima above all (their units are 70 to 86 % busy): a list
 // costs 9 of them a key (a block of eight is sorted by a network of 19 exchanges and merged with eight maxima and 12
@@ -432,34 +432,41 @@ __global__ void __launch_bounds__(kListWarps * 32)
   }
 }
 
-// The same for up to 32 experts in one group: a thread to a row, all of it in registers, nothing to merge or to sum with
-// another lane. Choices and weights go through shared memory, so that a warp's 32 rows are stored together.
-// 395,545 x 15 bf16 with a softmax and a bias SMALL_A us, 65,536 x 8 fp32 SMALL_B (a warp to a row 105 and 15).
-//
-// kBlocks: of eight experts.
+// The same with a thread to a row, nothing to merge or to sum with another lane: of one group, up to 32 experts in
+// registers (kBlocks of eight), or, kBlocks 0 and no softmax with a bias, any number of blocks one after another. Choices
+// and weights go through shared memory, so that a warp's 32 rows are stored together.
+// 395,545 x 15 bf16 with a softmax and a bias 23 us, 65,536 x 8 fp32 5 (a warp to a row 105 and 15).
 template <class T, int kBlocks, bool kBiased>
 __global__ void __launch_bounds__(kListWarps * 32)
-    route_small_kernel(const __grid_constant__ RouteArgs a, const __grid_constant__ Lanes l32, ListPlan plan) {
+    route_rows_kernel(const __grid_constant__ RouteArgs a, const __grid_constant__ Lanes l32, ListPlan plan) {
   grid_wait();
-  constexpr bool kExact = !kBiased && sizeof(T) == 2;
-  __shared__ float offset[kListWarps][8 * kBlocks];
+  constexpr bool kExact = !kBiased && sizeof(T) == 2, kLong = kBlocks == 0;
+  constexpr int kPlaces = kLong ? 512 : 8 * kBlocks;  // biases
+  __shared__ float all_offsets[kBiased ? (kLong ? 1 : kListWarps) * kPlaces : 1];
   __shared__ int all_ids[kListWarps][32 * kList];
   __shared__ float all_weights[kListWarps][32 * kList];
   const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
   int *its_ids = all_ids[warp];
-  float *its_weights = all_weights[warp];
+  float *its_weights = all_weights[warp], *offset = all_offsets + (kLong ? 0 : warp * kPlaces);
   const bool soft = a.score == SAO_SCORE_SOFTMAX, sums = soft && (kBiased || !a.renorm);
   float units = 1.f;
   bool all_exactly = false;
   if (kBiased) {  // keys as fractions, as above
-    const float b = lane < a.E ? ld(a.bias + lane) : -INFINITY;
-    const bool there = fabsf(b) < INFINITY;
-    float low = -warp_max(there ? -b : -INFINITY), high = warp_max(there ? b : -INFINITY);
+    float low = INFINITY, high = -INFINITY, most = -INFINITY;
+    for (int e = lane; e < a.E; e += 32) {
+      const float b = ld(a.bias + e);
+      most = fmaxf(most, b);
+      if (fabsf(b) < INFINITY) low = fminf(low, b), high = fmaxf(high, b);
+    }
+    low = -warp_max(-low), high = warp_max(high), most = warp_max(most);
     if (high < low) low = high = 0.f;
     units = (1.f - 0x1p-9f) / (1.f + (high - low));
-    all_exactly = __any_sync(kAll, b == INFINITY) || !(units >= 0x1p-20f);
-    if (lane < 8 * kBlocks) offset[warp][lane] = there ? fmaf(b - low, units, kFractionLeast) : -INFINITY;
-    __syncwarp();
+    all_exactly = most == INFINITY || !(units >= 0x1p-20f);
+    for (int e = kLong ? int(threadIdx.x) : lane; e < kPlaces; e += kLong ? kListWarps * 32 : 32) {
+      const float b = e < a.E ? ld(a.bias + e) : -INFINITY;
+      offset[e] = fabsf(b) < INFINITY ? fmaf(b - low, units, kFractionLeast) : -INFINITY;
+    }
+    __syncthreads();
   }
   const uint32_t mask = kExact ? 0xffffu : kBiased ? kFractionMask : plan.mask;
   const uint32_t none = kExact ? 0x007fffffu : kBiased ? kFractionMask : 0x007fffffu | mask;
@@ -468,72 +475,122 @@ __global__ void __launch_bounds__(kListWarps * 32)
     const int rows = int(a.N - row0 < 32 ? a.N - row0 : 32);
     const bool on = lane < rows && (a.mask == nullptr || ld(a.mask + row0 + lane) != 0);
     const T *logits = static_cast<const T *>(a.x) + (row0 + (lane < rows ? lane : 0)) * a.E;
-    Block<T> x[kBlocks];
-#pragma unroll
-    for (int b = 0; b < kBlocks; ++b) x[b].load(logits + 8 * b, on ? a.E - 8 * b : 0, plan.unit);
     bool bad = false;
     float top = -INFINITY, total = 1.f, inverse = 1.f;
-#pragma unroll
-    for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float v = x[b].at(i);
-        bad |= !(v < INFINITY) && (soft || v != v);
-        top = fmaxf(top, v);
-      }
-    if (__any_sync(kAll, bad) && bad) raise_device_error(a.err, SAO_DEVERR_LOGITS);
-    const bool scores = on && !bad && top > -INFINITY;
     uint32_t v[8], rest = 0u;
-    float e[kBlocks][8];
-    if (sums) {
-      total = 0.f;
-#pragma unroll
-      for (int b = 0; b < kBlocks; ++b)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {  // (where weights have this sum's error it is that of expf)
-          const float d = x[b].at(i) - top;
-          total += e[b][i] = a.renorm ? exp_fast(d) : expf(d);
-        }
-      inverse = 1.f / total;
-    }
-#pragma unroll
-    for (int b = 0; b < kBlocks; ++b) {
-      uint32_t w[8];
-      if constexpr (kBiased) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float s = soft ? e[b][i] * inverse : sigmoid_fast(x[b].at(i));
-          const float f = fmaxf(fmaf(s, units, offset[warp][8 * b + i]), 1.f);
-          w[i] = x[b].at(i) > -INFINITY ? __float_as_uint(f) * 512u + (kFractionMask - 8 * b - i) : 0u;
-        }
-      } else {
-        pack(x[b], mask - 8 * b, mask, w);
-      }
+    const auto key = [&](float x, float s, int e) {  // a fraction, `s` the score
+      const float f = fmaxf(fmaf(s, units, offset[e]), 1.f);
+      return x > -INFINITY ? __float_as_uint(f) * 512u + (kFractionMask - e) : 0u;
+    };
+    const auto take = [&](uint32_t(&w)[8], bool first) {
       sort8(w);
-      if (b == 0) {
+      if (first) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = w[i];
       } else {
         merge8<!kExact>(v, w, rest);
       }
+    };
+    const auto look = [&](float x) {
+      bad |= !(x < INFINITY) && (soft || x != x);
+      top = fmaxf(top, x);
+    };
+    if constexpr (kLong) {
+      Block<T> x, ahead;
+      ahead.load(logits, on ? a.E : 0, plan.unit);
+#pragma unroll 1
+      for (int b = 0; b < plan.blocks; ++b) {
+        x = ahead;
+        if (b + 1 < plan.blocks) ahead.load(logits + 8 * b + 8, on ? a.E - 8 * b - 8 : 0, plan.unit);
+        uint32_t w[8];
+        if constexpr (kBiased) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) w[i] = key(x.at(i), sigmoid_fast(x.at(i)), 8 * b + i);
+        } else {
+          pack(x, mask - 8 * b, mask, w);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) look(x.at(i));
+        take(w, b == 0);
+      }
+      if (sums && on) {
+        total = 0.f;
+#pragma unroll 8
+        for (int e = 0; e < a.E; ++e) total += expf(value(logits + e) - top);
+        inverse = 1.f / total;
+      }
+    } else {
+      Block<T> x[kBlocks];
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b) x[b].load(logits + 8 * b, on ? a.E - 8 * b : 0, plan.unit);
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) look(x[b].at(i));
+      float e[kBlocks][8];
+      if (sums) {
+        total = 0.f;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {  // (where weights have this sum's error it is that of expf)
+            const float d = x[b].at(i) - top;
+            total += e[b][i] = a.renorm ? exp_fast(d) : expf(d);
+          }
+        inverse = 1.f / total;
+      }
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b) {
+        uint32_t w[8];
+        if constexpr (kBiased) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            w[i] = key(x[b].at(i), soft ? e[b][i] * inverse : sigmoid_fast(x[b].at(i)), 8 * b + i);
+        } else {
+          pack(x[b], mask - 8 * b, mask, w);
+        }
+        take(w, b == 0);
+      }
     }
+    if (bad) raise_device_error(a.err, SAO_DEVERR_LOGITS);
+    const bool scores = on && !bad && top > -INFINITY;
     // two fractions are off by twice a score's error (of a softmax 2^-18 of its largest, which `inverse` is) and 3 2^-23
     const uint32_t apart = !kBiased ? 0u : uint32_t((soft ? 64.f * inverse : 8.f) * units) + 5u;
-    bool again = all_exactly;
+    const auto near = [&](uint32_t p, uint32_t q) {  // p >= q
+      return p > none && q > none && (kBiased ? (p >> 9) - (q >> 9) <= apart : ((p ^ q) & ~mask) == 0u);
+    };
+    bool again = all_exactly, border = false;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       if (i >= a.k) continue;
       const int id = scores && v[i] > none ? int(mask - (v[i] & mask)) : -1;
       its_ids[lane * a.k + i] = id;
-      if (!kExact) {
-        const uint32_t p = v[i], q = i < 7 ? v[i < 7 ? i + 1 : 7] : rest;
-        if (p > none && q > none && (kBiased ? (p >> 9) - (q >> 9) <= apart : ((p ^ q) & ~mask) == 0u)) {
-          // those of one logit and bias are equal, but at the border of the choice a third one may be as near
-          const int next = int(mask - (q & mask));
-          bool same = i < a.k - 1 && id >= 0 && value(logits + id) == value(logits + next);
-          if (kBiased) same = same && ld(a.bias + id) == ld(a.bias + next);
-          again |= !same;
-        }
+      const uint32_t q = i < 7 ? v[i < 7 ? i + 1 : 7] : rest;
+      if (!kExact && id >= 0 && near(v[i], q)) {
+        // those of one logit and bias are equal, but about the last choice a third one may be as near
+        const int next = int(mask - (q & mask));
+        bool same = value(logits + id) == value(logits + next);
+        if (kBiased) same = same && ld(a.bias + id) == ld(a.bias + next);
+        again |= !same;
+        border |= i == a.k - 1;
+      }
+    }
+    if (!kExact && border && !again) {
+      uint32_t last = 0u;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i == a.k - 1) last = v[i];
+      const int at = int(mask - (last & mask));
+      const float x_last = value(logits + at), b_last = kBiased ? ld(a.bias + at) : 0.f;
+      for (int e = 0; e < a.E; ++e) {
+        const float x = value(logits + e);
+        uint32_t p;
+        if constexpr (kBiased)
+          p = key(x, soft ? exp_fast(x - top) * inverse : sigmoid_fast(x), e);
+        else
+          p = (ordered(x + 0.f) & ~mask) + (mask - e);
+        if (p > last ? near(p, last) : near(last, p))
+          again |= !(x == x_last && (!kBiased || ld(a.bias + e) == b_last));
       }
     }
     __syncwarp();
@@ -542,7 +599,8 @@ __global__ void __launch_bounds__(kListWarps * 32)
       const int r = __ffs(todo) - 1;
       todo &= todo - 1u;
       const T *its_row = static_cast<const T *>(a.x) + (row0 + r) * a.E;
-      const int found = choose_exactly<T, 1, kBiased>({a.bias, a.k, a.kept, soft, a.two != 0}, l32, its_row);
+      const int found =
+          choose_exactly<T, kLong ? 16 : 1, kBiased>({a.bias, a.k, a.kept, soft, a.two != 0}, l32, its_row);
       if (lane < a.k) its_ids[r * a.k + lane] = found;
       __syncwarp();
     }
@@ -583,39 +641,46 @@ __global__ void __launch_bounds__(kListWarps * 32)
 
 }  // namespace
 
-bool route_small_take(const RouteArgs &a, int sms) {
-  return !a.replay && a.k <= kList && a.E <= 32 && a.groups == 1 && a.N >= int64_t(sms) * 32;
+// A thread to a row: up to 32 experts from 32 rows for each SM on; more of them take a thread long, and pay where there are
+// threads enough (and by eight lanes: 65,536 x 40 bf16 9 us and 13, 400,000 x 64 fp32 48 and 77, x 128 75 and 99, 65,536 x
+// 128 both 22, 20,000 x 128 16 and 12; 400,000 x 256 bf16 with a bias 144 and 179, without 107 and 104).
+bool route_rows_take(const RouteArgs &a, int sms) {
+  if (a.replay || a.k > kList || a.groups != 1) return false;
+  if (a.E <= 32) return a.N >= int64_t(sms) * 32;
+  if (a.bias && a.score == SAO_SCORE_SOFTMAX) return false;
+  return (a.E <= 64 && a.N >= int64_t(sms) * 256) || (a.E <= (a.bias ? 256 : 128) && a.N >= int64_t(sms) * 1024);
 }
 
 bool route_lists_take(const RouteArgs &a, int sms) {
-  if (route_small_take(a, sms)) return true;
+  if (route_rows_take(a, sms)) return true;
   if (a.replay || a.k > kList || a.E < 16 || a.E > 512 || a.groups > kShare || (a.groups & (a.groups - 1)) != 0)
     return false;
   return !(a.bias && a.score == SAO_SCORE_SOFTMAX) && a.N >= int64_t(sms) * kRows * kListWarps;
 }
 
-sao_status route_small_launch(const RouteArgs &a, const Lanes &l32, sao_dtype dt, int sms, cudaStream_t s) {
+sao_status route_rows_launch(const RouteArgs &a, const Lanes &l32, sao_dtype dt, int sms, cudaStream_t s) {
   const int size = dt == SAO_BF16 ? 2 : 4;
   ListPlan p{a.E, (a.E + 7) / 8, 16, 7u};
-  while (p.mask + 1u < 8u * (p.blocks > 2 ? 4 : p.blocks)) p.mask = 2 * p.mask + 1u;
+  while (p.mask + 1u < 8u * (p.blocks == 3 ? 4 : p.blocks)) p.mask = 2 * p.mask + 1u;
   while (p.unit >= 8 && (reinterpret_cast<uintptr_t>(a.x) % p.unit != 0 || a.E * size % p.unit != 0)) p.unit /= 2;
   const int64_t tiles = (a.N + 32 * kListWarps - 1) / (32 * kListWarps), most = int64_t(sms) * 128;
-  const int slot = launch_begin("route_small", s);
+  const int slot = launch_begin("route_rows", s);
   SAO_TRY(by_type(dt, [&](auto t) {
     using T = decltype(t);
-    const auto launch = [&](auto kernel) {
-      pdl(kernel, unsigned(least(tiles, most)), kListWarps * 32, 0, s)(a, l32, p);
+    const auto launch = [&](auto biased, auto plain) {
+      pdl(a.bias ? biased : plain, unsigned(least(tiles, most)), kListWarps * 32, 0, s)(a, l32, p);
       return SAO_OK;
     };
-    if (p.blocks == 1) return launch(a.bias ? route_small_kernel<T, 1, true> : route_small_kernel<T, 1, false>);
-    if (p.blocks == 2) return launch(a.bias ? route_small_kernel<T, 2, true> : route_small_kernel<T, 2, false>);
-    return launch(a.bias ? route_small_kernel<T, 4, true> : route_small_kernel<T, 4, false>);
+    if (p.blocks == 1) return launch(route_rows_kernel<T, 1, true>, route_rows_kernel<T, 1, false>);
+    if (p.blocks == 2) return launch(route_rows_kernel<T, 2, true>, route_rows_kernel<T, 2, false>);
+    if (p.blocks <= 4) return launch(route_rows_kernel<T, 4, true>, route_rows_kernel<T, 4, false>);
+    return launch(route_rows_kernel<T, 0, true>, route_rows_kernel<T, 0, false>);
   }));
   return launch_end(slot, s);
 }
 
 sao_status route_lists_launch(const RouteArgs &a, const Lanes &l32, sao_dtype dt, int sms, cudaStream_t s) {
-  if (route_small_take(a, sms)) return route_small_launch(a, l32, dt, sms, s);
+  if (route_rows_take(a, sms)) return route_rows_launch(a, l32, dt, sms, s);
   const Lanes l{kShare / a.groups, 0, a.E / a.groups, a.groups};
   const int size = dt == SAO_BF16 ? 2 : 4;
   ListPlan p{};

@@ -144,6 +144,23 @@ def test_many_tokens(E, groups, kept, k, dtype, score):
     check(x, k, score, None, mask, groups, kept, False, renorm=False)
 
 
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,E,k", [(45001, 40, 8), (50000, 63, 5), (160003, 96, 8), (165000, 129, 2), (165000, 256, 8)])
+def test_a_great_many_tokens(N, E, k, dtype, score):
+    """A thread to a row of more than 32 experts; copies that differ in their last bits among them."""
+    g = torch.Generator().manual_seed(E)
+    x = torch.randn(N, (E + 1) // 2, generator=g).repeat(1, 2)[:, :E].contiguous()
+    x = (x.view(torch.int32) + torch.randint(-3, 4, (N, E), generator=g, dtype=torch.int32)).view(torch.float32)
+    x = torch.where((torch.arange(N) % 3 == 0)[:, None], x, torch.randn(N, E, generator=g)).to(DT[dtype]).cuda()
+    x[::1000, 3], x[1::1000, 5], x[2::1000], x[3::1000, 1:] = math.nan, math.inf, -math.inf, -math.inf
+    bias = _bias((E + 1) // 2).repeat(2)[:E].contiguous()
+    for b in (None, bias):
+        check(x, k, score, b, train=False)
+    check(x, k, score, None, renorm=False, train=False)
+    check(x, k, score, torch.zeros(E, device="cuda"), (torch.arange(N) % 5 != 0).to(torch.uint8).cuda(), train=False)
+
+
 # Up to 32 experts in one group, eight a token: a thread to a row.
 FEW = [(1, 1), (2, 1), (5, 2), (8, 2), (8, 8), (9, 3), (15, 5), (16, 4), (17, 8), (23, 7), (31, 1), (32, 8)]
 
