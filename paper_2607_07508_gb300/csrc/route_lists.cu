@@ -432,8 +432,8 @@ __global__ void __launch_bounds__(kListWarps * 32)
   }
 }
 
-// The same with a thread to a row, nothing to merge or to sum with another lane: of one group, up to 32 experts in
-// registers (kBlocks of eight), or, kBlocks 0 and no softmax with a bias, any number of blocks one after another. Choices
+// The same with a thread to a row, nothing to merge or to sum with another lane: up to 32 experts in registers (kBlocks
+// of eight), or, kBlocks 0, one group and no softmax with a bias, any number of blocks one after another. Choices
 // and weights go through shared memory, so that a warp's 32 rows are stored together.
 // 395,545 x 15 bf16 with a softmax and a bias 23 us, 65,536 x 8 fp32 5 (a warp to a row 105 and 15).
 template <class T, int kBlocks, bool kBiased>
@@ -448,8 +448,10 @@ __global__ void __launch_bounds__(kListWarps * 32)
   const int lane = threadIdx.x & 31, warp = threadIdx.x / 32;
   int *its_ids = all_ids[warp];
   float *its_weights = all_weights[warp], *offset = all_offsets + (kLong ? 0 : warp * kPlaces);
+  __shared__ uint32_t all_worths[kLong ? 1 : kListWarps * 32 * 32];  // of each group, by lanes
+  uint32_t *worths = all_worths + (kLong ? 0 : warp * 32 * 32) + lane;
   const bool soft = a.score == SAO_SCORE_SOFTMAX, sums = soft && (kBiased || !a.renorm);
-  float units = 1.f;
+  float units = 1.f, least = 0.f;
   bool all_exactly = false;
   if (kBiased) {  // keys as fractions, as above
     float low = INFINITY, high = -INFINITY, most = -INFINITY;
@@ -460,6 +462,7 @@ __global__ void __launch_bounds__(kListWarps * 32)
     }
     low = -warp_max(-low), high = warp_max(high), most = warp_max(most);
     if (high < low) low = high = 0.f;
+    least = low;
     units = (1.f - 0x1p-9f) / (1.f + (high - low));
     all_exactly = most == INFINITY || !(units >= 0x1p-20f);
     for (int e = kLong ? int(threadIdx.x) : lane; e < kPlaces; e += kLong ? kListWarps * 32 : 32) {
@@ -478,10 +481,13 @@ __global__ void __launch_bounds__(kListWarps * 32)
     bool bad = false;
     float top = -INFINITY, total = 1.f, inverse = 1.f;
     uint32_t v[8], rest = 0u;
-    const auto key = [&](float x, float s, int e) {  // a fraction, `s` the score
-      const float f = fmaxf(fmaf(s, units, offset[e]), 1.f);
-      return x > -INFINITY ? __float_as_uint(f) * 512u + (kFractionMask - e) : 0u;
+    const auto fraction = [&](float x, float s, int e) {  // of score s; 1: out
+      return x > -INFINITY ? fmaxf(fmaf(s, units, offset[e]), 1.f) : 1.f;
     };
+    const auto key = [&](float x, float s, int e) {
+      return __float_as_uint(fraction(x, s, e)) * 512u + (kFractionMask - e);
+    };
+    bool again = all_exactly;
     const auto take = [&](uint32_t(&w)[8], bool first) {
       sort8(w);
       if (first) {
@@ -539,15 +545,83 @@ __global__ void __launch_bounds__(kListWarps * 32)
           }
         inverse = 1.f / total;
       }
+float f[kBiased ? kBlocks : 1][8];
+      if (kBiased) {
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            f[b][i] = fraction(x[b].at(i), soft ? e[b][i] * inverse : sigmoid_fast(x[b].at(i)), 8 * b + i);
+      }
+      unsigned stay = kAll;  // groups
+      if (a.groups > 1) {
+        const int size = a.E / a.groups;
+        const float out = kBiased ? 1.f : -INFINITY;
+        float b1 = out, b2 = out;
+        int group = 0, inside = 0;
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            if (group == a.groups) continue;
+            const float v = kBiased ? f[kBiased ? b : 0][i] : x[b].at(i) + 0.f;
+            b2 = fmaxf(b2, fminf(b1, v));
+            b1 = fmaxf(b1, v);
+            if (++inside < size) continue;
+            float worth = b1;
+            if (a.two) {
+              if (kBiased)
+                worth = (b1 - kFractionLeast) / units + least +
+                        (b2 > out ? (b2 - kFractionLeast) / units + least : 0.f);
+              else
+                worth = soft ? exp_fast(b1 - top) + exp_fast(b2 - top) : sigmoid_fast(b1) + sigmoid_fast(b2);
+            }
+            worths[32 * group] = b1 > out ? (ordered(worth) & ~31u) | (31u - group) : 0u;
+            b1 = b2 = out, inside = 0, ++group;
+          }
+        uint32_t last = ~0u;
+        for (int c = 0; c < a.kept; ++c) {
+          uint32_t best = 0u;
+          for (int g = 0; g < a.groups; ++g) {
+            const uint32_t u = worths[32 * g];
+            best = max(best, u < last ? u : 0u);
+          }
+          last = best;
+        }
+        uint32_t after = 0u;
+        stay = 0u;
+        for (int g = 0; g < a.groups; ++g) {
+          const uint32_t u = worths[32 * g];
+          stay |= u >= last ? 1u << g : 0u;
+          after = max(after, u < last ? u : 0u);
+        }
+        if (after != 0u && (!kExact || a.two)) {
+          const float p = unordered(last & ~31u), q = unordered(after & ~31u), reach = fabsf(p) + fabsf(q);
+          float error = 0x1p-18f * reach;  // of the five bits
+          if (kBiased && !a.two)
+            error += 0x1p-16f * (soft ? inverse : 0x1p-3f) * units + 0x1p-20f;
+          else if (a.two)
+            error += 0x1p-18f + 0x1p-20f / units + 0x1p-21f * reach + (kBiased && soft ? 0x1p-15f * inverse : 0.f);
+          again |= !(p - q > error);
+        }
+      }
+      int group = 0, inside = 0;
+      const int size = a.groups > 1 ? a.E / a.groups : 64;
 #pragma unroll
       for (int b = 0; b < kBlocks; ++b) {
         uint32_t w[8];
         if constexpr (kBiased) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            w[i] = key(x[b].at(i), soft ? e[b][i] * inverse : sigmoid_fast(x[b].at(i)), 8 * b + i);
+          for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(f[b][i]) * 512u + (kFractionMask - 8 * b - i);
         } else {
           pack(x[b], mask - 8 * b, mask, w);
+        }
+        if (a.groups > 1) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            if (!(stay >> group & 1u)) w[i] = 0u;
+            if (++inside == size) inside = 0, group = group < 31 ? group + 1 : 31;
+          }
         }
         take(w, b == 0);
       }
@@ -559,7 +633,7 @@ __global__ void __launch_bounds__(kListWarps * 32)
     const auto near = [&](uint32_t p, uint32_t q) {  // p >= q
       return p > none && q > none && (kBiased ? (p >> 9) - (q >> 9) <= apart : ((p ^ q) & ~mask) == 0u);
     };
-    bool again = all_exactly, border = false;
+    bool border = false;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       if (i >= a.k) continue;
@@ -600,7 +674,7 @@ __global__ void __launch_bounds__(kListWarps * 32)
       todo &= todo - 1u;
       const T *its_row = static_cast<const T *>(a.x) + (row0 + r) * a.E;
       const int found =
-          choose_exactly<T, kLong ? 16 : 1, kBiased>({a.bias, a.k, a.kept, soft, a.two != 0}, l32, its_row);
+          choose_exactly<T, kLong ? 16 : 2, kBiased>({a.bias, a.k, a.kept, soft, a.two != 0}, l32, its_row);
       if (lane < a.k) its_ids[r * a.k + lane] = found;
       __syncwarp();
     }
@@ -645,8 +719,9 @@ __global__ void __launch_bounds__(kListWarps * 32)
 // threads enough (and by eight lanes: 65,536 x 40 bf16 9 us and 13, 400,000 x 64 fp32 48 and 77, x 128 75 and 99, 65,536 x
 // 128 both 22, 20,000 x 128 16 and 12; 400,000 x 256 bf16 with a bias 144 and 179, without 107 and 104).
 bool route_rows_take(const RouteArgs &a, int sms) {
-  if (a.replay || a.k > kList || a.groups != 1) return false;
+  if (a.replay || a.k > kList) return false;
   if (a.E <= 32) return a.N >= int64_t(sms) * 32;
+  if (a.groups != 1) return false;
   if (a.bias && a.score == SAO_SCORE_SOFTMAX) return false;
   return (a.E <= 64 && a.N >= int64_t(sms) * 256) || (a.E <= (a.bias ? 256 : 128) && a.N >= int64_t(sms) * 1024);
 }

@@ -179,6 +179,25 @@ def test_few_experts(E, k, dtype, score):
 
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("E,groups,kept,k", [(2, 2, 1, 1), (6, 3, 2, 1), (8, 2, 1, 4), (16, 16, 11, 8), (20, 4, 1, 2), (24, 8, 3, 6),
+                                             (27, 9, 4, 5), (28, 4, 2, 3), (30, 5, 2, 8), (32, 4, 3, 8), (32, 32, 9, 8)])
+def test_few_experts_in_groups(E, groups, kept, k, dtype, score):
+    N = 6007
+    g = torch.Generator().manual_seed(E)
+    x = torch.randn(N, (E + 1) // 2, generator=g).repeat(1, 2)[:, :E].contiguous()
+    x = (x.view(torch.int32) + torch.randint(-3, 4, (N, E), generator=g, dtype=torch.int32)).view(torch.float32)
+    x = torch.where((torch.arange(N) % 2 == 0)[:, None], x, torch.randn(N, E, generator=g) * 2).to(DT[dtype]).cuda()
+    x[::50, 1], x[1::50, 0], x[2::50, :E // 2], x[3::50, 1:] = math.nan, math.inf, -math.inf, -math.inf
+    bias = _bias((E + 1) // 2).repeat(2)[:E].contiguous()
+    out = _bias(E, seed=1)
+    out[::3] = -math.inf
+    for b in (None, bias, torch.zeros(E, device="cuda"), out):
+        for two in (False, True):
+            check(x, k, score, b, None, groups, kept, two, renorm=not two, train=False)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("E,k", [(6, 2), (16, 8), (30, 5)])
 def test_few_experts_of_near_and_extraordinary_keys(E, k, dtype, score):
     """Copies that differ in their last bits, few different logits, NaN, infinities, the lowest value, biases that are out."""
