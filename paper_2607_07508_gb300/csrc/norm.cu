@@ -11,8 +11,8 @@
 // 128 of them never leaves a warp. The norm is that of the stored stream, as the backward sees it. Sums are fp32 over at
 // most 64 columns a lane, then by halves; dw's over the rows of a CTA, then over the CTAs in their order.
 //
-// 65,536 x 2,048 bf16: forward 157 us (1.07 GB, 6.8 TB/s), backward 169 (6.3 TB/s) and 2.5 for dw's sum. 16,384 x 6,144
-// with 32-column scales 145 us (0.71 GB, 4.9 TB/s): 31 instructions a column, and few warps to hide the loads behind them.
+// 65,536 x 2,048 bf16: forward 157 us (1.07 GB, 6.8 TB/s), backward 166 (6.5 TB/s) and 2 for dw's sum. 16,384 x 6,144
+// with 32-column scales 115 us (0.71 GB, 6.2 TB/s): instructions next, 25 a column.
 // 20,000 x 6,144 fp32 282 and 338 us (7.0 and 5.8 TB/s). Rows that are no whole vectors, and short ones: norm_tiles.cu.
 #include <cuda_bf16.h>
 #include <cuda_fp8.h>
@@ -368,9 +368,16 @@ __global__ void __launch_bounds__(32 * kSumWarps) norm_dw_kernel(const float *pa
   __shared__ float warp_sum[kSumWarps][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x / 32, c = blockIdx.x * 32 + lane;
   float s = 0.f;
-  if (c < h) {
-#pragma unroll 8
-    for (int p = warp; p < parts; p += kSumWarps) s += ld(partial + int64_t(p) * h + c);
+  constexpr int kBatch = 10;  // parts in flight: all of a warp's where there are two CTAs to an SM
+  for (int p0 = warp; c < h && p0 < parts; p0 += kSumWarps * kBatch) {
+    float v[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int p = p0 + i * kSumWarps;
+      v[i] = p < parts ? ld(partial + int64_t(p) * h + c) : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) s += v[i];
   }
   warp_sum[warp][lane] = s;
   __syncthreads();
