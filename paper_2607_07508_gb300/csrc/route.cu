@@ -8,9 +8,9 @@
 // two of them are nearer to one another than their errors, and not of the same logit and bias, fp64 decides.
 //
 // This form takes what route_lists.cu does not: few tokens, more than eight experts a token or 512 in all, softmax with a
-// bias, any number of groups, replayed choices. It is bound by instructions, 11 to 20 a pick and lane: a warp to a row keeps
-// latency low (7 x 256 in groups 7.7 us with nothing in the caches), and 65,536 x 256 with 10 experts a token take 35
-// us in bf16 and 41 in fp32, 3 to 5 times their bytes at the rate of HBM.
+// bias or replayed choices among more than 32, groups that are no power of two. It is bound by instructions, 11 to 20 a
+// pick and lane: a warp to a row keeps latency low (7 x 256 in groups 7.2 us with nothing in the caches), and 65,536 x
+// 256 with 10 experts a token take 35 us in bf16 and 41 in fp32, 3 to 5 times their bytes at the rate of HBM.
 #include "route_exact.cuh"
 
 namespace sao {

@@ -508,6 +508,9 @@ __global__ void __launch_bounds__(kListWarps * 32)
       for (int b = 0; b < plan.blocks; ++b) {
         x = ahead;
         if (b + 1 < plan.blocks) ahead.load(logits + 8 * b + 8, on ? a.E - 8 * b - 8 : 0, plan.unit);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) look(x.at(i));
+        if (a.replay) continue;
         uint32_t w[8];
         if constexpr (kBiased) {
 #pragma unroll
@@ -515,8 +518,6 @@ __global__ void __launch_bounds__(kListWarps * 32)
         } else {
           pack(x, mask - 8 * b, mask, w);
         }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) look(x.at(i));
         take(w, b == 0);
       }
       if (sums && on) {
@@ -554,7 +555,7 @@ float f[kBiased ? kBlocks : 1][8];
             f[b][i] = fraction(x[b].at(i), soft ? e[b][i] * inverse : sigmoid_fast(x[b].at(i)), 8 * b + i);
       }
       unsigned stay = kAll;  // groups
-      if (a.groups > 1) {
+      if (a.groups > 1 && !a.replay) {
         const int size = a.E / a.groups;
         const float out = kBiased ? 1.f : -INFINITY;
         float b1 = out, b2 = out;
@@ -634,9 +635,20 @@ float f[kBiased ? kBlocks : 1][8];
       return p > none && q > none && (kBiased ? (p >> 9) - (q >> 9) <= apart : ((p ^ q) & ~mask) == 0u);
     };
     bool border = false;
+    if (a.replay) {
+      for (int t = lane; t < rows * a.k; t += 32) {
+        int id = ld(a.ids + row0 * a.k + t);
+        if (id >= a.E) {  // (an error where the row takes part)
+          if (a.mask == nullptr || ld(a.mask + row0 + t / a.k) != 0) raise_device_error(a.err, SAO_DEVERR_EXPERT_ID);
+          id = -1;
+        }
+        its_ids[t] = id;
+      }
+      again = false;
+    }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      if (i >= a.k) continue;
+      if (i >= a.k || a.replay) continue;
       const int id = scores && v[i] > none ? int(mask - (v[i] & mask)) : -1;
       its_ids[lane * a.k + i] = id;
       const uint32_t q = i < 7 ? v[i < 7 ? i + 1 : 7] : rest;
@@ -681,7 +693,7 @@ float f[kBiased ? kBlocks : 1][8];
     float c[8], m = -INFINITY, sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int id = i < a.k ? its_ids[lane * a.k + i] : -1;
+      const int id = i < a.k && scores ? its_ids[lane * a.k + i] : -1;
       c[i] = id >= 0 ? value(logits + id) : -INFINITY;
       m = fmaxf(m, soft ? c[i] : fminf(c[i], 0.f));
     }
@@ -703,10 +715,10 @@ float f[kBiased ? kBlocks : 1][8];
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (i < a.k) its_weights[lane * a.k + i] = its_ids[lane * a.k + i] >= 0 ? a.scale * c[i] : 0.f;
+      if (i < a.k) its_weights[lane * a.k + i] = scores && its_ids[lane * a.k + i] >= 0 ? a.scale * c[i] : 0.f;
     __syncwarp();
     for (int t = lane; t < rows * a.k; t += 32) {
-      a.ids[row0 * a.k + t] = its_ids[t];
+      if (!a.replay) a.ids[row0 * a.k + t] = its_ids[t];
       a.weights[row0 * a.k + t] = its_weights[t];
     }
     __syncwarp();
@@ -719,7 +731,7 @@ float f[kBiased ? kBlocks : 1][8];
 // threads enough (and by eight lanes: 65,536 x 40 bf16 9 us and 13, 400,000 x 64 fp32 48 and 77, x 128 75 and 99, 65,536 x
 // 128 both 22, 20,000 x 128 16 and 12; 400,000 x 256 bf16 with a bias 144 and 179, without 107 and 104).
 bool route_rows_take(const RouteArgs &a, int sms) {
-  if (a.replay || a.k > kList) return false;
+  if (a.k > kList) return false;
   if (a.E <= 32) return a.N >= int64_t(sms) * 32;
   if (a.groups != 1) return false;
   if (a.bias && a.score == SAO_SCORE_SOFTMAX) return false;

@@ -399,21 +399,25 @@ def test_masked_rows(N, dtype, score):
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("renorm", [True, False])
-def test_replay(renorm, dtype, score):
+@pytest.mark.parametrize("N,E,k", [(500, 60, 9), (6001, 60, 8), (6001, 24, 5), (40000, 60, 4), (9001, 6, 8)])
+def test_replay(N, E, k, renorm, dtype, score):
     """A rollout's choices: others than the logits', the same expert twice, some of them missing, rows of none."""
-    x = _logits(500, 60, dtype, seed=12)
+    x = _logits(N, E, dtype, seed=12)
     g = torch.Generator().manual_seed(12)
-    given = torch.randint(-1, 60, (500, 9), generator=g, dtype=torch.int32).cuda()
-    given[7], given[8], given[9, 1:] = -1, 59, -(1 << 31)
-    x[10, 5] = -math.inf
+    k = min(k, E)
+    given = torch.randint(-1, E, (N, k), generator=g, dtype=torch.int32).cuda()
+    given[7], given[8], given[9, 1:] = -1, E - 1, -(1 << 31)
+    x[10, 5], x[11, 3], x[12] = -math.inf, math.nan, -math.inf
     given[10] = 5
-    mask = (torch.rand(500, generator=g) < 0.8).to(torch.uint8).cuda()
-    check(x, 9, score, mask=mask, renorm=renorm, given=given)
+    mask = (torch.rand(N, generator=g) < 0.8).to(torch.uint8).cuda()
+    check(x, k, score, mask=mask, renorm=renorm, given=given)
+    check(x, k, score, mask=None, renorm=renorm, given=given)
 
 
-def test_ids_past_the_last_expert():
-    x = _logits(20, 16)
-    given = torch.full((20, 3), 15, dtype=torch.int32, device="cuda")
+@pytest.mark.parametrize("N", [20, 6000])
+def test_ids_past_the_last_expert(N):
+    x = _logits(N, 16)
+    given = torch.full((N, 3), 15, dtype=torch.int32, device="cuda")
     given[4, 1], given[5, 2] = 16, (1 << 31) - 1
     ids, w = check(x, 3, given=given)
     assert w[4, 1] == 0 and w[5, 2] == 0 and (w[4, [0, 2]] == 1.25).all()
