@@ -260,7 +260,7 @@ __global__ void __launch_bounds__(kListWarps * 32)
     bool again = all_exactly, stays = true;  // again: choose_exactly
     if (l.groups > 1) {
       const bool one = v[0] > none, both = v[1] > none;
-      float worth = -INFINITY;
+      float worth = -INFINITY, x0 = 0.f, x1 = -INFINITY;  // the best two logits, where they are looked at
       if (kBiased) {
         const auto key = [&](uint32_t p) {
           return (__uint_as_float(0x3f800000u | p >> 9) - kFractionLeast) / units + least;
@@ -268,8 +268,26 @@ __global__ void __launch_bounds__(kListWarps * 32)
         if (one) worth = key(v[0]) + (a.two && both ? key(v[1]) : 0.f);
       } else if (a.two) {
         // scores of the two best logits (softmax: times their common sum)
-        const float x0 = one ? value(logits + (mask - (v[0] & mask))) : 0.f;
-        const float x1 = both ? value(logits + (mask - (v[1] & mask))) : -INFINITY;
+        if (one) x0 = value(logits + (mask - (v[0] & mask)));
+        if (both) x1 = value(logits + (mask - (v[1] & mask)));
+        if constexpr (!kExact) {
+          // An fp32 key has lost up to nine bits of its logit, 2^-14 of it: of those that share the second one's leading
+          // bits the list has the first, not the largest. The group's logits themselves tell.
+          const bool blurred = both && near(v[1], v[2]);
+          if (__any_sync(kAll, blurred)) {
+            float b1 = -INFINITY, b2 = -INFINITY;
+            for (int i = 0; i < (blurred ? n : 0); ++i) {
+              const float x = value(from + i);
+              b2 = fmaxf(b2, fminf(b1, x));
+              b1 = fmaxf(b1, x);
+            }
+            for (int o = 1; o < l.share; o <<= 1) {
+              const float c1 = __shfl_xor_sync(kAll, b1, o), c2 = __shfl_xor_sync(kAll, b2, o);
+              merge_two(b1, b2, c1, c2);
+            }
+            if (blurred) x0 = b1, x1 = b2;
+          }
+        }
         if (one) worth = soft ? exp_fast(x0 - top) + exp_fast(x1 - top) : sigmoid_fast(x0) + sigmoid_fast(x1);
       } else if (one) {
         worth = unordered(v[0] & ~mask);
@@ -291,9 +309,13 @@ __global__ void __launch_bounds__(kListWarps * 32)
                             : a.two ? 0x1p-18f
                                     : 0.f;
         const bool doubt = highest > -INFINITY && !(lowest - highest > error);
-        if (__any_sync(kAll, doubt)) {  // ranked again by fp64, a group's best one or two being certain
+        if (__any_sync(kAll, doubt)) {  // ranked again by fp64
+          const bool plain = !kBiased && a.two;  // x0 and x1 are there, and certain
           const int id0 = one ? int(mask - (v[0] & mask)) : -1, id1 = a.two && both ? int(mask - (v[1] & mask)) : -1;
-          const float x0 = id0 >= 0 ? value(logits + id0) : 0.f, x1 = id1 >= 0 ? value(logits + id1) : 0.f;
+          if (!plain) {
+            x0 = id0 >= 0 ? value(logits + id0) : 0.f;
+            x1 = id1 >= 0 ? value(logits + id1) : 0.f;
+          }
           const float b0 = kBiased && id0 >= 0 ? ld(a.bias + id0) : 0.f;
           const float b1 = kBiased && id1 >= 0 ? ld(a.bias + id1) : 0.f;
           const auto term = [&](float x, float b) {
@@ -305,7 +327,7 @@ __global__ void __launch_bounds__(kListWarps * 32)
           // uncertain: keys about the last of those, unless they are of one logit and bias
           const uint32_t least_of = a.two ? v[1] : v[0];
           const float x_of = a.two ? x1 : x0, b_of = a.two ? b1 : b0;
-          const bool unsure = doubt && border && near(least_of, a.two ? v[2] : v[1]);
+          const bool unsure = !plain && doubt && border && near(least_of, a.two ? v[2] : v[1]);
           if (__any_sync(kAll, unsure)) {
             int mixed = 0;
             for (int i = 0; i < (unsure ? n : 0); ++i) {
