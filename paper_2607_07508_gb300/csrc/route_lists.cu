@@ -245,17 +245,26 @@ __global__ void __launch_bounds__(kListWarps * 32)
       merge8<kRest>(v, w, rest);
     };
     for (int o = 1; o < l.share; o <<= 1) join(o);
-    float top = 0.f;  // a reference for exponentials: the row's largest logit, but for the bits that its key has lost
-    if (!kBiased && soft && (!a.renorm || a.two)) {
-      uint32_t first = v[0];
-      for (int o = l.share; o < kShare; o <<= 1) first = max(first, __shfl_xor_sync(kAll, first, o));
-      if (first > none) top = value(logits + (mask - (first & mask)));
-    }
     // whether two keys, the first of them not the smaller one, may be in another order than their exact values
     const auto near = [&](uint32_t p, uint32_t q) {
       if (kExact) return false;
       return p > none && q > none && (kBiased ? (p >> 9) - (q >> 9) <= apart : ((p ^ q) & ~mask) == 0u);
     };
+    float top = 0.f;  // the row's largest logit, for exponentials
+    if (!kBiased && soft && (!a.renorm || a.two)) {
+      uint32_t first = v[0];
+      for (int o = l.share; o < kShare; o <<= 1) first = max(first, __shfl_xor_sync(kAll, first, o));
+      if (first > none) top = value(logits + (mask - (first & mask)));
+      if constexpr (!kExact) {
+        // Of logits that share the leading bits of the first one's key another may be the largest, and of large ones by more
+        // than an exponential has room for.
+        const bool blurred = row_any(near(first, v[1]) || (v[0] != first && near(first, v[0])));
+        if (__any_sync(kAll, blurred)) {
+          for (int i = 0; i < (blurred ? n : 0); ++i) top = fmaxf(top, value(from + i));
+          for (int o = 1; o < kShare; o <<= 1) top = fmaxf(top, __shfl_xor_sync(kAll, top, o));
+        }
+      }
+    }
     const auto exactly = [&](float x, float b) { return kBiased ? sigmoid(double(x)) + double(b) : double(x); };
     bool again = all_exactly, stays = true;  // again: choose_exactly
     if (l.groups > 1) {
