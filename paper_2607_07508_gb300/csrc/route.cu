@@ -157,14 +157,17 @@ __global__ void __launch_bounds__(kWarps * 32, kPer <= 4 ? 5 : kPer <= 8 ? 3 : 1
       good |= 1u << r;
       float key[kPer];
       if (sums) {
-        float sum = 0.f;
+        constexpr int kParts = kPer > 32 ? 2 : 1;  // chains of 32 additions at most
+        float part[kParts] = {};
         if (a.renorm) {
 #pragma unroll
-          for (int i = 0; i < kPer; ++i) sum += key[i] = exp_fast(x[i] - top);
+          for (int i = 0; i < kPer; ++i) part[i % kParts] += key[i] = exp_fast(x[i] - top);
         } else {  // the weights have this sum's error
 #pragma unroll
-          for (int i = 0; i < kPer; ++i) sum += key[i] = expf(x[i] - top);
+          for (int i = 0; i < kPer; ++i) part[i % kParts] += key[i] = expf(x[i] - top);
         }
+        float sum = part[0];
+        if (kParts > 1) sum += part[kParts - 1];
         sum = warp_sum(sum);
         inverse = 1.f / sum;
         if (mine == r) peak = top, total = sum;

@@ -37,6 +37,26 @@ __device__ __forceinline__ F sigmoid(F x) {
   return (x < F(0) ? e : F(1)) / (F(1) + e);
 }
 
+// The sum of exp(x - top) over n logits from p on, in kParts (a power of two) chains of additions. (One chain of 128 was off by
+// 126 units of 2^-24 where each addition is rounded the same way.)
+template <int kParts, class T>
+__device__ __forceinline__ float sum_of_exponentials(const T *p, int n, float top) {
+  float part[kParts] = {};
+  int e = 0;
+#pragma unroll 1
+  for (; e + kParts <= n; e += kParts)
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) part[i] += expf(value(p + e + i) - top);
+#pragma unroll
+  for (int i = 0; i < kParts - 1; ++i)
+    if (e + i < n) part[i] += expf(value(p + e + i) - top);
+#pragma unroll
+  for (int o = kParts / 2; o > 0; o >>= 1)
+#pragma unroll
+    for (int i = 0; i < o; ++i) part[i] += part[i + o];
+  return part[0];
+}
+
 // Over the k lanes from `first` on, a multiple of k (`even`: k is a power of two).
 __device__ __forceinline__ float share_sum(float v, int first, int k, bool even) {
   if (even) {

@@ -450,10 +450,7 @@ __global__ void __launch_bounds__(kListWarps * 32)
     } else if (!soft) {
       w = sigmoid(chosen);
     } else {
-      float sum = 0.f;
-#pragma unroll 4
-      for (int i = 0; i < (scores ? n : 0); ++i) sum += expf(value(from + i) - top);
-      sum = share_sum(sum, 0, kShare, true);
+      const float sum = share_sum(sum_of_exponentials<4>(from, scores ? n : 0, top), 0, kShare, true);
       if (id >= 0) w = expf(chosen - top) / sum;
     }
     if (real && s < a.k) {
@@ -552,9 +549,7 @@ __global__ void __launch_bounds__(kListWarps * 32)
         take(w, b == 0);
       }
       if (sums && on) {
-        total = 0.f;
-#pragma unroll 8
-        for (int e = 0; e < a.E; ++e) total += expf(value(logits + e) - top);
+        total = sum_of_exponentials<8>(logits, a.E, top);
         inverse = 1.f / total;
       }
     } else {
