@@ -768,6 +768,7 @@ sao_status sao_grad_sumsq(const sao_tensor *grads, int32_t count, double *sumsq,
   SAO_RANGE();
   SAO_TRY(check_lists(grads, nullptr, count));
   if (!sumsq) return fail(SAO_ERR_INVALID_ARG, "NULL sumsq");
+  if (!aligned_to(sumsq, 8)) return fail(SAO_ERR_INVALID_ARG, "sumsq is not aligned to its elements");
   Ws w;
   SAO_TRY(take_ws(ws, ws_bytes, grad_ws_bytes(), &w));
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
@@ -782,6 +783,8 @@ sao_status sao_grad_clip(const sao_tensor *grads, const sao_tensor *out, int32_t
   SAO_TRY(check_lists(grads, out, count));
   if (!(max_norm > 0.f)) return fail(SAO_ERR_INVALID_ARG, "max_norm must be positive (%g)", max_norm);
   if (!sumsq || !norm || !coef) return fail(SAO_ERR_INVALID_ARG, "NULL sumsq, norm or coef");
+  if (!aligned_to(sumsq, 8) || !aligned_to(norm, 4) || !aligned_to(coef, 4))
+    return fail(SAO_ERR_INVALID_ARG, "sumsq, norm or coef is not aligned to its elements");
   Ws w;
   SAO_TRY(take_ws(ws, ws_bytes, 0, &w));
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
