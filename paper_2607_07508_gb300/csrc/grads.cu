@@ -253,10 +253,17 @@ __device__ __forceinline__ void chunk_scale(const void *src, void *dst, int n, f
   }
   for (int at = vectors * kPer + threadIdx.x; at < n; at += kClipThreads) {
     const uint32_t w = load_one<kBf16Src_>(src, at).x;
+    if constexpr (kBf16Src_ == kBf16Dst_) {
+      if (coef == 1.f) {
+        if constexpr (kBf16Dst_)
+          static_cast<uint16_t *>(dst)[at] = uint16_t(w);
+        else
+          static_cast<uint32_t *>(dst)[at] = w;
+        continue;
+      }
+    }
     const float f = __uint_as_float(kBf16Src_ ? w << 16 : w) * coef;
-    if (kBf16Src_ && kBf16Dst_ && coef == 1.f)
-      static_cast<uint16_t *>(dst)[at] = uint16_t(w);
-    else if constexpr (kBf16Dst_)
+    if constexpr (kBf16Dst_)
       static_cast<__nv_bfloat16 *>(dst)[at] = __float2bfloat16_rn(f);
     else
       static_cast<float *>(dst)[at] = f;
