@@ -70,23 +70,23 @@ __device__ __forceinline__ int tensor_of(const List<kCap> &l, int64_t c) {
 __device__ __forceinline__ float bf16_low(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_high(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
-// 16 bytes' squares.
+// 16 bytes' squares, in chains of four.
 template <bool kBf16>
 __device__ __forceinline__ float squares(const uint4 &v) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-  float s = 0.f;
+  float s = 0.f, t = 0.f;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     if constexpr (kBf16) {
       const float a = bf16_low(w[i]), b = bf16_high(w[i]);
       s = fmaf(a, a, s);
-      s = fmaf(b, b, s);
+      t = fmaf(b, b, t);
     } else {
       const float a = __uint_as_float(w[i]);
       s = fmaf(a, a, s);
     }
   }
-  return s;
+  return kBf16 ? s + t : s;
 }
 template <bool kBf16>
 __device__ __noinline__ double squares64(uint4 v) {
