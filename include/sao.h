@@ -654,8 +654,9 @@ SAO_API sao_status sao_route_bwd(const void *logits, sao_dtype dt, const uint8_t
  *   y8 [N, h] uint8 (e4m3)            scales as `scaling` says
  * residual and sum are both given or both NULL; rstd and one of y and y8 may be NULL;
  * y8 and scales with scaling != SAO_SCALE_NONE only. sum may be x or residual; the
- * other outputs overlap nothing. Squares are summed in fp32: |sum| up to 2^56. (A row of
- * zeros with eps 0 has no norm: NaN.)
+ * other outputs overlap nothing. Squares are summed in fp32: |sum| up to 2^56; small ones
+ * keep their digits, whatever eps. (A row of zeros with eps 0 has no norm: NaN. An rstd past
+ * fp32's range, of a root mean square below 2^-128, reads +inf.)
  * 1 <= h <= SAO_NORM_MAX_H; eps >= 0 and finite. The forward's workspace: the error word's 256
  * bytes; the backward's: sao_norm_workspace_bytes(N, h), which never falls as one of
  * them grows.

@@ -229,8 +229,8 @@ __device__ __forceinline__ void quantise(Share &share, const NormFwd &a, int64_t
   }
 }
 
-// Shared memory: the tile of the stream, then that of the 8-bit rows if there are any.
-template <class T>
+// Shared memory: the tile of the stream, then that of the 8-bit rows if there are any. kTiny: eps is below kSmall.
+template <class T, bool kTiny>
 __global__ void __launch_bounds__(kThreads, 4) norm_fwd_tiles(const __grid_constant__ NormFwd a, bool w_bf16,
                                                            TilePlan plan) {
   grid_wait();
@@ -259,7 +259,20 @@ __global__ void __launch_bounds__(kThreads, 4) norm_fwd_tiles(const __grid_const
       float s = 0.f;
 #pragma unroll 4
       for (int c = share.column; c < (real ? a.h : 0); c += share.step) s = fmaf(get(row + c), get(row + c), s);
-      const float rstd = 1.f / sqrtf(fmaf(share.sum(s), mean, a.eps));
+      const float square = fmaf(share.sum(s), mean, a.eps);
+      float rstd = 1.f / sqrtf(square);
+      if (kTiny) {
+        const bool small = real && square < kSmall;
+        if (share.warps > 1 ? __syncthreads_or(small) : __any_sync(kAll, small)) {
+          s = 0.f;
+          for (int c = share.column; c < (real ? a.h : 0); c += share.step) {
+            const float v = get(row + c) * kUp;
+            s = fmaf(v, v, s);
+          }
+          s = share.sum(s);
+          if (small) rstd = 1.f / sqrtf(fmaf(s, mean, a.eps * kUp * kUp)) * kUp;
+        }
+      }
       if (real && a.rstd && share.column == 0) a.rstd[row0 + r] = rstd;
       const auto value = [&](int c) { return get(row + c) * rstd * column_weight(a.weight, w_bf16, c); };
       if (a.y8) {
@@ -381,9 +394,12 @@ TilePlan plan_of(int64_t N, int h, int size, int sms) {
 // Shared memory beyond 48 KB is asked for once on each device.
 template <class T>
 sao_status allow(int device, size_t most) {
-  static PerDevice<cudaError_t> forward, backward;
+  static PerDevice<cudaError_t> forward, tiny, backward;
   SAO_CUDA_TRY(forward.get(device, [&] {
-    return cudaFuncSetAttribute(norm_fwd_tiles<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(most));
+    return cudaFuncSetAttribute(norm_fwd_tiles<T, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(most));
+  }));
+  SAO_CUDA_TRY(tiny.get(device, [&] {
+    return cudaFuncSetAttribute(norm_fwd_tiles<T, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(most));
   }));
   SAO_CUDA_TRY(backward.get(device, [&] {
     return cudaFuncSetAttribute(norm_bwd_tiles<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(most));
@@ -404,7 +420,8 @@ sao_status fwd(const NormFwd &a, bool w_bf16, const DeviceInfo &di, cudaStream_t
   const size_t bytes = p.bytes + (a.y8 ? size_t(p.rows) * a.h + 32 : 0);
   const int64_t tiles = (a.N + p.rows - 1) / p.rows, most = int64_t(di.sm_count) * 4 * ctas_of(bytes, 6);
   const int slot = launch_begin("norm_fwd", s);
-  pdl(norm_fwd_tiles<T>, unsigned(tiles < most ? tiles : most), kThreads, bytes, s)(a, w_bf16, p);
+  const auto kernel = a.eps < kSmall ? norm_fwd_tiles<T, true> : norm_fwd_tiles<T, false>;
+  pdl(kernel, unsigned(tiles < most ? tiles : most), kThreads, bytes, s)(a, w_bf16, p);
   return launch_end(slot, s);
 }
 
