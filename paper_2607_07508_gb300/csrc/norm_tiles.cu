@@ -12,6 +12,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <initializer_list>
+
 #include "norm.cuh"
 #include "per_device.h"
 #include "sao_common.cuh"
@@ -229,8 +231,12 @@ __device__ __forceinline__ void quantise(Share &share, const NormFwd &a, int64_t
   }
 }
 
-// Shared memory: the tile of the stream, then that of the 8-bit rows if there are any. kTiny: eps is below kSmall.
-template <class T, bool kTiny>
+// Squares of a row: kLong, in two chains, of rows longer than 32 columns a thread (for all rows this took up to 4 % of a
+// call); kTiny, with an eps below kSmall too.
+enum Squares { kPlain, kLong, kTiny };
+
+// Shared memory: the tile of the stream, then that of the 8-bit rows if there are any.
+template <class T, Squares kSquares>
 __global__ void __launch_bounds__(kThreads, 4) norm_fwd_tiles(const __grid_constant__ NormFwd a, bool w_bf16,
                                                            TilePlan plan) {
   grid_wait();
@@ -256,20 +262,27 @@ __global__ void __launch_bounds__(kThreads, 4) norm_fwd_tiles(const __grid_const
       const int r = r0 + share.row;
       const bool real = r < rows;
       T *row = first + (real ? r : 0) * a.h;
-      float s = 0.f;
+      const int end = real ? a.h : 0;
+      const auto squares = [&](int c, int to, float by) {
+        float s = 0.f;
 #pragma unroll 4
-      for (int c = share.column; c < (real ? a.h : 0); c += share.step) s = fmaf(get(row + c), get(row + c), s);
-      const float square = fmaf(share.sum(s), mean, a.eps);
+        for (; c < to; c += share.step) {
+          const float v = kSquares == kTiny ? get(row + c) * by : get(row + c);
+          s = fmaf(v, v, s);
+        }
+        return s;
+      };
+      const auto all_squares = [&](float by) {
+        if (kSquares == kPlain) return squares(share.column, end, by);
+        const int half = 32 * share.step;
+        return squares(share.column, end < half ? end : half, by) + squares(share.column + half, end, by);
+      };
+      const float square = fmaf(share.sum(all_squares(1.f)), mean, a.eps);
       float rstd = 1.f / sqrtf(square);
-      if (kTiny) {
+      if (kSquares == kTiny) {
         const bool small = real && square < kSmall;
         if (share.warps > 1 ? __syncthreads_or(small) : __any_sync(kAll, small)) {
-          s = 0.f;
-          for (int c = share.column; c < (real ? a.h : 0); c += share.step) {
-            const float v = get(row + c) * kUp;
-            s = fmaf(v, v, s);
-          }
-          s = share.sum(s);
+          const float s = share.sum(all_squares(kUp));
           if (small) rstd = 1.f / sqrtf(fmaf(s, mean, a.eps * kUp * kUp)) * kUp;
         }
       }
@@ -394,12 +407,13 @@ TilePlan plan_of(int64_t N, int h, int size, int sms) {
 // Shared memory beyond 48 KB is asked for once on each device.
 template <class T>
 sao_status allow(int device, size_t most) {
-  static PerDevice<cudaError_t> forward, tiny, backward;
+  static PerDevice<cudaError_t> forward, backward;
   SAO_CUDA_TRY(forward.get(device, [&] {
-    return cudaFuncSetAttribute(norm_fwd_tiles<T, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(most));
-  }));
-  SAO_CUDA_TRY(tiny.get(device, [&] {
-    return cudaFuncSetAttribute(norm_fwd_tiles<T, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(most));
+    for (const auto kernel : {norm_fwd_tiles<T, kPlain>, norm_fwd_tiles<T, kLong>, norm_fwd_tiles<T, kTiny>}) {
+      const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(most));
+      if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
   }));
   SAO_CUDA_TRY(backward.get(device, [&] {
     return cudaFuncSetAttribute(norm_bwd_tiles<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(most));
@@ -420,7 +434,9 @@ sao_status fwd(const NormFwd &a, bool w_bf16, const DeviceInfo &di, cudaStream_t
   const size_t bytes = p.bytes + (a.y8 ? size_t(p.rows) * a.h + 32 : 0);
   const int64_t tiles = (a.N + p.rows - 1) / p.rows, most = int64_t(di.sm_count) * 4 * ctas_of(bytes, 6);
   const int slot = launch_begin("norm_fwd", s);
-  const auto kernel = a.eps < kSmall ? norm_fwd_tiles<T, true> : norm_fwd_tiles<T, false>;
+  const auto kernel = a.eps < kSmall          ? norm_fwd_tiles<T, kTiny>
+                      : a.h > 32 * kThreads ? norm_fwd_tiles<T, kLong>
+                                            : norm_fwd_tiles<T, kPlain>;
   pdl(kernel, unsigned(tiles < most ? tiles : most), kThreads, bytes, s)(a, w_bf16, p);
   return launch_end(slot, s);
 }
