@@ -161,7 +161,7 @@ def _arg(t: Optional[torch.Tensor], dtype, n: int, name: str) -> Optional[int]:
         raise ValueError(f"{name} must have {n} elements, got {t.numel()}")
     if not t.is_cuda:
         raise ValueError("libsao takes CUDA tensors")
-    if not t.is_contiguous():
+    if n != 1 and not t.is_contiguous():
         raise ValueError("libsao takes contiguous tensors")
     return t.data_ptr()
 
@@ -657,9 +657,8 @@ class _Tensor(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("n", ctypes.c_int64), ("dt", ctypes.c_int)]
 
 
-class TensorList:
-    """Gradients, or their clipped copies, as the calls below take them: made once for tensors that stay where
-    they are, which it keeps alive."""
+class _Tensors:
+    """A list of tensors for one call."""
 
     def __init__(self, tensors):
         self.tensors = list(tensors)
@@ -673,6 +672,30 @@ class TensorList:
         return len(self.tensors)
 
 
+class TensorList(_Tensors):
+    """Gradients, or their clipped copies, as the calls below take them: made once for tensors that stay where
+    they are, which it keeps alive, and their memory. A list of which a tensor has since moved to other memory is refused
+    (ValueError): make another one."""
+
+    def __init__(self, tensors):
+        super().__init__(tensors)
+        # the memory that the addresses are of: while it is held, no other tensor can come to lie there
+        self._held = [t.detach() for t in self.tensors]
+        self._place_of = [t.data_ptr for t in self.tensors]
+        self._places = [place() for place in self._place_of]
+
+    def check(self):
+        if [place() for place in self._place_of] != self._places:
+            raise ValueError("a tensor of the list has moved since the list was made")
+
+
+def _listed(tensors) -> _Tensors:
+    if not isinstance(tensors, TensorList):
+        return _Tensors(tensors)
+    tensors.check()
+    return tensors
+
+
 def sao_grad_workspace_bytes() -> int:
     return int(load().sao_grad_workspace_bytes())
 
@@ -684,7 +707,7 @@ def grad_workspace(device=None) -> torch.Tensor:
 
 def sao_grad_sumsq(grads, sumsq, ws, stream=None):
     """grads: a TensorList, or tensors; sumsq fp64."""
-    grads = grads if isinstance(grads, TensorList) else TensorList(grads)
+    grads = _listed(grads)
     _current(grads.device)
     _check(load().sao_grad_sumsq(grads.array, len(grads), _arg(sumsq, _F64, 1, "sumsq"), _ptr(ws), ws.numel(),
                                  _stream(stream)))
@@ -692,8 +715,8 @@ def sao_grad_sumsq(grads, sumsq, ws, stream=None):
 
 def sao_grad_clip(grads, sumsq, max_norm, norm, coef, ws, out=None, stream=None):
     """grads, out: TensorLists, or tensors; out None: in place."""
-    grads = grads if isinstance(grads, TensorList) else TensorList(grads)
-    out = out if out is None or isinstance(out, TensorList) else TensorList(out)
+    grads = _listed(grads)
+    out = None if out is None else _listed(out)
     if out is not None and (len(out) != len(grads) or out.device != grads.device):
         raise ValueError("out must have a tensor for each of grads, on their device")
     _current(grads.device)
