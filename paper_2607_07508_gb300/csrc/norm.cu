@@ -500,7 +500,6 @@ sao_status by_types(sao_dtype dt, sao_dtype w_dt, bool wide, F f) {
 // us, 400,003 x 64 76 and 113, x 128 142 and 118; 4,099 x 515 9 and 13.5, in fp32 16 and 14, 20,001 x 4,099 190
 // and 256, in fp32 270 and 322. Backward: 300,000 x 20 34 and 111, 400,003 x 64 140 and 161, x 77 192 and 171; it
 // reads its tiles three times.)
-constexpr int kShortRow = 64;
 bool fwd_by_tiles(int h, sao_dtype dt, bool wide, bool to8) {
   return h <= kShortRow || (!wide && (to8 || dt == SAO_BF16 || h > 1024));
 }

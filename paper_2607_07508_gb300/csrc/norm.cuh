@@ -68,8 +68,9 @@ size_t norm_ws_bytes(int64_t N, int32_t h);
 sao_status norm_fwd_launch(const NormFwd &a, sao_dtype dt, sao_dtype w_dt, cudaStream_t s);
 sao_status norm_bwd_launch(const NormBwd &a, sao_dtype dt, sao_dtype w_dt, void *ws, size_t ws_bytes, cudaStream_t s);
 
-// norm_tiles.cu: the same for rows of any length, arrays on 16 bytes. The backward has at most
-// `most` CTAs, and writes how many (`parts`) have sums for dw in `partial`.
+// norm_tiles.cu: the same, arrays on 16 bytes; the forward for rows of any length, the backward for those of up to
+// kShortRow. The backward has at most `most` CTAs, and writes how many (`parts`) have sums for dw in `partial`.
+constexpr int kShortRow = 64;
 sao_status norm_fwd_tiles_launch(const NormFwd &a, sao_dtype dt, sao_dtype w_dt, cudaStream_t s);
 sao_status norm_bwd_tiles_launch(const NormBwd &a, sao_dtype dt, sao_dtype w_dt, float *partial, int most, int *parts,
                                  cudaStream_t s);

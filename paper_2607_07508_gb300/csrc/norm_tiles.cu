@@ -24,6 +24,7 @@ namespace {
 using namespace norm;
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
+static_assert(kShortRow < kThreads, "the backward's sums");
 constexpr unsigned kAll = 0xffffffffu;
 
 __device__ __forceinline__ float get(const float *p) { return *p; }
@@ -310,9 +311,8 @@ __global__ void __launch_bounds__(kThreads, 4) norm_fwd_tiles(const __grid_const
   }
 }
 
-// A CTA's sums for dw go to row blockIdx.x of `partial`. Shared memory: the tiles of the stream and of dy, then
-// sums for dw (kThreads / h of each column where rows are shorter than that), then each row's rstd and factor of
-// the stream.
+// Rows shorter than kThreads. A CTA's sums for dw go to row blockIdx.x of `partial`. Shared memory: the tiles of the
+// stream and of dy, then kThreads / h sums of each column for dw, then each row's rstd and factor of the stream.
 template <class T>
 __global__ void __launch_bounds__(kThreads, 4) norm_bwd_tiles(const __grid_constant__ NormBwd a, bool w_bf16,
                                                            TilePlan plan, float *partial) {
@@ -322,14 +322,13 @@ __global__ void __launch_bounds__(kThreads, 4) norm_bwd_tiles(const __grid_const
   constexpr int kVec = 16 / int(sizeof(T));
   T *stream = reinterpret_cast<T *>(shared), *grad = reinterpret_cast<T *>(shared + plan.bytes);
   float *sums = reinterpret_cast<float *>(shared + 2 * plan.bytes);
-  const int parts = a.h < kThreads ? kThreads / a.h : 1;
-  float *row_rstd = sums + (a.h < kThreads ? kThreads : a.h), *row_c = row_rstd + plan.rows;
+  const int parts = kThreads / a.h;
+  float *row_rstd = sums + kThreads, *row_c = row_rstd + plan.rows;
   Share share(plan, slots);
   const float mean = 1.f / float(a.h);
   for (int i = threadIdx.x; i < parts * a.h; i += kThreads) sums[i] = 0.f;
-  const int64_t tiles = (a.N + plan.rows - 1) / plan.rows;
-  for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
-    const int64_t row0 = t * plan.rows, from = row0 * a.h;
+  for (int64_t row0 = int64_t(blockIdx.x) * plan.rows; row0 < a.N; row0 += int64_t(gridDim.x) * plan.rows) {
+    const int64_t from = row0 * a.h;
     const int rows = int(a.N - row0 < plan.rows ? a.N - row0 : plan.rows), count = rows * a.h;
     load_tile<T>(stream, static_cast<const T *>(a.x), from, count);
     load_tile<T>(grad, static_cast<const T *>(a.dy), from, count);
@@ -350,21 +349,13 @@ __global__ void __launch_bounds__(kThreads, 4) norm_bwd_tiles(const __grid_const
       if (real && share.column == 0) row_c[r] = s * mean * rstd;  // times the stream and rstd, below
     }
     __syncthreads();
-    if (partial != nullptr) {  // each thread its columns, or its part of one's rows
-      if (a.h < kThreads) {
-        const int part = threadIdx.x / a.h, c = threadIdx.x - part * a.h;
-        if (part < parts) {
-          float s = 0.f;
-          for (int r = part; r < rows; r += parts)
-            s = fmaf(get(d + r * a.h + c), get(x + r * a.h + c) * row_rstd[r], s);
-          sums[threadIdx.x] += s;
-        }
-      } else {
-        for (int c = threadIdx.x; c < a.h; c += kThreads) {
-          float s = 0.f;
-          for (int r = 0; r < rows; ++r) s = fmaf(get(d + r * a.h + c), get(x + r * a.h + c) * row_rstd[r], s);
-          sums[c] += s;
-        }
+    if (partial != nullptr) {  // each thread its part of a column's rows
+      const int part = threadIdx.x / a.h, c = threadIdx.x - part * a.h;
+      if (part < parts) {
+        float s = 0.f;
+        for (int r = part; r < rows; r += parts)
+          s = fmaf(get(d + r * a.h + c), get(x + r * a.h + c) * row_rstd[r], s);
+        sums[threadIdx.x] += s;
       }
       __syncthreads();
     }
@@ -446,7 +437,7 @@ sao_status bwd(const NormBwd &a, bool w_bf16, const DeviceInfo &di, float *parti
                cudaStream_t s) {
   SAO_TRY(allow<T>(di.device, kMostShared));
   const TilePlan p = plan_of(a.N, a.h, sizeof(T), di.sm_count);
-  const size_t bytes = 2 * size_t(p.bytes) + sizeof(float) * (size_t(a.h < kThreads ? kThreads : a.h) + 2 * p.rows);
+  const size_t bytes = 2 * size_t(p.bytes) + sizeof(float) * (size_t(kThreads) + 2 * p.rows);
   const int64_t tiles = (a.N + p.rows - 1) / p.rows;
   *parts = int(tiles < most ? tiles : most);
   const int slot = launch_begin("norm_bwd", s);
