@@ -498,7 +498,7 @@ sao_status by_types(sao_dtype dt, sao_dtype w_dt, bool wide, F f) {
 // Whether rows go by tiles: short ones, which leave most of a warp idle, and in the forward those that are no
 // whole vectors, but for fp32 ones of up to 1,024 columns. (Forward by tiles and else: 300,000 x 20 bf16 21 and 93
 // us, 400,003 x 64 76 and 113, x 128 142 and 118; 4,099 x 515 9 and 13.5, in fp32 16 and 14, 20,001 x 4,099 190
-// and 256, in fp32 270 and 322. Backward: 300,000 x 20 34 and 111, 400,003 x 64 140 and 161, x 77 192 and 171; it
+// and 256, in fp32 270 and 322. Backward: 300,000 x 20 31 and 111, 400,003 x 64 130 and 161, x 77 192 and 171; it
 // reads its tiles three times.)
 bool fwd_by_tiles(int h, sao_dtype dt, bool wide, bool to8) {
   return h <= kShortRow || (!wide && (to8 || dt == SAO_BF16 || h > 1024));

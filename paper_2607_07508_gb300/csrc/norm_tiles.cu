@@ -4,9 +4,9 @@
 // Rows lie one after another, so a tile of them is one run of memory, whatever their length: it is loaded and stored by
 // vectors (but for its first and last few elements), every lane busy, and only shared memory is read column by column,
 // by a part of a warp, a warp or several to a row. That takes two passes of the forward and three of the backward over
-// shared memory, whose instructions bound it: 300,000 x 20 bf16 21 and 34 us (48 MB each, 2.3 and 1.4 TB/s; a warp to a row
-// 93 and 111), forward of 20,001 x 4,099 190 us (0.66 GB, 3.5 TB/s; single columns from memory 256, vectors that the
-// rows' ends cut 191). Which calls come here: fwd_by_tiles in norm.cu.
+// shared memory, and no load is in flight while a CTA computes: 300,000 x 20 bf16 20 and 31 us (48 MB each, 2.4 and
+// 1.5 TB/s; a warp to a row 93 and 111), forward of 20,001 x 4,099 190 to 202 us (0.66 GB, 3.3 to 3.5 TB/s; single columns
+// from memory 256, vectors that the rows' ends cut 191). Which calls come here: fwd_by_tiles in norm.cu.
 #include <cuda_bf16.h>
 #include <cuda_fp8.h>
 #include <math.h>

@@ -1,12 +1,14 @@
 // Routing to experts, the forms for many tokens: eight lanes take a row, each an eighth of its experts, and keep the
 // largest eight keys of those in a sorted list; three exchanges merge the lists. Or a thread takes a row (below).
 //
-// What bounds it is the number of instructions, minima and maxima above all (their units are 70 to 86 % busy): a list
-// costs 9 of them a key (a block of eight is sorted by a network of 19 exchanges and merged with eight maxima and 12
-// exchanges), where picking one expert after another from a warp's 32 lanes costs 11 to 20 a pick and lane, and nothing
-// is summed or compared over a whole warp. 8 of 65,536 x 128 fp32 22 us (205 instructions a row; by warps 23 us, 300), of
-// 65,536 x 256 bf16 in groups with a bias 38 (410; 57, 675), of 2^20 x 160 bf16 in groups 282 (258; 419, 357): 335 MB of
-// logits at 1.2 TB/s.
+// A list costs 9 minima and maxima a key (a block of eight is sorted by a network of 19 exchanges and merged with eight maxima
+// and 12 exchanges), where picking one expert after another from a warp's 32 lanes costs 11 to 20 instructions a pick and
+// lane, and nothing is summed or compared over a whole warp. 8 of 65,536 x 128 fp32 19 to 22 us (205 instructions a row; by
+// warps 23 us, 300), of 65,536 x 256 bf16 in groups with a bias 38 (410; 57, 675), of 2^20 x 160 bf16 in groups 282 (258;
+// 419, 357): 335 MB of logits at 1.2 TB/s. The last is bound by the units of minima and maxima, 85 % busy. The others
+// are not at a unit's limit: 72 % busy for 128 fp32 experts and 48 % with groups and a bias, with 56 to 62 % of the issue
+// slots used, and a warp waits for its loads first. A block of logits is asked for and used at once, and 72 to 80
+// registers leave 27 to 37 % of the warps to hide that.
 //
 // Keys are packed in 32 bits, the expert's index (inverted: the lower of equal keys is the larger) below
 //   a bf16 logit, which leaves room for it;
@@ -572,7 +574,7 @@ __global__ void __launch_bounds__(kListWarps * 32)
           }
         inverse = 1.f / total;
       }
-float f[kBiased ? kBlocks : 1][8];
+      float f[kBiased ? kBlocks : 1][8];
       if (kBiased) {
 #pragma unroll
         for (int b = 0; b < kBlocks; ++b)

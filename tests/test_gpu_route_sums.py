@@ -19,9 +19,9 @@ U = 2.0 ** -24
 
 @pytest.mark.parametrize("replay", [False, True])
 @pytest.mark.parametrize("first", [0, 60])
-@pytest.mark.parametrize("N,E,k,groups,kept", [(160003, 128, 8, 1, 1), (160003, 100, 3, 1, 1), (9001, 32, 8, 1, 1), (2503, 512, 8, 1, 1),
-                                               (2503, 512, 8, 2, 1), (300, 512, 8, 1, 1), (100, 1024, 32, 1, 1),
-                                               (100, 1020, 9, 17, 3), (100, 1017, 9, 9, 2)])
+@pytest.mark.parametrize("N,E,k,groups,kept", [(160003, 128, 8, 1, 1), (160003, 100, 3, 1, 1), (9001, 32, 8, 1, 1),
+                                               (2503, 512, 8, 1, 1), (2503, 512, 8, 2, 1), (300, 512, 8, 1, 1),
+                                               (100, 1024, 32, 1, 1), (100, 1020, 9, 17, 3), (100, 1017, 9, 9, 2)])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_one_score_and_many_small_ones(dtype, N, E, k, groups, kept, first, replay):
     x = torch.full((N, E), -16.625, dtype=dtype, device="cuda")
