@@ -589,7 +589,7 @@ SAO_API sao_status sao_balance_loss_bwd(const void *logits, sao_dtype dt, const 
  * stay, by their largest key or the sum of their two largest (group_score), equal ones
  * by the lower index, and the choice is among their experts.
  * Choices are those of the exact scores: keys too near one another for fp32 are
- * compared in 64 bits, keys without a bias by their logits. (Softmax and sigmoid keep
+ * compared in 64 bits, whose own rounding decides below that, keys without a bias by their logits. (Softmax and sigmoid keep
  * the logits' order, so experts whose scores are equal in any precision, as of
  * logits past 40, go by the logits too unless there is a bias.)
  * An expert of logit -inf, or of a bias that is -inf or NaN, is never chosen and counts for nothing in

@@ -140,8 +140,8 @@ struct Team {
   }
 };
 
-// kTiny: eps is below kSmall. (As a condition of one kernel this cost every call registers, 16,384 x 6,144 in 8 bits 121 us to
-// 138. Calls with an eps of 0 take up to a tenth longer than others: 65,536 x 2,048 bf16 178 us and 161.)
+// kTiny: eps is below kSmall. (As a condition of one kernel this cost every call registers, 16,384 x 6,144 in 8 bits 121
+// us to 138. Calls with an eps of 0 take up to a tenth longer than others: 65,536 x 2,048 bf16 178 us and 161.)
 template <class T, class WT, int kVec, int kLoads, bool kTiny>
 __global__ void __launch_bounds__(kMaxThreads, kVec < 8 && kVec * kLoads == 32 ? 1 : 2)
     norm_fwd_kernel(NormFwd a, int warps) {

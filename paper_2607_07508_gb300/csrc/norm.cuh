@@ -42,8 +42,8 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   return m;
 }
 
-// Squares of values below 2^-63 lose digits in fp32, and vanish. Where eps does not hide that, a row whose mean of squares
-// (with eps) is below kSmall is summed again, times kUp: its values are then 2^-49 to 2^57.
+// Squares of values below 2^-63 lose digits in fp32, and vanish. Where eps does not hide that, a row whose mean of
+// squares (with eps) is below kSmall is summed again, times kUp: its values are then 2^-49 to 2^57.
 constexpr float kSmall = 0x1p-100f, kUp = 0x1p100f;
 
 // A block's scale and what its values are multiplied by. amax / 448 is the largest e4m3 value's.

@@ -8,12 +8,12 @@
 // two of them are nearer to one another than their errors, and not of the same logit and bias, fp64 decides.
 //
 // This form takes what route_lists.cu does not: few tokens, more than eight experts a token or 512 in all, and, among more
-// than 32 experts, softmax with a bias, groups that are no power of two, and replayed choices (but for up to 64 experts of
-// 256 tokens for each SM and up to 128 of 1,024, which a thread to a row takes). A warp to a row keeps latency low (7 x 256 in
-// groups 7.2 us with nothing in the caches). With many rows its instructions count, 11 to 20 a pick and lane: 65,536 x 256
-// with 10 experts a token take 32 us in bf16 and 38 in fp32, 5 and 3 times their bytes at the rate of HBM, with 70 % of the issue
-// slots used at 34 % of the warps; what a warp waits for first is the result of the instruction before, a chain of reductions
-// over the warp.
+// than 32 experts, softmax with a bias, groups that are no power of two, and replayed choices (which a thread to a row
+// takes among up to 64 experts from 256 tokens for each SM on, among up to 128 from 1,024). A warp to a row keeps latency
+// low: 7 x 256 in groups 7.2 us with nothing in the caches. With many rows its instructions count, 11 to 20 a pick and
+// lane: 65,536 x 256 with 10 experts a token take 32 us in bf16 and 38 in fp32, 6 and 4 times their bytes at the rate of
+// HBM, with 70 % of the issue slots used at 34 % of the warps; a warp waits first for the instruction before, its picks
+// being a chain of reductions.
 #include "route_exact.cuh"
 
 namespace sao {
@@ -390,7 +390,7 @@ sao_status by_count(int E, int per, F f) {
   if (per <= 12) return part(integral_constant<int, 12>());
   if (per <= 16) return part(integral_constant<int, 16>());
   if (per <= 32) return part(integral_constant<int, 32>());
-  return part(integral_constant<int, 64>());  // groups of few lanes: 3 of 341 experts (43 a lane), 9 of 113 (57), 17 of 60 (60)
+  return part(integral_constant<int, 64>());  // groups of few lanes: 3 of 341 experts (43 a lane), 9 of 113 (57), 17 of 60
 }
 
 }  // namespace

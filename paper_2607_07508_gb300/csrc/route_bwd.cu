@@ -4,8 +4,8 @@
 //   sigmoid d x_j = w_j g_j (1 - s_j);  c = sum_j g_j w_j
 //
 // It writes every logit's gradient, most of them 0 (renormalised weights, and sigmoid scores, depend on the chosen
-// logits alone): 2^20 x 160 bf16 91 us, 4.8 TB/s, 1.4 times the bytes at the rate of HBM; 65,536 x 128 fp32 8 to 10 us (34 MB
-// written). A warp waits first for its tile in shared memory and for its choices' ids, weights and gradients: 623,932
+// logits alone): 2^20 x 160 bf16 91 us, 4.8 TB/s, 1.4 times the bytes at the rate of HBM; 65,536 x 128 fp32 8 to 10 us
+// (34 MB written). A warp waits first for its tile in shared memory and for its choices' ids, weights and gradients: 623,932
 // rows of 6 of 16 experts, of little but choices, take 41 us for 65 MB. The gradient of every logit of a softmax takes 21 us
 // for 98,301 x 63 bf16, with 52 % of the issue slots used at 30 % of the warps, which wait for shared memory first.
 #include "bulk.cuh"

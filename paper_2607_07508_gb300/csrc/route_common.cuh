@@ -37,8 +37,8 @@ __device__ __forceinline__ F sigmoid(F x) {
   return (x < F(0) ? e : F(1)) / (F(1) + e);
 }
 
-// The sum of exp(x - top) over n logits from p on, in kParts (a power of two) chains of additions. (One chain of 128 was off by
-// 126 units of 2^-24 where each addition is rounded the same way.)
+// The sum of exp(x - top) over n logits from p on, in kParts (a power of two) chains of additions. (One chain of 128 was
+// off by 126 units of 2^-24 where each addition is rounded the same way.)
 template <int kParts, class T>
 __device__ __forceinline__ float sum_of_exponentials(const T *p, int n, float top) {
   float part[kParts] = {};
